@@ -80,6 +80,7 @@ typedef enum {
 } dessert_status_t;
 
 enum { DESSERT_I8 = 0, DESSERT_F16 = 1 };                       /* vector element type */
+enum { DESSERT_BF16 = 2, DESSERT_F32 = 3 };                     /* with DESSERT_F16: element types beside the search (below) */
 enum { DESSERT_PROJ_RADEMACHER_I8 = 0, DESSERT_PROJ_GAUSSIAN_F32 = 1 };
 
 /* Kernel variants, for cross-checking and measurement (dessert_set_algo). */
@@ -359,6 +360,76 @@ const char *dessert_last_score_kernel(const dessert_index_t *index);
  * for dessert_build_index on this GPU, to set beside the nameplate 8 TB/s.  Both buffers dev, 16-byte aligned. */
 dessert_status_t dessert_probe_mix_bandwidth(const void *in_dev, void *out_dev, size_t out_bytes, int device, void *stream,
                                              int reps, float *ms_per_pass);
+
+/* ---- Beside the search ------------------------------------------------------------------------------------------
+ * The library's vectors come out of a language model, and the documents it finds go into one.  These calls are the
+ * int8 products and the likelihoods at the two ends: dessert_quantize_rows and dessert_scaled_matmul take an encoder's
+ * states through its last layer to the vectors that dessert_build_index and dessert_search take; dessert_token_logprobs
+ * and dessert_head_logprobs give the log probabilities by which candidate documents are ranked again (the sum over a
+ * query's tokens, each given the document) and generated text is scored.
+ * They use only the device and the stream of the index (no built index needed) and are a fixed sequence of kernel
+ * launches: asynchronous, capturable, nothing allocated.  A workspace is scratch of one call at a time: calls that may
+ * overlap (other streams, captured graphs that may replay at the same time) need one each.  Strides count elements
+ * from row to row; what lies between the rows is neither used nor written.  Outputs may not overlap inputs.  Arrays
+ * need the alignment of their elements, workspaces 256 bytes; rows that begin at multiples of 16 bytes are read
+ * faster.  Results are the same bits from call to call. */
+
+/* Rows of numbers to int8 codes with one scale a row, x ~ scale * code:
+ *   DESSERT_SCALE_MAXABS: scale = max |x| / 127 (32-bit float), code = x / scale, in [-127, 127]
+ *   DESSERT_SCALE_UNIT:   code = 127 x / |x| with the Euclidean norm, the vectors of an int8 index; scale = |x| / 127
+ * each code the integer nearest to the quotient of these numbers, ties to even.  A row of zeros (or one whose scale
+ * underflows to zero) has codes 0 and scale 0; a row that holds an infinity or NaN has codes 0 and scale NaN, so that
+ * its products come out as NaN.
+ *   x_dev           dev, [n_rows][n_cols] of dtype (DESSERT_F16, DESSERT_BF16, DESSERT_F32), rows row_stride apart
+ *   out_codes_dev   dev, out, [n_rows][n_cols], no padding
+ *   out_scales_dev  dev, out, [n_rows] */
+enum { DESSERT_SCALE_MAXABS = 0, DESSERT_SCALE_UNIT = 1 };
+dessert_status_t dessert_quantize_rows(const dessert_index_t *index, const void *x_dev, uint32_t dtype, uint64_t n_rows,
+                                       uint32_t n_cols, uint64_t row_stride, int scaling, int8_t *out_codes_dev,
+                                       float *out_scales_dev);
+
+/* Product of int8 matrices with a scale for each row of a (token) and each row of b (channel):
+ *   out[i][j] = float(sum_c a[i][c] * b[j][c]) * (a_scales[i] * b_scales[j]) + bias[j], rounded to out_dtype
+ * The sum is exact in 32-bit integers (n_cols <= 131071); the rest is 32-bit float.
+ *   a_dev, b_dev   dev, [n_rows][n_cols] and [n_channels][n_cols], rows a_stride / b_stride apart
+ *   bias_dev       dev, [n_channels], or NULL
+ *   out_dev        dev, out, [n_rows][n_channels] of out_dtype (DESSERT_F16, DESSERT_BF16, DESSERT_F32), rows out_stride apart
+ *   workspace_dev  dev, dessert_scaled_matmul_workspace_bytes(...) bytes (may be NULL where that is 0) */
+size_t dessert_scaled_matmul_workspace_bytes(const dessert_index_t *index, uint64_t n_rows, uint64_t n_channels, uint32_t n_cols);
+dessert_status_t dessert_scaled_matmul(const dessert_index_t *index, const int8_t *a_dev, uint64_t a_stride,
+                                       const float *a_scales_dev, uint64_t n_rows, const int8_t *b_dev, uint64_t b_stride,
+                                       const float *b_scales_dev, const float *bias_dev, uint64_t n_channels, uint32_t n_cols,
+                                       uint32_t out_dtype, void *out_dev, uint64_t out_stride, void *workspace_dev,
+                                       size_t workspace_bytes);
+
+/* Log probabilities under the softmax of each row of logits l:
+ *   out_logprobs[i]     l[i][tokens[i]] - log sum_j e^l[i][j]
+ *   out_entropy[i]      -sum_j p_j log p_j, in nats
+ *   out_top_ids / out_top_logprobs[i][0 .. n_top)   the n_top most probable entries, descending, ties to the lower id
+ * A token of 0xFFFFFFFF marks a padded position, whose log probability is 0; any other id outside the vocabulary has
+ * -inf.  Logits of -inf are masked out: no probability, never among the alternatives, whose unused slots hold id
+ * 0xFFFFFFFF and -inf.  A row that is masked out altogether has log probability -inf and entropy 0.  A row that holds
+ * +inf or NaN gives NaN and no ids.
+ *   logits_dev   dev, [n_rows][n_vocab] of dtype (DESSERT_F16, DESSERT_BF16, DESSERT_F32), rows row_stride apart
+ *   tokens_dev   dev, [n_rows] u32, or NULL together with out_logprobs_dev
+ *   out_*_dev    dev, out; out_entropy_dev may be NULL, the two top arrays may be with n_top = 0; n_top <= 64
+ *   workspace_dev   dev, dessert_token_logprobs_workspace_bytes(...) bytes (may be NULL where that is 0) */
+size_t dessert_token_logprobs_workspace_bytes(const dessert_index_t *index, uint64_t n_rows, uint32_t n_vocab, uint32_t n_top);
+dessert_status_t dessert_token_logprobs(const dessert_index_t *index, const void *logits_dev, uint32_t dtype, uint64_t n_rows,
+                                        uint32_t n_vocab, uint64_t row_stride, const uint32_t *tokens_dev, uint32_t n_top,
+                                        void *workspace_dev, size_t workspace_bytes, float *out_logprobs_dev,
+                                        float *out_entropy_dev, uint32_t *out_top_ids_dev, float *out_top_logprobs_dev);
+
+/* The same from a model's last states and its vocabulary matrix in int8, without the logits in memory:
+ *   l[i][j] = float(sum_c a[i][c] * vocab[j][c]) * (a_scales[i] * vocab_scales[j])
+ * in 32-bit float, operands as in dessert_scaled_matmul, outputs and tokens as in dessert_token_logprobs. */
+size_t dessert_head_logprobs_workspace_bytes(const dessert_index_t *index, uint64_t n_rows, uint32_t n_vocab, uint32_t n_cols,
+                                             uint32_t n_top);
+dessert_status_t dessert_head_logprobs(const dessert_index_t *index, const int8_t *a_dev, uint64_t a_stride,
+                                       const float *a_scales_dev, uint64_t n_rows, const int8_t *vocab_dev, uint64_t vocab_stride,
+                                       const float *vocab_scales_dev, uint32_t n_vocab, uint32_t n_cols, const uint32_t *tokens_dev,
+                                       uint32_t n_top, void *workspace_dev, size_t workspace_bytes, float *out_logprobs_dev,
+                                       float *out_entropy_dev, uint32_t *out_top_ids_dev, float *out_top_logprobs_dev);
 
 const char *dessert_last_error(void);
 const char *dessert_version(void);

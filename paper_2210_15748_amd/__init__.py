@@ -7,7 +7,8 @@ built (run ``python -m paper_2210_15748_amd.build`` or ``__graft_entry__.build()
 
 Function names mirror the C entry points without the ``dessert_`` prefix:
 ``create`` / ``destroy`` / ``hash`` / ``build_index`` / ``search`` / ``scores`` /
-``set_algo`` / ``set_score_transform`` / ``get_projection`` / ``enable_timing`` / ``get_timing``.
+``set_algo`` / ``set_score_transform`` / ``get_projection`` / ``enable_timing`` / ``get_timing``, and beside the
+search ``quantize_rows`` / ``scaled_matmul`` / ``token_logprobs`` / ``head_logprobs``.
 """
 from __future__ import annotations
 
@@ -23,7 +24,8 @@ _HERE = pathlib.Path(__file__).resolve().parent
 LIB_PATH = _HERE / "libdessert_hip.so"
 
 OK, EINVAL, ENOMEM, EHIP, ESTATE = range(5)
-I8, F16 = 0, 1
+I8, F16, BF16, F32 = 0, 1, 2, 3
+SCALE_MAXABS, SCALE_UNIT = 0, 1
 PROJ_RADEMACHER_I8, PROJ_GAUSSIAN_F32 = 0, 1
 HASH_AUTO, HASH_SCALAR, HASH_MFMA = 0, 1, 2
 SCORE_AUTO, SCORE_BYTECMP, SCORE_MASKLUT = 0, 1, 2
@@ -41,6 +43,9 @@ EXPORTS = [
     "dessert_filter_kmeans_workspace_bytes", "dessert_filter_kmeans",
     "dessert_filter_build", "dessert_filter_workspace_bytes", "dessert_filter_query",
     "dessert_filter_search_workspace_bytes", "dessert_filter_search",
+    "dessert_quantize_rows", "dessert_scaled_matmul_workspace_bytes", "dessert_scaled_matmul",
+    "dessert_token_logprobs_workspace_bytes", "dessert_token_logprobs",
+    "dessert_head_logprobs_workspace_bytes", "dessert_head_logprobs",
     "dessert_enable_timing", "dessert_get_timing", "dessert_probe_read_bandwidth", "dessert_probe_mix_bandwidth", "dessert_last_error",
     "dessert_version",
 ]
@@ -103,6 +108,16 @@ def lib() -> C.CDLL:
     l.dessert_filter_search_workspace_bytes.argtypes = [vp, u32, u64, u32, u32, u32, u32]
     l.dessert_filter_search_workspace_bytes.restype = sz
     l.dessert_filter_search.argtypes = [vp, vp, vp, u32, u32, u32, u32, vp, sz, vp, vp]
+    l.dessert_quantize_rows.argtypes = [vp, vp, u32, u64, u32, u64, C.c_int, vp, vp]
+    l.dessert_scaled_matmul_workspace_bytes.argtypes = [vp, u64, u64, u32]
+    l.dessert_scaled_matmul_workspace_bytes.restype = sz
+    l.dessert_scaled_matmul.argtypes = [vp, vp, u64, vp, u64, vp, u64, vp, vp, u64, u32, u32, vp, u64, vp, sz]
+    l.dessert_token_logprobs_workspace_bytes.argtypes = [vp, u64, u32, u32]
+    l.dessert_token_logprobs_workspace_bytes.restype = sz
+    l.dessert_token_logprobs.argtypes = [vp, vp, u32, u64, u32, u64, vp, u32, vp, sz, vp, vp, vp, vp]
+    l.dessert_head_logprobs_workspace_bytes.argtypes = [vp, u64, u32, u32, u32]
+    l.dessert_head_logprobs_workspace_bytes.restype = sz
+    l.dessert_head_logprobs.argtypes = [vp, vp, u64, vp, u64, vp, u64, vp, u32, u32, vp, u32, vp, sz, vp, vp, vp, vp]
     l.dessert_enable_timing.argtypes = [vp, C.c_int]
     l.dessert_get_timing.argtypes = [vp, u32, C.POINTER(C.c_float)]
     l.dessert_probe_read_bandwidth.argtypes = [vp, sz, C.c_int, vp, C.c_int, C.POINTER(C.c_float)]
@@ -429,6 +444,180 @@ def filter_search(ix: Index, q_vectors: torch.Tensor, q_lengths, filter_probe: i
     _check(lib().dessert_filter_search(ix.handle, q_vectors.data_ptr(), ql.ctypes.data, B, filter_probe, filter_k, k,
                                        workspace.data_ptr(), workspace.numel(), out_ids.data_ptr(), out_scores.data_ptr()))
     return out_ids, out_scores
+
+
+# ---- beside the search ----------------------------------------------------------------------------------------------------
+_FLOAT_TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _lend(ix: Index, made) -> None:
+    """Tensors that were allocated or copied on the current stream go to work on the index's stream: it waits for them, and
+    they are not handed out again before it is done with them."""
+    made = [t for t in made if t is not None]
+    if not made:
+        return
+    current = torch.cuda.current_stream(ix.device)
+    if current.cuda_stream == (ix.cfg.stream or 0):
+        return
+    stream = torch.cuda.ExternalStream(ix.cfg.stream, device=ix.device) if ix.cfg.stream else torch.cuda.default_stream(ix.device)
+    stream.wait_stream(current)
+    for t in made:
+        t.record_stream(stream)
+
+
+def _rows(ix: Index, t: torch.Tensor, name: str, made, *dtypes) -> torch.Tensor:
+    """A matrix on the index's device as the library reads it: elements of a row side by side, rows in order."""
+    if t.dim() != 2 or t.dtype not in dtypes or t.device != ix.device:
+        raise ValueError(f"{name} must be a matrix on {ix.device} of dtype " + " / ".join(str(d) for d in dtypes))
+    n_rows, n_cols = t.shape
+    if (n_cols > 1 and t.stride(1) != 1) or (n_rows > 1 and t.stride(0) < n_cols):
+        t = t.contiguous()
+        made.append(t)
+    return t
+
+
+def _stride(t: torch.Tensor) -> int:
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(ix: Index, t: torch.Tensor, n: int, name: str, made, *dtypes) -> torch.Tensor:
+    if t.dim() != 1 or t.shape[0] != n or t.dtype not in dtypes or t.device != ix.device:
+        raise ValueError(f"{name} must be [{n}] on {ix.device} of dtype " + " / ".join(str(d) for d in dtypes))
+    if n > 1 and t.stride(0) != 1:
+        t = t.contiguous()
+        made.append(t)
+    return t
+
+
+def _output(ix: Index, t: Optional[torch.Tensor], shape, name: str, made, dtype) -> torch.Tensor:
+    if t is None:
+        t = torch.empty(shape, dtype=dtype, device=ix.device)
+        made.append(t)
+        return t
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != ix.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} on {ix.device} of dtype {dtype}")
+    return t
+
+
+def _workspace(ix: Index, workspace: Optional[torch.Tensor], made, nbytes, *sizes):
+    """(address, bytes) of the given workspace, or of one of nbytes(ix, *sizes) bytes"""
+    if workspace is None:
+        need = nbytes(ix, *sizes)
+        if need == 0:
+            return None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=ix.device)
+        made.append(workspace)
+    elif workspace.device != ix.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {ix.device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def quantize_rows(ix: Index, x: torch.Tensor, scaling: int = SCALE_MAXABS, out: Optional[torch.Tensor] = None,
+                  out_scales: Optional[torch.Tensor] = None):
+    """dessert_quantize_rows: x [n, c] of float16 / bfloat16 / float32 (rows may lie apart).  Returns (codes [n, c] int8,
+    scales [n] float32)."""
+    made = []
+    x = _rows(ix, x, "x", made, *_FLOAT_TYPES)
+    n, c = x.shape
+    out = _output(ix, out, (n, c), "out", made, torch.int8)
+    out_scales = _output(ix, out_scales, (n,), "out_scales", made, torch.float32)
+    _lend(ix, made)
+    _check(lib().dessert_quantize_rows(ix.handle, x.data_ptr(), _FLOAT_TYPES[x.dtype], n, c, _stride(x), scaling, out.data_ptr(),
+                                       out_scales.data_ptr()))
+    return out, out_scales
+
+
+def scaled_matmul_workspace_bytes(ix: Index, n_rows: int, n_channels: int, n_cols: int) -> int:
+    return int(lib().dessert_scaled_matmul_workspace_bytes(ix.handle, n_rows, n_channels, n_cols))
+
+
+def scaled_matmul(ix: Index, a: torch.Tensor, a_scales: torch.Tensor, b: torch.Tensor, b_scales: torch.Tensor,
+                  bias: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dessert_scaled_matmul: a [m, k] and b [n, k] int8 (rows may lie apart), scales [m] and [n] float32, bias [n] float32
+    or None.  Returns [m, n] of out_dtype; ``out`` (rows may lie apart) decides the type if given."""
+    made = []
+    a, b = _rows(ix, a, "a", made, torch.int8), _rows(ix, b, "b", made, torch.int8)
+    (m, k), n = a.shape, b.shape[0]
+    if b.shape[1] != k:
+        raise ValueError(f"a has {k} columns, b has {b.shape[1]}")
+    a_scales = _vector(ix, a_scales, m, "a_scales", made, torch.float32)
+    b_scales = _vector(ix, b_scales, n, "b_scales", made, torch.float32)
+    if bias is not None:
+        bias = _vector(ix, bias, n, "bias", made, torch.float32)
+    if out is None:
+        if out_dtype not in _FLOAT_TYPES:
+            raise ValueError("out_dtype must be float16, bfloat16 or float32")
+        out = _output(ix, None, (m, n), "out", made, out_dtype)
+    elif tuple(out.shape) != (m, n) or _rows(ix, out, "out", [], *_FLOAT_TYPES) is not out:
+        raise ValueError(f"out must be [{m}, {n}] with the elements of a row side by side")
+    ws_ptr, ws_bytes = _workspace(ix, workspace, made, scaled_matmul_workspace_bytes, m, n, k)
+    _lend(ix, made)
+    _check(lib().dessert_scaled_matmul(ix.handle, a.data_ptr(), _stride(a), a_scales.data_ptr(), m, b.data_ptr(), _stride(b),
+                                       b_scales.data_ptr(), _ptr(bias), n, k, _FLOAT_TYPES[out.dtype], out.data_ptr(), _stride(out),
+                                       ws_ptr, ws_bytes))
+    return out
+
+
+def _tokens(ix: Index, tokens: Optional[torch.Tensor], n: int, made) -> Optional[torch.Tensor]:
+    if tokens is None:
+        return None
+    if tokens.dtype == torch.int64:     # ids outside 32 bits are ids outside any vocabulary; -1 is the padding mark
+        tokens = torch.where((tokens < -1) | (tokens > 0x7FFFFFFF), 0x7FFFFFFF, tokens).to(torch.int32)
+    return _vector(ix, tokens, n, "tokens", made, torch.int32, torch.uint32)
+
+
+def _logprob_outputs(ix: Index, n: int, n_top: int, tokens, outs, made):
+    o = (None,) * 4 if outs is None else outs
+    return (None if tokens is None else _output(ix, o[0], (n,), "outs[0]", made, torch.float32),
+            _output(ix, o[1], (n,), "outs[1]", made, torch.float32),
+            _output(ix, o[2], (n, n_top), "outs[2]", made, torch.uint32),
+            _output(ix, o[3], (n, n_top), "outs[3]", made, torch.float32))
+
+
+def token_logprobs_workspace_bytes(ix: Index, n_rows: int, n_vocab: int, n_top: int) -> int:
+    return int(lib().dessert_token_logprobs_workspace_bytes(ix.handle, n_rows, n_vocab, n_top))
+
+
+def token_logprobs(ix: Index, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, n_top: int = 0,
+                   workspace: Optional[torch.Tensor] = None, outs=None):
+    """dessert_token_logprobs: logits [n, V] of float16 / bfloat16 / float32 (rows may lie apart), tokens [n] int32 / uint32 /
+    int64 (-1: padded position) or None.  Returns (logprobs [n] or None, entropy [n], top ids [n, n_top] uint32, top logprobs
+    [n, n_top]); ``outs``: the four tensors to write."""
+    made = []
+    logits = _rows(ix, logits, "logits", made, *_FLOAT_TYPES)
+    n, V = logits.shape
+    tokens = _tokens(ix, tokens, n, made)
+    o = _logprob_outputs(ix, n, n_top, tokens, outs, made)
+    ws_ptr, ws_bytes = _workspace(ix, workspace, made, token_logprobs_workspace_bytes, n, V, n_top)
+    _lend(ix, made)
+    _check(lib().dessert_token_logprobs(ix.handle, logits.data_ptr(), _FLOAT_TYPES[logits.dtype], n, V, _stride(logits), _ptr(tokens),
+                                        n_top, ws_ptr, ws_bytes, *map(_ptr, o)))
+    return o
+
+
+def head_logprobs_workspace_bytes(ix: Index, n_rows: int, n_vocab: int, n_cols: int, n_top: int) -> int:
+    return int(lib().dessert_head_logprobs_workspace_bytes(ix.handle, n_rows, n_vocab, n_cols, n_top))
+
+
+def head_logprobs(ix: Index, a: torch.Tensor, a_scales: torch.Tensor, vocab: torch.Tensor, vocab_scales: torch.Tensor,
+                  tokens: Optional[torch.Tensor] = None, n_top: int = 0, workspace: Optional[torch.Tensor] = None, outs=None):
+    """dessert_head_logprobs: states a [n, k] and vocabulary matrix [V, k] int8 with scales [n] and [V] float32; the rest as
+    token_logprobs."""
+    made = []
+    a, vocab = _rows(ix, a, "a", made, torch.int8), _rows(ix, vocab, "vocab", made, torch.int8)
+    (n, k), V = a.shape, vocab.shape[0]
+    if vocab.shape[1] != k:
+        raise ValueError(f"a has {k} columns, vocab has {vocab.shape[1]}")
+    a_scales = _vector(ix, a_scales, n, "a_scales", made, torch.float32)
+    vocab_scales = _vector(ix, vocab_scales, V, "vocab_scales", made, torch.float32)
+    tokens = _tokens(ix, tokens, n, made)
+    o = _logprob_outputs(ix, n, n_top, tokens, outs, made)
+    ws_ptr, ws_bytes = _workspace(ix, workspace, made, head_logprobs_workspace_bytes, n, V, k, n_top)
+    _lend(ix, made)
+    _check(lib().dessert_head_logprobs(ix.handle, a.data_ptr(), _stride(a), a_scales.data_ptr(), n, vocab.data_ptr(), _stride(vocab),
+                                       vocab_scales.data_ptr(), V, k, _ptr(tokens), n_top, ws_ptr, ws_bytes, *map(_ptr, o)))
+    return o
 
 
 def enable_timing(ix: Index, enable=True) -> None:

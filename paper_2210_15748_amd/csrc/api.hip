@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "kernels.hpp"
+#include "number_formats.hpp"
 
 using namespace dessert;
 
@@ -1288,6 +1289,199 @@ dessert_status_t dessert_get_timing(dessert_index_t* ix, uint32_t calls_back, fl
     if (ts.score) HIP_TRY(hipEventElapsedTime(&ms[1], ts.ev[1], ts.ev[2]));
     if (ts.topk) HIP_TRY(hipEventElapsedTime(&ms[2], ts.ev[2], ts.ev[3]));
     HIP_TRY(hipEventElapsedTime(&ms[3], ts.ev[0], ts.ev[4]));
+    return DESSERT_OK;
+}
+
+// ---- beside the search ---------------------------------------------------------------------------------------------------
+
+namespace {
+bool float_type(uint32_t dtype) { return dtype == DESSERT_F16 || dtype == DESSERT_BF16 || dtype == DESSERT_F32; }
+size_t type_size(uint32_t dtype) { return dtype == DESSERT_F32 ? 4 : 2; }
+// Rows and vocabulary entries per call, and the elements that a row may lie apart: products of them stay far below 2^64.
+constexpr uint64_t MAX_ROWS = 1ull << 31, MAX_STRIDE = 1ull << 31;
+constexpr uint32_t MAX_COLS = (1u << 30);
+constexpr uint32_t MAX_PRODUCT_COLS = 131071;   // 128 * 128 * 131071 < 2^31
+
+// The operands of an int8 product (dessert_scaled_matmul, dessert_head_logprobs).
+dessert_status_t check_product(const int8_t* a, uint64_t a_stride, const float* a_scales, uint64_t m, const int8_t* b, uint64_t b_stride,
+                               const float* b_scales, uint64_t n, uint32_t k) {
+    if (k == 0 || k > MAX_PRODUCT_COLS) return fail(DESSERT_EINVAL, "n_cols must be in 1..%u (32-bit sums)", MAX_PRODUCT_COLS);
+    if (m >= MAX_ROWS || n >= MAX_ROWS) return fail(DESSERT_EINVAL, "at most 2^31-1 rows of either operand");
+    if ((m && (!a || !a_scales)) || (n && (!b || !b_scales))) return fail(DESSERT_EINVAL, "NULL argument");
+    if (a_stride < k || b_stride < k || a_stride >= MAX_STRIDE || b_stride >= MAX_STRIDE)
+        return fail(DESSERT_EINVAL, "rows of %u columns need strides of %u to 2^31-1", k, k);
+    if ((uintptr_t)a_scales % 4 || (uintptr_t)b_scales % 4) return fail(DESSERT_EINVAL, "scales must be 4-byte aligned");
+    return DESSERT_OK;
+}
+
+dessert_status_t check_workspace(const void* workspace, size_t given, size_t need) {
+    if (need == 0) return DESSERT_OK;
+    if (!workspace) return fail(DESSERT_EINVAL, "workspace_dev is NULL");
+    if ((uintptr_t)workspace % 256) return fail(DESSERT_EINVAL, "workspace_dev must be 256-byte aligned");
+    if (given < need) return fail(DESSERT_EINVAL, "workspace too small: %zu bytes given, %zu needed", given, need);
+    return DESSERT_OK;
+}
+
+// What a log-probability call writes.
+dessert_status_t check_logprob_outputs(uint64_t rows, uint32_t vocab, const uint32_t* tokens, const float* logprobs, const float* entropy,
+                                       uint32_t n_top, const uint32_t* top_ids, const float* top_logprobs) {
+    if (vocab == 0 || vocab > MAX_COLS) return fail(DESSERT_EINVAL, "n_vocab must be in 1..2^30");
+    if (rows >= MAX_ROWS) return fail(DESSERT_EINVAL, "at most 2^31-1 rows");
+    if (n_top > LOGPROB_MAX_TOP) return fail(DESSERT_EINVAL, "n_top must be at most %u", LOGPROB_MAX_TOP);
+    if (rows == 0) return DESSERT_OK;
+    if ((uintptr_t)tokens % 4 || (uintptr_t)logprobs % 4 || (uintptr_t)top_ids % 4 || (uintptr_t)top_logprobs % 4 || (uintptr_t)entropy % 4)
+        return fail(DESSERT_EINVAL, "tokens and outputs must be aligned to their elements");
+    if ((tokens == nullptr) != (logprobs == nullptr))
+        return fail(DESSERT_EINVAL, "tokens_dev and out_logprobs_dev go together: both or neither");
+    if (n_top && (!top_ids || !top_logprobs)) return fail(DESSERT_EINVAL, "out_top_ids_dev / out_top_logprobs_dev is NULL with n_top > 0");
+    return DESSERT_OK;
+}
+}  // namespace
+
+dessert_status_t dessert_quantize_rows(const dessert_index_t* ix, const void* x_dev, uint32_t dtype, uint64_t n_rows, uint32_t n_cols,
+                                       uint64_t row_stride, int scaling, int8_t* out_codes_dev, float* out_scales_dev) {
+    if (!float_type(dtype)) return fail(DESSERT_EINVAL, "dtype must be DESSERT_F16, DESSERT_BF16 or DESSERT_F32");
+    if (scaling != DESSERT_SCALE_MAXABS && scaling != DESSERT_SCALE_UNIT) return fail(DESSERT_EINVAL, "unknown scaling %d", scaling);
+    if (n_cols == 0 || n_cols > MAX_COLS) return fail(DESSERT_EINVAL, "n_cols must be in 1..2^30");
+    if (n_rows >= MAX_ROWS) return fail(DESSERT_EINVAL, "at most 2^31-1 rows");
+    if (n_rows && (!x_dev || !out_codes_dev || !out_scales_dev)) return fail(DESSERT_EINVAL, "NULL argument");
+    if (row_stride < n_cols || row_stride >= MAX_STRIDE) return fail(DESSERT_EINVAL, "rows of %u columns need a stride of %u to 2^31-1", n_cols, n_cols);
+    if ((uintptr_t)x_dev % type_size(dtype) || (uintptr_t)out_scales_dev % 4)
+        return fail(DESSERT_EINVAL, "x_dev and out_scales_dev must be aligned to their elements");
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    if (n_rows == 0) return DESSERT_OK;
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    HIP_TRY(launch_quantize_rows(x_dev, dtype, n_rows, n_cols, row_stride, scaling == DESSERT_SCALE_UNIT, out_codes_dev, out_scales_dev,
+                                 ix->stream));
+    return DESSERT_OK;
+}
+
+size_t dessert_scaled_matmul_workspace_bytes(const dessert_index_t* ix, uint64_t n_rows, uint64_t n_channels, uint32_t n_cols) {
+    if (!ix) return 0;
+    return scaled_matmul_workspace(n_rows, n_channels, n_cols);
+}
+
+dessert_status_t dessert_scaled_matmul(const dessert_index_t* ix, const int8_t* a_dev, uint64_t a_stride, const float* a_scales_dev,
+                                       uint64_t n_rows, const int8_t* b_dev, uint64_t b_stride, const float* b_scales_dev,
+                                       const float* bias_dev, uint64_t n_channels, uint32_t n_cols, uint32_t out_dtype, void* out_dev,
+                                       uint64_t out_stride, void* workspace_dev, size_t workspace_bytes) {
+    if (!float_type(out_dtype)) return fail(DESSERT_EINVAL, "out_dtype must be DESSERT_F16, DESSERT_BF16 or DESSERT_F32");
+    dessert_status_t st = check_product(a_dev, a_stride, a_scales_dev, n_rows, b_dev, b_stride, b_scales_dev, n_channels, n_cols);
+    if (st != DESSERT_OK) return st;
+    if (n_rows && n_channels && !out_dev) return fail(DESSERT_EINVAL, "out_dev is NULL");
+    if (out_stride < n_channels || out_stride >= MAX_STRIDE)
+        return fail(DESSERT_EINVAL, "out_stride must be n_channels to 2^31-1");
+    if ((uintptr_t)out_dev % type_size(out_dtype) || (uintptr_t)bias_dev % 4)
+        return fail(DESSERT_EINVAL, "out_dev and bias_dev must be aligned to their elements");
+    if (((n_rows + 63) / 64) * ((n_channels + 63) / 64) > 0x7FFFFFFFull) return fail(DESSERT_EINVAL, "product too large for one launch");
+    st = check_workspace(workspace_dev, workspace_bytes, scaled_matmul_workspace(n_rows, n_channels, n_cols));
+    if (st != DESSERT_OK) return st;
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    if (n_rows == 0 || n_channels == 0) return DESSERT_OK;
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    MatmulArgs g{};
+    g.a = a_dev; g.lda = a_stride; g.sa = a_scales_dev; g.m = n_rows;
+    g.b = b_dev; g.ldb = b_stride; g.sb = b_scales_dev; g.bias = bias_dev; g.n = n_channels;
+    g.k = n_cols; g.out = out_dev; g.ldo = out_stride;
+    HIP_TRY(launch_scaled_matmul(g, out_dtype, workspace_dev, ix->stream));
+    return DESSERT_OK;
+}
+
+size_t dessert_token_logprobs_workspace_bytes(const dessert_index_t* ix, uint64_t n_rows, uint32_t n_vocab, uint32_t n_top) {
+    if (!ix || n_vocab == 0 || n_vocab > MAX_COLS || n_rows == 0 || n_rows >= MAX_ROWS) return 0;
+    return logprob_plan(n_rows, n_vocab, n_top).bytes;
+}
+
+dessert_status_t dessert_token_logprobs(const dessert_index_t* ix, const void* logits_dev, uint32_t dtype, uint64_t n_rows,
+                                        uint32_t n_vocab, uint64_t row_stride, const uint32_t* tokens_dev, uint32_t n_top,
+                                        void* workspace_dev, size_t workspace_bytes, float* out_logprobs_dev, float* out_entropy_dev,
+                                        uint32_t* out_top_ids_dev, float* out_top_logprobs_dev) {
+    if (!float_type(dtype)) return fail(DESSERT_EINVAL, "dtype must be DESSERT_F16, DESSERT_BF16 or DESSERT_F32");
+    dessert_status_t st = check_logprob_outputs(n_rows, n_vocab, tokens_dev, out_logprobs_dev, out_entropy_dev, n_top, out_top_ids_dev, out_top_logprobs_dev);
+    if (st != DESSERT_OK) return st;
+    if (n_rows && !logits_dev) return fail(DESSERT_EINVAL, "logits_dev is NULL");
+    if ((uintptr_t)logits_dev % type_size(dtype)) return fail(DESSERT_EINVAL, "logits_dev must be aligned to its elements");
+    if (row_stride < n_vocab || row_stride >= MAX_STRIDE) return fail(DESSERT_EINVAL, "row_stride must be n_vocab to 2^31-1");
+    const LogprobPlan p = logprob_plan(n_rows ? n_rows : 1, n_vocab, n_top);
+    st = check_workspace(workspace_dev, workspace_bytes, n_rows ? p.bytes : 0);
+    if (st != DESSERT_OK) return st;
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    if (n_rows == 0) return DESSERT_OK;
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    LogprobArgs g{};
+    g.logits = logits_dev; g.stride = row_stride; g.rows = n_rows; g.vocab = n_vocab; g.n_top = n_top;
+    g.tokens = tokens_dev; g.logprobs = out_logprobs_dev; g.entropy = out_entropy_dev;
+    g.top_ids = out_top_ids_dev; g.top_logprobs = out_top_logprobs_dev;
+    HIP_TRY(launch_token_logprobs(g, dtype, p, workspace_dev, ix->stream));
+    return DESSERT_OK;
+}
+
+namespace {
+// The head form goes through the rows in turns whose 32-bit logits fit this much: they then stay in the 256 MB cache
+// between the product that writes them and the pass that reads them.
+constexpr size_t HEAD_LOGITS_BYTES = 96u << 20;
+struct HeadPlan {
+    uint64_t rows;     // of a turn
+    uint64_t stride;   // floats from row to row
+    LogprobPlan pass;
+    size_t logits_bytes, pass_bytes, bytes;
+};
+HeadPlan head_plan(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
+    HeadPlan h{};
+    h.stride = ((uint64_t)vocab + 31) / 32 * 32;
+    h.rows = HEAD_LOGITS_BYTES / 4 / h.stride;
+    h.rows = h.rows < 256 ? 256 : h.rows / 256 * 256;
+    if (h.rows > rows) h.rows = rows;
+    h.pass = logprob_plan(h.rows, vocab, n_top);
+    h.logits_bytes = align_up((size_t)h.rows * h.stride * 4, 256);
+    h.pass_bytes = align_up(h.pass.bytes, 256);
+    h.bytes = h.logits_bytes + h.pass_bytes + scaled_matmul_workspace(h.rows, vocab, k);
+    return h;
+}
+}  // namespace
+
+size_t dessert_head_logprobs_workspace_bytes(const dessert_index_t* ix, uint64_t n_rows, uint32_t n_vocab, uint32_t n_cols, uint32_t n_top) {
+    if (!ix || n_vocab == 0 || n_vocab > MAX_COLS || n_rows == 0 || n_rows >= MAX_ROWS) return 0;
+    return head_plan(n_rows, n_vocab, n_cols, n_top).bytes;
+}
+
+dessert_status_t dessert_head_logprobs(const dessert_index_t* ix, const int8_t* a_dev, uint64_t a_stride, const float* a_scales_dev,
+                                       uint64_t n_rows, const int8_t* vocab_dev, uint64_t vocab_stride, const float* vocab_scales_dev,
+                                       uint32_t n_vocab, uint32_t n_cols, const uint32_t* tokens_dev, uint32_t n_top, void* workspace_dev,
+                                       size_t workspace_bytes, float* out_logprobs_dev, float* out_entropy_dev, uint32_t* out_top_ids_dev,
+                                       float* out_top_logprobs_dev) {
+    dessert_status_t st = check_logprob_outputs(n_rows, n_vocab, tokens_dev, out_logprobs_dev, out_entropy_dev, n_top, out_top_ids_dev, out_top_logprobs_dev);
+    if (st != DESSERT_OK) return st;
+    st = check_product(a_dev, a_stride, a_scales_dev, n_rows, vocab_dev, vocab_stride, vocab_scales_dev, n_vocab, n_cols);
+    if (st != DESSERT_OK) return st;
+    const HeadPlan h = head_plan(n_rows ? n_rows : 1, n_vocab, n_cols, n_top);
+    st = check_workspace(workspace_dev, workspace_bytes, n_rows ? h.bytes : 0);
+    if (st != DESSERT_OK) return st;
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    if (n_rows == 0) return DESSERT_OK;
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    char* ws = (char*)workspace_dev;
+    for (uint64_t r = 0; r < n_rows; r += h.rows) {
+        const uint64_t rows = n_rows - r < h.rows ? n_rows - r : h.rows;
+        MatmulArgs g{};
+        g.a = a_dev + r * a_stride; g.lda = a_stride; g.sa = a_scales_dev + r; g.m = rows;
+        g.b = vocab_dev; g.ldb = vocab_stride; g.sb = vocab_scales_dev; g.n = n_vocab;
+        g.k = n_cols; g.out = ws; g.ldo = h.stride;
+        HIP_TRY(launch_scaled_matmul(g, TYPE_F32, ws + h.logits_bytes + h.pass_bytes, ix->stream));
+        LogprobArgs p{};
+        p.logits = ws; p.stride = h.stride; p.rows = rows; p.vocab = n_vocab; p.n_top = n_top;
+        p.tokens = tokens_dev ? tokens_dev + r : nullptr;
+        p.logprobs = out_logprobs_dev ? out_logprobs_dev + r : nullptr;
+        p.entropy = out_entropy_dev ? out_entropy_dev + r : nullptr;
+        p.top_ids = n_top ? out_top_ids_dev + r * n_top : nullptr;
+        p.top_logprobs = n_top ? out_top_logprobs_dev + r * n_top : nullptr;
+        // the last turn's fewer rows go by the same plan, whose parts fit
+        HIP_TRY(launch_token_logprobs(p, TYPE_F32, h.pass, ws + h.logits_bytes, ix->stream));
+    }
     return DESSERT_OK;
 }
 

@@ -239,4 +239,46 @@ hipError_t launch_topk_lists(const uint64_t* lists, uint64_t list_stride, const 
                              uint32_t k, uint32_t max_score, uint64_t max_id, const FilterHistPlan* hp, uint32_t* out_ids,
                              int32_t* out_scores, bool ordered, hipStream_t stream, uint32_t* emit_plan = nullptr);
 
+// ---- beside the search: int8 rows, scaled int8 products, log probabilities -----------------
+// rows [rows][cols] of dtype (as in dessert.h: F16, BF16, F32), `stride` elements apart, to codes [rows][cols] and scales [rows]
+hipError_t launch_quantize_rows(const void* x, uint32_t dtype, uint64_t rows, uint32_t cols, uint64_t stride, bool unit, int8_t* codes,
+                                float* scales, hipStream_t stream);
+struct MatmulArgs {
+    const int8_t* a;    // [m] rows of k, lda apart
+    uint64_t lda;
+    const float* sa;    // [m]
+    uint64_t m;
+    const int8_t* b;    // [n] rows of k, ldb apart
+    uint64_t ldb;
+    const float* sb;    // [n]
+    const float* bias;  // [n] or nullptr
+    uint64_t n;
+    uint32_t k;
+    void* out;          // [m] rows of n, ldo apart
+    uint64_t ldo;
+    uint32_t tiles_m, tiles_n;   // set by the launch
+};
+size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k);
+hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void* workspace, hipStream_t stream);
+struct LogprobArgs {
+    const void* logits;       // [rows] rows of vocab, stride apart
+    uint64_t stride, rows;
+    uint32_t vocab, n_top;
+    const uint32_t* tokens;   // [rows] or nullptr
+    float* logprobs;          // [rows] (with tokens)
+    float* entropy;           // [rows] or nullptr
+    uint32_t* top_ids;        // [rows][n_top]
+    float* top_logprobs;      // [rows][n_top]
+    uint32_t splits, segment; // of a row over workgroups; set by the launch, as the parts are
+    float* part_sums;
+    uint64_t* part_keys;
+};
+constexpr uint32_t LOGPROB_MAX_TOP = 64;   // one entry of the list a lane
+struct LogprobPlan {
+    uint32_t splits, segment;
+    size_t sums_bytes, bytes;   // workspace: of the sums, and altogether
+};
+LogprobPlan logprob_plan(uint64_t rows, uint32_t vocab, uint32_t n_top);
+hipError_t launch_token_logprobs(LogprobArgs g, uint32_t dtype, const LogprobPlan& p, void* workspace, hipStream_t stream);
+
 }  // namespace dessert
