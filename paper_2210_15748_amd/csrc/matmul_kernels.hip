@@ -2,6 +2,8 @@
 //     out[i][j] = T( float(sum_c a[i][c] * b[j][c]) * (sa[i] * sb[j]) + bias[j] )
 // The sums are exact in int32 whatever their order, so any split of the columns gives the same bits.  Both operands lie with
 // their columns side by side, which is the order that v_mfma_i32_16x16x64_i8 takes: 16 bytes of one row per lane.
+#include <type_traits>
+
 #include "kernels.hpp"
 #include "number_formats.hpp"
 
@@ -11,6 +13,25 @@ namespace {
 
 constexpr int STEP = 128;   // columns (bytes) of a row per round of the tile kernel: one line of 128 bytes
 
+// ---- tiles ------------------------------------------------------------------------------------------------------------------
+// A workgroup of WM x WN waves goes through tiles of TM tokens x TN channels, 128 columns a step.  A step's rows lie in LDS, 128
+// bytes each, double-buffered: while the waves multiply one step, the next one is on its way, across the border between two tiles
+// too, so that a tile's results leave while the next tile's first columns arrive.  Rows whose bytes are 16-byte aligned (ALIGNED)
+// go from memory to LDS directly; others through registers.
+//
+// The buffers are four arrays by name and the two steps of a round stand one after the other in the code: the compiler then knows
+// that reads of one buffer do not wait for what is arriving in the other.  The products appear once per buffer and nowhere else
+// (no tail outside the loop): a second copy of the accumulators would not fit the registers.
+template <int TM_, int TN_, int WM_, int WN_, bool ALIGNED_>
+struct Tile {
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_;
+    static constexpr bool ALIGNED = ALIGNED_;
+    static constexpr int W = WM * WN;
+    static constexpr int FM = TM / WM / 16, FQ = TN / WN / 64;   // a wave's fragments: of 16 tokens, and 4 x 16 channels
+    static constexpr int LA = TM / 8 / W, LB = TN / 8 / W;       // 1 KB pieces (8 rows) that a wave fetches per step
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
 // 16 bytes of a row from column c on; columns from k on read as zero.
 __device__ inline v4i load_chunk(const int8_t* row, uint32_t c, uint32_t k) {
     v4i v = {0, 0, 0, 0};
@@ -27,104 +48,289 @@ __device__ inline v4i load_chunk(const int8_t* row, uint32_t c, uint32_t k) {
 
 __device__ inline v4i mfma(v4i x, v4i y, v4i acc) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, acc, 0, 0, 0); }
 
-template <typename T>
-__device__ inline void store_channels(const MatmulArgs& g, uint64_t token, uint64_t channel, const int (&sum)[16]) {
-    const float sa = g.sa[token];
-    T* out = (T*)g.out + token * g.ldo + channel;
-    float y[16];
-    if (channel + 16 <= g.n) {
-        float sb[16], bias[16];
-        load_run<float, 16>(g.sb + channel, sb);
-        if (g.bias) load_run<float, 16>(g.bias + channel, bias);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = g.bias ? fmaf((float)sum[i], sa * sb[i], bias[i]) : (float)sum[i] * (sa * sb[i]);
-        store_run<T, 16>(out, y);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (channel + i < g.n) {
-                const float s = sa * g.sb[channel + i];
-                out[i] = (T)(g.bias ? fmaf((float)sum[i], s, g.bias[channel + i]) : (float)sum[i] * s);
-            }
-    }
+// In LDS the 16-byte parts of a row's 128 bytes are permuted by a key of the row (part ^ key), so that the 8 lanes that read
+// together, same part of 8 rows, meet 8 different groups of banks (SQ_LDS_BANK_CONFLICT 0).
+__device__ inline uint32_t row_key(uint32_t row) { return row & 7; }
+// Workgroups go to the 8 dies in turn, each of which has an L2 of its own: a die takes tiles side by side, in bands of 4 rows of tiles.
+__device__ inline void place_tile(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
+    constexpr uint32_t DIES = 8, BAND = 4;
+    const uint32_t total = tiles_m * tiles_n, per = total / DIES, rest = total % DIES, die = id % DIES;
+    const uint32_t at = die * per + (die < rest ? die : rest) + id / DIES;
+    const uint32_t first = at / (BAND * tiles_n) * BAND, high = tiles_m - first < BAND ? tiles_m - first : BAND, in = at - first * tiles_n;
+    tm = first + in % high;
+    tn = in / high;
 }
 
-// Rows' positions within a 128-byte line of LDS are permuted by a key of the row, so that the 8 lanes that read in one cycle
-// meet 8 different quarters of banks.  Tokens: 16 consecutive rows a fragment.  Channels: fragment f of a block of 64 holds
-// rows 16 * (i / 4) + 4 * f + i % 4, so that a lane's results over the 4 fragments are 16 consecutive channels.
-__device__ inline uint32_t token_key(uint32_t row) { return row & 7; }
-__device__ inline uint32_t channel_key(uint32_t row) { return (row & 3) | ((row >> 2) & 4); }
+typedef __attribute__((address_space(3))) int8_t lds_byte;
 
-// One workgroup: TM tokens x TN channels, WM x WN waves.
-template <typename T, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void scaled_matmul_tile_kernel(MatmulArgs g) {
-    constexpr int W = WM * WN, FM = TM / WM / 16, FQ = TN / WN / 64;
-    __shared__ __align__(16) int8_t sa_tile[TM * STEP];
-    __shared__ __align__(16) int8_t sb_tile[TN * STEP];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t tile = blockIdx.x;
-    const uint64_t m0 = (uint64_t)(tile % g.tiles_m) * TM, n0 = (uint64_t)(tile / g.tiles_m) * TN;
-    const uint32_t wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN);
-    v4i acc[FM][FQ][4] = {};
-    for (uint32_t c0 = 0; c0 < g.k; c0 += STEP) {
-        __syncthreads();
+// Where the steps' rows come from: the tile and step that are fetched next.
+template <typename G>
+struct Source {
+    const MatmulArgs& g;
+    uint32_t tiles, steps, lane, wave;
+    uint32_t tile, step = 0;
+    __amdgpu_buffer_rsrc_t ra, rb;
+    const int8_t *pa, *pb;                // of the tile's first rows
+    using offset = std::conditional_t<G::ALIGNED, uint32_t, uint64_t>;
+    offset oa[G::LA], ob[G::LB];          // a lane's 16 bytes within the tile's rows, of step 0
+    v4i va[G::ALIGNED ? 1 : G::LA], vb[G::ALIGNED ? 1 : G::LB];
+
+    __device__ uint32_t row_of(int j) const { return (j * G::W + wave) * 8 + lane / 8; }
+    __device__ uint32_t part() const { return (lane & 7) ^ row_key(lane / 8); }   // of any j: rows of a piece begin at a multiple of 8
+
+    __device__ void aim() {
+        uint32_t tm, tn;
+        place_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
+        const uint64_t m0 = (uint64_t)tm * G::TM, n0 = (uint64_t)tn * G::TN;
+        const uint32_t last_a = (uint32_t)(g.m - m0 < G::TM ? g.m - m0 : G::TM) - 1, last_b = (uint32_t)(g.n - n0 < G::TN ? g.n - n0 : G::TN) - 1;
+        pa = g.a + m0 * g.lda;
+        pb = g.b + n0 * g.ldb;
+        // rows past the last one: the last one again (their results are not stored)
 #pragma unroll
-        for (int j = 0; j < TM / 8 / W; ++j) {
-            const uint32_t row = (j * W + wave) * 8 + lane / 8, chunk = (lane & 7) ^ token_key(row);
-            const uint64_t r = m0 + row < g.m ? m0 + row : g.m - 1;
-            *(v4i*)(sa_tile + row * STEP + (lane & 7) * 16) = load_chunk(g.a + r * g.lda, c0 + chunk * 16, g.k);
+        for (int j = 0; j < G::LA; ++j) oa[j] = min(row_of(j), last_a) * (offset)g.lda + part() * 16;
+#pragma unroll
+        for (int j = 0; j < G::LB; ++j) ob[j] = min(row_of(j), last_b) * (offset)g.ldb + part() * 16;
+        if constexpr (G::ALIGNED) {
+            ra = __builtin_amdgcn_make_buffer_rsrc((void*)pa, 0, last_a * (uint32_t)g.lda + g.k, 0x00020000);
+            rb = __builtin_amdgcn_make_buffer_rsrc((void*)pb, 0, last_b * (uint32_t)g.ldb + g.k, 0x00020000);
+            if (steps == 1) fold();
+        }
+    }
+    // The last step, if the columns end within it: lanes whose part lies behind the end read the step's first part instead.
+    __device__ void fold() {
+        const uint32_t left = g.k - (steps - 1) * STEP;
+        if (left == STEP) return;
+#pragma unroll
+        for (int j = 0; j < G::LA; ++j)
+            if (part() * 16 >= left) oa[j] -= part() * 16;
+#pragma unroll
+        for (int j = 0; j < G::LB; ++j)
+            if (part() * 16 >= left) ob[j] -= part() * 16;
+    }
+    // Start the transfer of a step (ALIGNED: to LDS; otherwise into registers, for land()).
+    __device__ void fetch(int8_t* a, int8_t* b) {
+        if constexpr (G::ALIGNED) {
+#pragma unroll
+            for (int j = 0; j < G::LA; ++j)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte*)(a + (j * G::W + wave) * 1024), 16, oa[j], step * STEP, 0, 0);
+#pragma unroll
+            for (int j = 0; j < G::LB; ++j)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte*)(b + (j * G::W + wave) * 1024), 16, ob[j], step * STEP, 0, 0);
+        } else {
+            const uint32_t c = step * STEP;
+#pragma unroll
+            for (int j = 0; j < G::LA; ++j) va[j] = load_chunk(pa + (oa[j] - part() * 16), c + part() * 16, g.k);
+#pragma unroll
+            for (int j = 0; j < G::LB; ++j) vb[j] = load_chunk(pb + (ob[j] - part() * 16), c + part() * 16, g.k);
+        }
+    }
+    __device__ void land(int8_t* a, int8_t* b) {
+        if constexpr (!G::ALIGNED) {
+#pragma unroll
+            for (int j = 0; j < G::LA; ++j) *(v4i*)(a + (j * G::W + wave) * 1024 + lane * 16) = va[j];
+#pragma unroll
+            for (int j = 0; j < G::LB; ++j) *(v4i*)(b + (j * G::W + wave) * 1024 + lane * 16) = vb[j];
+        }
+    }
+    // After the last tile the fetches repeat its steps, which nobody reads.
+    __device__ void advance() {
+        if (++step == steps) {
+            step = 0;
+            if (tile + gridDim.x < tiles) tile += gridDim.x;
+            aim();
+        } else if (G::ALIGNED && step == steps - 1) {
+            fold();
+        }
+    }
+    // Before a step is multiplied, where the columns end within it: zeros for the tokens' parts behind the end, by the wave that
+    // fetched them (the channels' may hold anything then).
+    __device__ void clear_tail(int8_t* a) const {
+        const uint32_t left = g.k - (steps - 1) * STEP;
+        __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): the transfers to LDS have landed
+#pragma unroll
+        for (int j = 0; j < G::LA; ++j)
+            if (part() * 16 >= left) *(v4i*)(a + (j * G::W + wave) * 1024 + lane * 16) = v4i{0, 0, 0, 0};
+    }
+};
+
+// The products of one step.
+template <typename G>
+__device__ inline void multiply_step(v4i (&acc)[G::FM][G::FQ][4], const int8_t* a, const int8_t* b, uint32_t wm, uint32_t wn, uint32_t lane) {
+    constexpr int R = G::FM + G::FQ * 4, M = G::FM * G::FQ * 4, V = G::LA + G::LB;
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+        v4i tok[G::FM], ch[G::FQ][4];
+#pragma unroll
+        for (int f = 0; f < G::FM; ++f) {
+            const uint32_t row = wm + f * 16 + lane % 16;
+            tok[f] = *(const v4i*)(a + row * STEP + ((kk * 4 + lane / 16) ^ row_key(row)) * 16);
         }
 #pragma unroll
-        for (int j = 0; j < TN / 8 / W; ++j) {
-            const uint32_t row = (j * W + wave) * 8 + lane / 8, chunk = (lane & 7) ^ channel_key(row);
-            const uint64_t r = n0 + row < g.n ? n0 + row : g.n - 1;
-            *(v4i*)(sb_tile + row * STEP + (lane & 7) * 16) = load_chunk(g.b + r * g.ldb, c0 + chunk * 16, g.k);
-        }
-        __syncthreads();
+        for (int q = 0; q < G::FQ; ++q)
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            v4i tok[FM], ch[FQ][4];
-#pragma unroll
-            for (int f = 0; f < FM; ++f) {
-                const uint32_t row = wm + f * 16 + lane % 16;
-                tok[f] = *(const v4i*)(sa_tile + row * STEP + ((kk * 4 + lane / 16) ^ token_key(row)) * 16);
+            for (int f = 0; f < 4; ++f) {
+                const uint32_t row = wn + q * 64 + f * 16 + lane % 16;
+                ch[q][f] = *(const v4i*)(b + row * STEP + ((kk * 4 + lane / 16) ^ row_key(row)) * 16);
             }
 #pragma unroll
-            for (int q = 0; q < FQ; ++q)
+        for (int fm = 0; fm < G::FM; ++fm)
 #pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    const uint32_t i = lane % 16, row = wn + q * 64 + i / 4 * 16 + f * 4 + i % 4;
-                    ch[q][f] = *(const v4i*)(sb_tile + row * STEP + ((kk * 4 + lane / 16) ^ channel_key(row)) * 16);
+            for (int q = 0; q < G::FQ; ++q)
+#pragma unroll
+                for (int f = 0; f < 4; ++f) acc[fm][q][f] = mfma(ch[q][f], tok[fm], acc[fm][q][f]);
+    }
+    if constexpr (G::ALIGNED) {
+        // Order: the first half's reads; its products with the second half's reads and the next step's transfers between them (a
+        // burst of transfers at the step's start held the products up: 8192^3 486 -> 427 us with this and the rounds over tiles);
+        // the second half's products.
+        constexpr int N = M < 8 ? M : 8;
+        __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, M / N, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, (V + N - 1) / N, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, (R + N - 1) / N, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+}
+
+// LDS written by some lanes of a wave and read by others of it: their order in the code is the order that they are done in.
+__device__ inline void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A wave's results of a tile, scaled, to memory, 16 tokens x 64 channels at a time: through 4 KB of LDS of its own, so that a store's
+// lanes write the channels of a token side by side (lines of 128 bytes).  16-byte parts of a token's 256 are permuted by its number.
+template <typename T, typename G>
+__device__ inline void store_tile(const MatmulArgs& g, v4i (&acc)[G::FM][G::FQ][4], float* turn, uint64_t m0, uint64_t n0, uint32_t lane) {
+    constexpr int RUN = 16 / sizeof(T), PARTS = RUN / 4, LANES = 64 / RUN, ROWS = 64 / LANES;   // channels a lane, lanes a token
+#pragma unroll
+    for (int q = 0; q < G::FQ; ++q) {
+        const uint64_t channel = n0 + q * 64 + lane % LANES * RUN;
+        float sb[RUN], bias[RUN];
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            const uint64_t c = min(channel + i, g.n - 1);
+            sb[i] = g.sb[c];
+            bias[i] = g.bias ? g.bias[c] : 0.f;
+        }
+#pragma unroll
+        for (int fm = 0; fm < G::FM; ++fm) {
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                const uint32_t token = lane % 16;
+                typedef float v4f __attribute__((ext_vector_type(4)));
+                *(v4f*)(turn + token * 64 + ((f * 4 + lane / 16) ^ token) * 4) = __builtin_convertvector(acc[fm][q][f], v4f);
+                acc[fm][q][f] = v4i{0, 0, 0, 0};
+            }
+            wave_sync();
+#pragma unroll
+            for (int r = 0; r < 16; r += ROWS) {
+                const uint32_t row = r + lane / LANES;
+                const uint64_t token = m0 + fm * 16 + row;
+                if (token < g.m) {
+                    const float sa = g.sa[token];
+                    float y[RUN];
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            y[p * 4 + i] = fmaf(turn[row * 64 + ((lane % LANES * PARTS + p) ^ row) * 4 + i], sa * sb[p * 4 + i], bias[p * 4 + i]);
+                    T* out = (T*)g.out + token * g.ldo + channel;
+                    if (channel + RUN <= g.n) store_run<T, RUN>(out, y);
+                    else
+#pragma unroll
+                        for (int i = 0; i < RUN; ++i)
+                            if (channel + i < g.n) out[i] = (T)y[i];
                 }
-#pragma unroll
-            for (int fm = 0; fm < FM; ++fm)
-#pragma unroll
-                for (int q = 0; q < FQ; ++q)
-#pragma unroll
-                    for (int f = 0; f < 4; ++f) acc[fm][q][f] = mfma(ch[q][f], tok[fm], acc[fm][q][f]);
-        }
-    }
-#pragma unroll
-    for (int fm = 0; fm < FM; ++fm) {
-        const uint64_t token = m0 + wm + fm * 16 + lane % 16;
-        if (token >= g.m) continue;
-#pragma unroll
-        for (int q = 0; q < FQ; ++q) {
-            int sum[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sum[i] = acc[fm][q][i / 4][i % 4];
-            store_channels<T>(g, token, n0 + wn + q * 64 + lane / 16 * 16, sum);
+            }
+            wave_sync();
         }
     }
 }
+#endif
+
+template <typename T, typename G>
+__global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    __shared__ __align__(16) int8_t a0[G::TM * STEP], b0[G::TN * STEP], a1[G::TM * STEP], b1[G::TN * STEP];
+    __shared__ __align__(16) float turns[G::W][16 * 64];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t wm = wave % G::WM * (G::TM / G::WM), wn = wave / G::WM * (G::TN / G::WN);
+    const uint32_t tiles = g.tiles_m * g.tiles_n, steps = (g.k + STEP - 1) / STEP;
+    const bool partial = G::ALIGNED && g.k % STEP != 0;
+    Source<G> src{g, tiles, steps, lane, wave, blockIdx.x};
+    src.aim();
+    v4i acc[G::FM][G::FQ][4] = {};
+    uint32_t tile = blockIdx.x, step = 0;
+    src.fetch(a0, b0);
+    src.land(a0, b0);
+    src.advance();
+    for (;;) {
+        if (partial && step == steps - 1) src.clear_tail(a0);
+        __syncthreads();
+        src.fetch(a1, b1);
+        multiply_step<G>(acc, a0, b0, wm, wn, lane);
+        src.land(a1, b1);
+        src.advance();
+        if (++step == steps) {
+            uint32_t tm, tn;
+            place_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
+            store_tile<T, G>(g, acc, turns[wave], (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            step = 0;
+            tile += gridDim.x;
+            if (tile >= tiles) break;
+        }
+        if (partial && step == steps - 1) src.clear_tail(a1);
+        __syncthreads();
+        src.fetch(a0, b0);
+        multiply_step<G>(acc, a1, b1, wm, wn, lane);
+        src.land(a0, b0);
+        src.advance();
+        if (++step == steps) {
+            uint32_t tm, tn;
+            place_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
+            store_tile<T, G>(g, acc, turns[wave], (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            step = 0;
+            tile += gridDim.x;
+            if (tile >= tiles) break;
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): nothing arrives in LDS that is no longer this workgroup's
+#endif
+}
+
+template <typename T, typename G>
+hipError_t launch_tile_shape(MatmulArgs g, hipStream_t stream) {
+    const uint64_t tm = (g.m + G::TM - 1) / G::TM, tn = (g.n + G::TN - 1) / G::TN;
+    g.tiles_m = (uint32_t)tm;
+    g.tiles_n = (uint32_t)tn;
+    // as many workgroups as the 256 CUs, with 160 KB of LDS each, hold at once
+    const uint64_t most = 256 * (163840 / (2 * (G::TM + G::TN) * STEP + G::W * 4096));
+    const uint64_t tiles = tm * tn;
+    scaled_matmul_kernel<T, G><<<dim3((uint32_t)(tiles < most ? tiles : most)), dim3(64 * G::W), 0, stream>>>(g);
+    return hipGetLastError();
+}
+
+template <typename T, bool ALIGNED>
+hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
+    const uint64_t large = ((g.m + 255) / 256) * ((g.n + 255) / 256), middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
+    if constexpr (ALIGNED)
+        if (large >= 128) return launch_tile_shape<T, Tile<256, 256, 4, 2, true>>(g, stream);
+    if (middle >= 192) return launch_tile_shape<T, Tile<128, 128, 2, 2, ALIGNED>>(g, stream);
+    return launch_tile_shape<T, Tile<64, 64, 4, 1, ALIGNED>>(g, stream);
+}
 
 template <typename T>
-hipError_t launch_tiles(MatmulArgs g, hipStream_t stream) {
-    constexpr int TM = 128, TN = 128;
-    g.tiles_m = (uint32_t)((g.m + TM - 1) / TM);
-    g.tiles_n = (uint32_t)((g.n + TN - 1) / TN);
-    scaled_matmul_tile_kernel<T, TM, TN, 2, 2><<<dim3(g.tiles_m * g.tiles_n), dim3(256), 0, stream>>>(g);
-    return hipGetLastError();
+hipError_t launch_type(const MatmulArgs& g, hipStream_t stream) {
+    // ALIGNED: 16-byte parts of rows, which either lie within the columns or behind them, at 32-bit offsets within a tile
+    const bool aligned = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.k % 16 == 0 &&
+                         g.lda < (1u << 23) && g.ldb < (1u << 23);
+    return aligned ? launch_tiles<T, true>(g, stream) : launch_tiles<T, false>(g, stream);
 }
 
 }  // namespace
@@ -133,9 +339,9 @@ size_t scaled_matmul_workspace(uint64_t, uint64_t, uint32_t) { return 0; }
 
 hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void*, hipStream_t stream) {
     if (g.m == 0 || g.n == 0) return hipSuccess;
-    if (out_dtype == TYPE_F16) return launch_tiles<f16_t>(g, stream);
-    if (out_dtype == TYPE_BF16) return launch_tiles<bf16_t>(g, stream);
-    return launch_tiles<float>(g, stream);
+    if (out_dtype == TYPE_F16) return launch_type<f16_t>(g, stream);
+    if (out_dtype == TYPE_BF16) return launch_type<bf16_t>(g, stream);
+    return launch_type<float>(g, stream);
 }
 
 }  // namespace dessert
