@@ -304,6 +304,97 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
 #endif
 }
 
+// ---- few tokens -------------------------------------------------------------------------------------------------------------
+// Up to 64 tokens: reading b is all there is, so that many waves, each with several loads on their way, matter more than the
+// matrix cores' rate.  A wave takes 16 channels and every KS-th 128 columns, straight from memory into the fragments' order (16
+// bytes of each of 16 rows); the 8 waves of a workgroup are KS parts of 8 / KS groups of channels and are added up in LDS.
+template <typename T, int MT, int KS, bool ALIGNED>
+__global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int GROUPS = 8 / KS, AHEAD = MT == 4 ? 2 : 4;   // 128-column steps loaded before they are multiplied
+    __shared__ __align__(16) v4i parts[KS == 1 ? 1 : 8][MT][64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t n0 = ((uint64_t)blockIdx.x * GROUPS + wave / KS) * 16;
+    const int8_t* row_b = g.b + min(n0 + lane % 16, g.n - 1) * g.ldb;
+    const int8_t* row_a[MT];
+#pragma unroll
+    for (int f = 0; f < MT; ++f) row_a[f] = g.a + min((uint64_t)(f * 16 + lane % 16), g.m - 1) * g.lda;
+    v4i acc[MT] = {};
+    for (uint32_t c0 = wave % KS * STEP; c0 < g.k; c0 += KS * STEP * AHEAD) {
+        v4i ch[AHEAD][2], tok[AHEAD][2][MT];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t c = c0 + u * KS * STEP + h * 64 + lane / 16 * 16;
+                if constexpr (ALIGNED) {   // columns behind the end: any channels' bytes, times zeros
+                    const bool in = c < g.k;
+                    const uint32_t at = in ? c : 0;
+                    ch[u][h] = *(const v4i*)(row_b + at);
+#pragma unroll
+                    for (int f = 0; f < MT; ++f) {
+                        const v4i v = *(const v4i*)(row_a[f] + at);
+                        tok[u][h][f] = in ? v : v4i{0, 0, 0, 0};
+                    }
+                } else {
+                    ch[u][h] = load_chunk(row_b, c, g.k);
+#pragma unroll
+                    for (int f = 0; f < MT; ++f) tok[u][h][f] = load_chunk(row_a[f], c, g.k);
+                }
+            }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int f = 0; f < MT; ++f) acc[f] = mfma(ch[u][h], tok[u][h][f], acc[f]);
+    }
+    if constexpr (KS > 1) {
+#pragma unroll
+        for (int f = 0; f < MT; ++f) parts[wave][f][lane] = acc[f];
+        __syncthreads();
+        // the group's waves share the fragments to add up
+        const uint32_t first = wave / KS * KS;
+#pragma unroll
+        for (int f = 0; f < MT; ++f) {
+            if (f % KS != wave % KS) continue;
+            acc[f] = parts[first][f][lane];
+            for (int p = 1; p < KS; ++p) acc[f] += parts[first + p][f][lane];
+        }
+    }
+    const uint64_t channel = n0 + lane / 16 * 4;
+#pragma unroll
+    for (int f = 0; f < MT; ++f) {
+        const uint64_t token = f * 16 + lane % 16;
+        if (f % KS != wave % KS || token >= g.m) continue;
+        const float sa = g.sa[token];
+        T* out = (T*)g.out + token * g.ldo + channel;
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t c = min(channel + i, g.n - 1);
+            y[i] = fmaf((float)acc[f][i], sa * g.sb[c], g.bias ? g.bias[c] : 0.f);
+        }
+        if (channel + 4 <= g.n) store_run<T, 4>(out, y);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (channel + i < g.n) out[i] = (T)y[i];
+    }
+#endif
+}
+
+template <typename T, int MT, bool ALIGNED>
+hipError_t launch_few(const MatmulArgs& g, hipStream_t stream) {
+    const uint32_t steps = (g.k + STEP - 1) / STEP;
+    const uint64_t groups = (g.n + 15) / 16;
+    const auto grid = [&](int ks) { return dim3((uint32_t)((groups + 8 / ks - 1) / (8 / ks))); };
+    if (steps >= 16 || (steps >= 8 && groups < 512)) scaled_matmul_few_kernel<T, MT, 8, ALIGNED><<<grid(8), dim3(512), 0, stream>>>(g);
+    else if (steps >= 4) scaled_matmul_few_kernel<T, MT, 4, ALIGNED><<<grid(4), dim3(512), 0, stream>>>(g);
+    else scaled_matmul_few_kernel<T, MT, 1, ALIGNED><<<grid(1), dim3(512), 0, stream>>>(g);
+    return hipGetLastError();
+}
+
 template <typename T, typename G>
 hipError_t launch_tile_shape(MatmulArgs g, hipStream_t stream) {
     const uint64_t tm = (g.m + G::TM - 1) / G::TM, tn = (g.n + G::TN - 1) / G::TN;
@@ -330,6 +421,9 @@ hipError_t launch_type(const MatmulArgs& g, hipStream_t stream) {
     // ALIGNED: 16-byte parts of rows, which either lie within the columns or behind them, at 32-bit offsets within a tile
     const bool aligned = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.k % 16 == 0 &&
                          g.lda < (1u << 23) && g.ldb < (1u << 23);
+    if (g.m <= 16) return aligned ? launch_few<T, 1, true>(g, stream) : launch_few<T, 1, false>(g, stream);
+    if (g.m <= 32) return aligned ? launch_few<T, 2, true>(g, stream) : launch_few<T, 2, false>(g, stream);
+    if (g.m <= 64) return aligned ? launch_few<T, 4, true>(g, stream) : launch_few<T, 4, false>(g, stream);
     return aligned ? launch_tiles<T, true>(g, stream) : launch_tiles<T, false>(g, stream);
 }
 
