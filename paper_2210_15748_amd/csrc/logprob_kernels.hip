@@ -43,39 +43,65 @@ __device__ inline Sums join(Sums a, Sums b) {
 }
 
 // A key orders entries by value, then by lower column; 0 stands for none.  Values are whole floats; -0 counts as +0.
-__device__ inline uint64_t key_of(float x, uint32_t col) {
-    uint32_t u = __float_as_uint(x + 0.f);
-    u = u & 0x80000000u ? ~u : u | 0x80000000u;
-    return (uint64_t)u << 32 | (uint32_t)~col;
+__device__ inline uint32_t order_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ inline float key_value(uint64_t key) {
-    const uint32_t u = (uint32_t)(key >> 32);
-    return __uint_as_float(u & 0x80000000u ? u & 0x7FFFFFFFu : ~u);
-}
-constexpr uint64_t KEY_FLOOR = (uint64_t)0x007FFFFFu << 32 | 0xFFFFFFFFu;   // an entry of -inf: no key up to this one is an alternative
+__device__ inline float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order & 0x7FFFFFFFu : ~order); }
+__device__ inline uint64_t key_of(uint32_t order, uint32_t col) { return (uint64_t)order << 32 | (uint32_t)~col; }
+constexpr uint32_t ORDER_FLOOR = 0x007FFFFFu;   // of -inf, which is no alternative
+constexpr uint64_t KEY_FLOOR = (uint64_t)ORDER_FLOOR << 32 | 0xFFFFFFFFu;
 
-// The wave's list: lane j holds the j-th largest key.
-__device__ inline void insert(uint64_t& list, uint64_t key, uint32_t lane) {
-    const uint32_t at = __popcll(__ballot(list > key));
-    const uint64_t left = __shfl_up(list, 1);
-    if (lane == at) list = key;
-    else if (lane > at) list = left;
+__device__ inline uint64_t read_lane(uint64_t v, uint32_t lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), (int)lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, (int)lane);
 }
-// Offer one key a lane; the list's entry at n_top - 1 is the threshold.
-__device__ inline void offer(uint64_t& list, uint64_t key, uint32_t n_top, uint32_t lane) {
-    uint64_t least = __shfl(list, (int)n_top - 1);
-    if (least < KEY_FLOOR) least = KEY_FLOOR;
-    uint64_t want = __ballot(key > least);
-    while (want) {
-        const int from = __ffsll((unsigned long long)want) - 1;
-        const uint64_t k = __shfl(key, from);
-        if (lane == (uint32_t)from) key = 0;
-        insert(list, k, lane);
-        least = __shfl(list, (int)n_top - 1);
-        if (least < KEY_FLOOR) least = KEY_FLOOR;
-        want = __ballot(key > least);
+
+// A wave's list of the best entries it has seen: lane j holds the j-th largest key, 0 where there is none.
+struct Best {
+    uint64_t list = 0, least = KEY_FLOOR;   // least: what a key has to beat, list[n_top - 1] or the floor
+
+    // One key, the same in all lanes, that beats `least`.
+    __device__ void insert(uint64_t key, uint32_t n_top, uint32_t lane) {
+        const uint32_t at = __popcll(__ballot(list > key));
+        // the neighbour's entry: the whole wave moves up by one lane
+        const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(list >> 32), 0x138, 0xF, 0xF, false);
+        const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)list, 0x138, 0xF, 0xF, false);
+        if (lane == at) list = key;
+        else if (lane > at) list = (uint64_t)hi << 32 | lo;
+        const uint64_t last = read_lane(list, n_top - 1);
+        least = last > KEY_FLOOR ? last : KEY_FLOOR;
     }
-}
+    // A key from every lane.
+    __device__ void offer(uint64_t key, uint32_t n_top, uint32_t lane) {
+        uint64_t want = __ballot(key > least);
+        while (want) {
+            const uint32_t from = __ffsll((unsigned long long)want) - 1;
+            insert(read_lane(key, from), n_top, lane);
+            want &= want - 1;
+            want &= __ballot(key > least);
+        }
+    }
+    // V values from every lane, `peak` the largest of a lane's; col(i) the column of value i.  An entry can be among the n_top best
+    // only if it is not below the n_top-th largest of the 64 peaks: that bound (its upper 18 bits, by bisection) leaves little more
+    // than n_top values to insert, where an empty list would let in n_top * ln(64 V / n_top) more.
+    template <int V, typename Col>
+    __device__ void offer_all(const float (&v)[V], float peak, uint32_t n_top, uint32_t lane, Col col) {
+        const uint32_t top = order_of(peak);
+        if (!__ballot(top >= (uint32_t)(least >> 32))) return;
+        uint32_t bound = 0;
+#pragma unroll
+        for (int bit = 31; bit >= 14; --bit) {
+            const uint32_t t = bound | 1u << bit;
+            if ((uint32_t)__popcll(__ballot(top >= t)) >= n_top) bound = t;
+        }
+        const uint32_t floor = (uint32_t)(least >> 32);
+        if (bound < floor) bound = floor;
+        const float from = value_of(bound);   // compared as floats: no order to be formed for entries that are out
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (__ballot(v[i] >= from)) offer(v[i] >= from ? key_of(order_of(v[i]), col(i)) : 0, n_top, lane);
+    }
+};
 
 __device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, float given, uint64_t list, uint32_t lane) {
     const float log_s = logf(z.s);
@@ -91,7 +117,7 @@ __device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, float 
     if (lane < g.n_top) {
         const bool some = list > KEY_FLOOR && !nan;
         g.top_ids[row * g.n_top + lane] = some ? ~(uint32_t)list : NONE;
-        g.top_logprobs[row * g.n_top + lane] = nan ? z.s : some ? (key_value(list) - z.m) - log_s : MINUS_INF;
+        g.top_logprobs[row * g.n_top + lane] = nan ? z.s : some ? (value_of((uint32_t)(list >> 32)) - z.m) - log_s : MINUS_INF;
     }
 }
 
@@ -116,24 +142,28 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(LogprobArgs g) {
         const uint32_t end = g.vocab - begin < g.segment ? g.vocab : begin + g.segment;
         const T* x = (const T*)g.logits + row * g.stride;
         Sums z{MINUS_INF, 0.f, 0.f};
-        uint64_t list = 0;
+        Best best;
         for (uint32_t c0 = begin; c0 < end; c0 += 256 * V) {
             float v[V];
-            float peak = MINUS_INF;
+            if (c0 + 256 * V <= end) {   // the loads of all runs are on their way at once
 #pragma unroll
-            for (int j = 0; j < V / RUN; ++j) {
-                const uint32_t c = c0 + (j * 256 + threadIdx.x) * RUN;
-                float part[RUN];
-                if (c + RUN <= end) load_run<T, RUN>(x + c, part);
-                else
+                for (int j = 0; j < V / RUN; ++j) load_run<T, RUN>(x + c0 + (j * 256 + threadIdx.x) * RUN, *(float(*)[RUN])(v + j * RUN));
+            } else {
 #pragma unroll
-                    for (int i = 0; i < RUN; ++i) part[i] = c + i < end ? (float)x[c + i] : MINUS_INF;
+                for (int j = 0; j < V / RUN; ++j) {
+                    const uint32_t c = c0 + (j * 256 + threadIdx.x) * RUN;
+                    float part[RUN];
+                    if (c + RUN <= end) load_run<T, RUN>(x + c, part);
+                    else
 #pragma unroll
-                for (int i = 0; i < RUN; ++i) {
-                    v[j * RUN + i] = part[i];
-                    peak = fmaxf(peak, part[i]);
+                        for (int i = 0; i < RUN; ++i) part[i] = c + i < end ? (float)x[c + i] : MINUS_INF;
+#pragma unroll
+                    for (int i = 0; i < RUN; ++i) v[j * RUN + i] = part[i];
                 }
             }
+            float peak = MINUS_INF;
+#pragma unroll
+            for (int i = 0; i < V; ++i) peak = fmaxf(peak, v[i]);
             const float m = fmaxf(z.m, peak);
             const float base = m == MINUS_INF ? 0.f : m;
             if (z.m != MINUS_INF) {
@@ -146,34 +176,32 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(LogprobArgs g) {
             for (int i = 0; i < V; ++i) {
                 const float d = v[i] - base, e = exp_of(d);
                 z.s += e;
-                z.t += e * fmaxf(d, -3.4e38f);   // an entry of -inf adds 0, not 0 * inf
+                z.t = fmaf(e, fmaxf(d, -1000.f), z.t);   // an entry of -inf adds 0, not 0 * inf; e^-1000 is 0 as well
             }
-            if (g.n_top) {
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    offer(list, key_of(v[i], c0 + ((i / RUN) * 256 + threadIdx.x) * RUN + i % RUN), g.n_top, lane);
-            }
+            if (g.n_top)
+                best.offer_all<V>(v, peak, g.n_top, lane,
+                                  [&](int i) { return c0 + ((i / RUN) * 256 + threadIdx.x) * RUN + i % RUN; });
         }
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) z = join(z, Sums{__shfl_xor(z.m, o), __shfl_xor(z.s, o), __shfl_xor(z.t, o)});
         __syncthreads();
         if (lane == 0) s_sums[wave] = z;
-        s_list[wave][lane] = list;
+        s_list[wave][lane] = best.list;
         __syncthreads();
         if (wave == 0) {
             for (int o = 1; o < 4; ++o) {
                 z = join(z, s_sums[o]);
-                if (g.n_top) offer(list, lane < g.n_top ? s_list[o][lane] : 0, g.n_top, lane);
+                if (g.n_top) best.offer(lane < g.n_top ? s_list[o][lane] : 0, g.n_top, lane);
             }
             if (g.splits == 1) {
-                finish(g, row, z, given_logit<T>(g, row), list, lane);
+                finish(g, row, z, given_logit<T>(g, row), best.list, lane);
             } else {
                 if (lane == 0) {
                     g.part_sums[3 * w] = z.m;
                     g.part_sums[3 * w + 1] = z.s;
                     g.part_sums[3 * w + 2] = z.t;
                 }
-                if (lane < g.n_top) g.part_keys[w * g.n_top + lane] = list;
+                if (lane < g.n_top) g.part_keys[w * g.n_top + lane] = best.list;
             }
         }
         __syncthreads();
@@ -190,11 +218,11 @@ __global__ __launch_bounds__(64) void join_logprobs_kernel(LogprobArgs g) {
         for (uint32_t i = lane; i < g.splits; i += 64) z = join(z, Sums{sums[3 * i], sums[3 * i + 1], sums[3 * i + 2]});
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) z = join(z, Sums{__shfl_xor(z.m, o), __shfl_xor(z.s, o), __shfl_xor(z.t, o)});
-        uint64_t list = 0;
+        Best best;
         const uint64_t* keys = g.part_keys + row * g.splits * g.n_top;
         for (uint32_t i = 0; i < g.splits * g.n_top; i += 64)
-            offer(list, i + lane < g.splits * g.n_top ? keys[i + lane] : 0, g.n_top, lane);
-        finish(g, row, z, given_logit<T>(g, row), list, lane);
+            best.offer(i + lane < g.splits * g.n_top ? keys[i + lane] : 0, g.n_top, lane);
+        finish(g, row, z, given_logit<T>(g, row), best.list, lane);
     }
 }
 
