@@ -64,6 +64,8 @@ constexpr uint32_t POOL = 256;   // keys a wave keeps
 struct Pool {
     uint64_t* keys;
     uint32_t count = 0, bound = ORDER_FLOOR;
+    uint32_t grown = 0;             // keys since the bound was last looked for
+    uint32_t peaks[4] = {0, 0, 0, 0};   // the orders of the largest of four parts of the entries that the lane has had
 
     // The n_top largest of `count` keys, sorted: a key's place is the number of larger ones (no two are equal).
     __device__ void compress(uint32_t n_top, uint32_t lane) {
@@ -74,10 +76,10 @@ struct Pool {
             mine[j] = j * 64 + lane < count ? keys[j * 64 + lane] : 0;
             place[j] = 0;
         }
-        for (uint32_t i = 0; i < count; ++i) {
-            const uint64_t k = keys[i];
+        for (uint32_t i = 0; i < count; i += 2) {
+            const uint64_t k0 = keys[i], k1 = i + 1 < count ? keys[i + 1] : 0;
 #pragma unroll
-            for (uint32_t j = 0; j < POOL / 64; ++j) place[j] += k > mine[j];
+            for (uint32_t j = 0; j < POOL / 64; ++j) place[j] += (uint32_t)(k0 > mine[j]) + (uint32_t)(k1 > mine[j]);
         }
         wave_sync();
 #pragma unroll
@@ -89,23 +91,43 @@ struct Pool {
             bound = max(bound, (uint32_t)__builtin_amdgcn_readfirstlane((int)(keys[n_top - 1] >> 32)));
         }
     }
-    __device__ void add(bool want, uint64_t key, uint32_t n_top, uint32_t lane) {
+    // A key from every lane that wants one in; there has to be room.
+    __device__ void add(bool want, uint64_t key) {
         const uint64_t all = __ballot(want);
         if (!all) return;
-        if (count > POOL - 64) compress(n_top, lane);
+        grown += __popcll(all);
         if (want) keys[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = key;
         count += __popcll(all);
-        wave_sync();
     }
-    // `peak`: the order of the largest entry of each lane.  The n_top-th largest of the 64 peaks bounds the n_top-th largest entry from
-    // below; its upper 18 bits, by bisection, leave in little more than n_top entries of a wave's.
-    __device__ bool raise(uint32_t peak, uint32_t n_top) {
-        if (!__ballot(peak > bound)) return false;
-        uint32_t b = 0;
+    // now: the orders of the largest of four parts of the entries that the lane has now.  false: none can be among the best.  The n_top-th
+    // largest of the peaks so far bounds the n_top-th largest entry so far from below; its upper 18 bits, by bisection, leave in little
+    // more than n_top entries of the first ones and few of the later ones.  (The lanes' own peaks do for a few alternatives; of 64 they
+    // would be the least.)
+    __device__ bool raise(const uint32_t (&now)[4], uint32_t n_top) {
+        const uint32_t best = max(max(now[0], now[1]), max(now[2], now[3]));
+        const uint32_t above = __popcll(__ballot(best > bound));
 #pragma unroll
-        for (int bit = 31; bit >= 14; --bit) {
-            const uint32_t t = b | 1u << bit;
-            if ((uint32_t)__popcll(__ballot(peak >= t)) >= n_top) b = t;
+        for (int q = 0; q < 4; ++q) peaks[q] = max(peaks[q], now[q]);
+        if (above == 0) return false;
+        if (grown + above < n_top) return true;
+        grown = 0;
+        uint32_t b = 0;
+        if (n_top <= 16) {
+            const uint32_t peak = max(max(peaks[0], peaks[1]), max(peaks[2], peaks[3]));
+#pragma unroll
+            for (int bit = 31; bit >= 14; --bit) {
+                const uint32_t t = b | 1u << bit;
+                if ((uint32_t)__popcll(__ballot(peak >= t)) >= n_top) b = t;
+            }
+        } else {
+#pragma unroll 1
+            for (int bit = 31; bit >= 14; --bit) {
+                const uint32_t t = b | 1u << bit;
+                uint32_t n = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) n += __popcll(__ballot(peaks[q] >= t));
+                if (n >= n_top) b = t;
+            }
         }
         bound = max(bound, b);
         return true;
@@ -116,8 +138,39 @@ struct Pool {
 // are the workgroup's; all 256 threads take part.
 struct Totals {
     Sums sums[4];
-    uint32_t bound[4], count;
+    uint32_t bound[4], count, above[2][4];
 };
+
+// The bound once more, over the whole workgroup's `count` keys (at most 1024), where they are many: those below it go.  All threads take part;
+// `spare` has room for the keys.
+__device__ inline uint32_t thin_out(uint64_t* finals, uint64_t* spare, Totals& totals, uint32_t count, uint32_t n_top) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint64_t mine[POOL / 64];
+#pragma unroll
+    for (uint32_t j = 0; j < POOL / 64; ++j) mine[j] = threadIdx.x + 256 * j < count ? finals[threadIdx.x + 256 * j] : 0;
+    uint32_t b = 0;
+#pragma unroll 1
+    for (int bit = 31; bit >= 14; --bit) {
+        const uint32_t t = b | 1u << bit;
+        uint32_t n = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < POOL / 64; ++j) n += __popcll(__ballot((uint32_t)(mine[j] >> 32) >= t));
+        uint32_t* above = totals.above[bit & 1];   // the other turn's are read until the next barrier
+        if (lane == 0) above[wave] = n;
+        __syncthreads();
+        if (above[0] + above[1] + above[2] + above[3] >= n_top) b = t;
+    }
+    if (threadIdx.x == 0) totals.count = 0;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t j = 0; j < POOL / 64; ++j)
+        if (mine[j] && (uint32_t)(mine[j] >> 32) >= b) spare[atomicAdd(&totals.count, 1u)] = mine[j];
+    __syncthreads();
+    const uint32_t left = totals.count;
+    for (uint32_t i = threadIdx.x; i < left; i += 256) finals[i] = spare[i];
+    __syncthreads();
+    return left;
+}
 __device__ inline Sums wave_total(Sums z) {
     float m = z.m;
 #pragma unroll
@@ -132,7 +185,7 @@ __device__ inline Sums wave_total(Sums z) {
 }
 
 template <typename T>
-__device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, Pool& pool, uint64_t* finals, Totals& totals, uint64_t part) {
+__device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, Pool& pool, uint64_t* pools, uint64_t* finals, Totals& totals, uint64_t part) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     z = wave_total(z);
     if (lane == 0) {
@@ -164,13 +217,20 @@ __device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, Pool& 
     for (uint32_t i = lane; i < pool.count; i += 64)
         if ((uint32_t)(pool.keys[i] >> 32) >= bound) finals[atomicAdd(&totals.count, 1u)] = pool.keys[i];
     __syncthreads();
-    const uint32_t count = totals.count;
+    uint32_t count = totals.count;
+    if (count > 2 * g.n_top && count > 96) count = thin_out(finals, pools, totals, count, g.n_top);
     for (uint32_t j = threadIdx.x; j < max(count, g.n_top); j += 256) {
         const uint64_t mine = j < count ? finals[j] : 0;
         uint32_t place = j;   // behind the last key: an unused slot
         if (j < count) {
             place = 0;
-            for (uint32_t i = 0; i < count; ++i) place += finals[i] > mine;
+            for (uint32_t i = 0; i < count; i += 8) {   // what lies behind the last key is read, but not counted
+                uint64_t other[8];
+#pragma unroll
+                for (uint32_t u = 0; u < 8; ++u) other[u] = finals[i + u];
+#pragma unroll
+                for (uint32_t u = 0; u < 8; ++u) place += (uint32_t)(i + u < count) & (uint32_t)(other[u] > mine);
+            }
         }
         if (place >= g.n_top) continue;
         if (!whole) {
@@ -183,41 +243,69 @@ __device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, Pool& 
     }
 }
 
-// A workgroup takes a segment of a row, 256 * V entries at a time.
+// Entries c0 + (256 j + thread) * 8 ... of a row, 8 for each j, as they lie in memory; -inf from `end` on.
+template <typename T, int V>
+struct Entries {
+    static constexpr int WORDS = 8 * sizeof(T) / 16;   // of 16 bytes a run
+    uint4 raw[V / 8][WORDS];
+
+    __device__ void load(const T* x, uint32_t c0, uint32_t end) {
+        const uint32_t c = c0 + threadIdx.x * 8;
+        if (c0 + 256 * V <= end) {   // the loads of all runs are on their way at once
+#pragma unroll
+            for (int j = 0; j < V / 8; ++j) __builtin_memcpy(raw[j], x + c + j * 2048, sizeof(raw[j]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < V / 8; ++j) {
+                if (c + j * 2048 + 8 <= end) {
+                    __builtin_memcpy(raw[j], x + c + j * 2048, sizeof(raw[j]));
+                } else {
+                    T part[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) part[i] = c + j * 2048 + i < end ? x[c + j * 2048 + i] : (T)MINUS_INF;
+                    __builtin_memcpy(raw[j], part, sizeof(raw[j]));
+                }
+            }
+        }
+    }
+    __device__ void values(float (&v)[V]) const {
+#pragma unroll
+        for (int j = 0; j < V / 8; ++j) {
+            T part[8];
+            __builtin_memcpy(part, raw[j], sizeof(part));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j * 8 + i] = (float)part[i];
+        }
+    }
+};
+
+// A workgroup takes a segment of a row, 256 * V entries at a time.  (Loading the next ones ahead gained nothing: 2048 x 32000 bf16 without
+// alternatives 33.8 -> 35.5 us; 8 workgroups a CU have enough loads on their way.)
 template <typename T, int V>
 __global__ __launch_bounds__(256) void token_logprobs_kernel(LogprobArgs g) {
-    constexpr int RUN = 8;
-    __shared__ uint64_t pools[4][POOL], finals[4 * POOL];
+    __shared__ uint64_t pools[4][POOL], finals[4 * POOL + 8];
     __shared__ Totals totals;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t w = blockIdx.x, row = w / g.splits;
     const uint32_t begin = (uint32_t)(w % g.splits) * g.segment;
     const uint32_t end = g.vocab - begin < g.segment ? g.vocab : begin + g.segment;
     const T* x = (const T*)g.logits + row * g.stride;
+    const auto column = [&](uint32_t c0, int i) { return c0 + (i / 8 * 256 + threadIdx.x) * 8 + i % 8; };
     Sums z{MINUS_INF, 0.f, 0.f};
     Pool pool{pools[wave]};
     for (uint32_t c0 = begin; c0 < end; c0 += 256 * V) {
         float v[V];
-        if (c0 + 256 * V <= end) {   // the loads of all runs are on their way at once
+        Entries<T, V> entries;
+        entries.load(x, c0, end);
+        entries.values(v);
+        float peaks[4];
 #pragma unroll
-            for (int j = 0; j < V / RUN; ++j) load_run<T, RUN>(x + c0 + (j * 256 + threadIdx.x) * RUN, *(float(*)[RUN])(v + j * RUN));
-        } else {
+        for (int q = 0; q < 4; ++q) {
+            peaks[q] = v[q * (V / 4)];
 #pragma unroll
-            for (int j = 0; j < V / RUN; ++j) {
-                const uint32_t c = c0 + (j * 256 + threadIdx.x) * RUN;
-                float part[RUN];
-                if (c + RUN <= end) load_run<T, RUN>(x + c, part);
-                else
-#pragma unroll
-                    for (int i = 0; i < RUN; ++i) part[i] = c + i < end ? (float)x[c + i] : MINUS_INF;
-#pragma unroll
-                for (int i = 0; i < RUN; ++i) v[j * RUN + i] = part[i];
-            }
+            for (int i = 1; i < V / 4; ++i) peaks[q] = fmaxf(peaks[q], v[q * (V / 4) + i]);
         }
-        float peak = MINUS_INF;
-#pragma unroll
-        for (int i = 0; i < V; ++i) peak = fmaxf(peak, v[i]);
-        const float m = fmaxf(z.m, peak);
+        const float peak = fmaxf(fmaxf(peaks[0], peaks[1]), fmaxf(peaks[2], peaks[3])), m = fmaxf(z.m, peak);
         const float base = m == MINUS_INF ? 0.f : m;
         z = join(z, Sums{m, 0.f, 0.f});
 #pragma unroll
@@ -226,19 +314,38 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(LogprobArgs g) {
             z.s += e;
             z.t = fmaf(e, fmaxf(d, -1000.f), z.t);   // an entry of -inf adds 0, not 0 * inf; e^-1000 is 0 as well
         }
-        if (g.n_top && pool.raise(order_of(peak), g.n_top)) {
+        if (!g.n_top) continue;
+        const uint32_t orders[4] = {order_of(peaks[0]), order_of(peaks[1]), order_of(peaks[2]), order_of(peaks[3])};
+        if (!pool.raise(orders, g.n_top)) continue;
+        const float from = value_of(max(pool.bound, ORDER_FLOOR + 1));   // floats compare as their orders do
+        uint32_t n = V * __popcll(__ballot(peak >= from));   // at most, and counted where that is too many
+        if (pool.count + n > POOL) {
+            n = 0;
 #pragma unroll
-            for (int i = 0; i < V; ++i)   // floats compare as their orders do
-                pool.add(v[i] >= value_of(max(pool.bound, ORDER_FLOOR + 1)), key_of(order_of(v[i]), c0 + ((i / RUN) * 256 + threadIdx.x) * RUN + i % RUN), g.n_top, lane);
+            for (int i = 0; i < V; ++i) n += __popcll(__ballot(v[i] >= from));
+        }
+        if (pool.count + n <= POOL) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) pool.add(v[i] >= from, key_of(order_of(v[i]), column(c0, i)));
+            wave_sync();
+        } else {   // equal entries, or one lane's above all others: from memory again, with room made on the way
+#pragma unroll 1
+            for (int i = 0; i < V; ++i) {
+                const uint32_t c = column(c0, i);
+                const uint32_t order = c < end ? order_of((float)x[c]) : 0;
+                if (pool.count > POOL - 64) pool.compress(g.n_top, lane);
+                pool.add(order >= max(pool.bound, ORDER_FLOOR + 1), key_of(order, c));
+                wave_sync();
+            }
         }
     }
-    finish<T>(g, row, z, pool, finals, totals, g.splits == 1 ? ~0ull : w);
+    finish<T>(g, row, z, pool, pools[0], finals, totals, g.splits == 1 ? ~0ull : w);
 }
 
 // Joins the segments' parts of a row.
 template <typename T>
 __global__ __launch_bounds__(256) void join_logprobs_kernel(LogprobArgs g) {
-    __shared__ uint64_t pools[4][POOL], finals[4 * POOL];
+    __shared__ uint64_t pools[4][POOL], finals[4 * POOL + 8];
     __shared__ Totals totals;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t row = blockIdx.x;
@@ -250,16 +357,20 @@ __global__ __launch_bounds__(256) void join_logprobs_kernel(LogprobArgs g) {
     const uint32_t n = g.splits * g.n_top;
     for (uint32_t i = wave * 64; i < n; i += 256) {
         const uint64_t key = i + lane < n ? keys[i + lane] : 0;
-        if (pool.raise((uint32_t)(key >> 32), g.n_top)) pool.add(key && (uint32_t)(key >> 32) >= pool.bound, key, g.n_top, lane);
+        const uint32_t order = (uint32_t)(key >> 32), orders[4] = {order, 0, 0, 0};
+        if (!pool.raise(orders, g.n_top)) continue;
+        if (pool.count > POOL - 64) pool.compress(g.n_top, lane);
+        pool.add(order >= max(pool.bound, ORDER_FLOOR + 1), key);
+        wave_sync();
     }
-    finish<T>(g, row, z, pool, finals, totals, ~0ull);
+    finish<T>(g, row, z, pool, pools[0], finals, totals, ~0ull);
 }
 
 template <typename T>
 hipError_t launch_type(const LogprobArgs& g, hipStream_t stream) {
     const dim3 grid((uint32_t)(g.rows * g.splits));
     if (g.segment <= 2048) token_logprobs_kernel<T, 8><<<grid, dim3(256), 0, stream>>>(g);
-    else token_logprobs_kernel<T, 32><<<grid, dim3(256), 0, stream>>>(g);
+    else token_logprobs_kernel<T, 16><<<grid, dim3(256), 0, stream>>>(g);
     if (g.splits > 1) {
         hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
