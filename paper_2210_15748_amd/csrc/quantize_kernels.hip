@@ -4,6 +4,8 @@
 //                      in 32 bits would move some of them over a half)
 // each code the nearest integer to the real quotient, ties to even.  Bound by memory: rows are read once and kept in registers between the
 // reduction and the codes.  A row with an infinity or NaN gets codes 0 and scale NaN.
+#include <type_traits>
+
 #include "kernels.hpp"
 #include "number_formats.hpp"
 
@@ -11,70 +13,113 @@ namespace dessert {
 
 namespace {
 
-// What turns a row's numbers into codes: num / den, also as a 32-bit factor.
-struct Quotient {
-    double num, den;
-    float factor;
-    bool zero, fast;   // fast: the factor is good to 2^-23
+// What a row's elements are reduced to: the largest magnitude's bits, or the sum of the squares.  Bits order magnitudes as their
+// values, infinities and NaN above all; a sum of squares of 32-bit floats cannot overflow 64 bits.
+template <bool UNIT>
+struct Reduced {
+    using type = std::conditional_t<UNIT, double, uint32_t>;
+    type v = 0;
 
-    __device__ Quotient(float peak, double squares, bool bad, bool unit, float& scale) {
-        const double norm = sqrt(squares);
-        scale = bad ? __builtin_nanf("") : unit ? (float)(norm / 127.0) : peak / 127.f;
-        num = unit ? 127.0 : 1.0;
-        den = unit ? norm : (double)scale;
-        zero = bad || den == 0.0;
-        factor = zero ? 0.f : (float)(num / den);
-        fast = factor < 0x1p125f && factor > 0x1p-125f;
+    template <typename T>
+    __device__ void take(const T (&x)[8]) {
+        if constexpr (UNIT) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v = fma((double)(float)x[i], (double)(float)x[i], v);
+        } else if constexpr (sizeof(T) == 2) {   // two at a time
+            typedef uint16_t pair __attribute__((ext_vector_type(2)));
+            pair m[4];
+            __builtin_memcpy(m, x, 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m[i] &= (uint16_t)0x7FFF;
+            const pair p = __builtin_elementwise_max(__builtin_elementwise_max(m[0], m[1]), __builtin_elementwise_max(m[2], m[3]));
+            v = max(v, (uint32_t)max(p.x, p.y));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v = max(v, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+        }
     }
-    // The factor is off by 2^-24 and the product by as much, of at most 127: less than 2^-15.  Where that could matter, next to a half,
-    // the quotient is formed in 64 bits: num * x is exact there, and a quotient of such numbers that is no half is further than its
-    // rounding away from one.
-    __device__ int code(float x) const {
-        if (zero) return 0;
-        const float t = x * factor;
-        float n = rintf(t);
-        if (!fast || fabsf(fabsf(t - n) - 0.5f) < 0x1p-14f) n = (float)rint(num * (double)x / den);
-        return (int)fminf(fmaxf(n, -127.f), 127.f);
+    __device__ void join(type o) {
+        if constexpr (UNIT) v += o;
+        else v = max(v, o);
+    }
+    // over the G consecutive lanes of a row (a power of two)
+    template <int G>
+    __device__ void join_lanes() {
+#pragma unroll
+        for (int o = 1; o < (G < 64 ? G : 64); o *= 2) join(__shfl_xor(v, o));
+        if constexpr (G > 64) {
+            __shared__ type parts[G / 64];
+            if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = v;
+            __syncthreads();
+            v = parts[0];
+#pragma unroll
+            for (int w = 1; w < G / 64; ++w) join(parts[w]);
+        }
     }
 };
 
-// Over the lanes of a row: G consecutive lanes (a power of two).
-template <int G>
-__device__ inline void reduce_row(float& peak, double& squares, bool& bad) {
-    float b = bad ? 1.f : 0.f;
-#pragma unroll
-    for (int o = 1; o < (G < 64 ? G : 64); o *= 2) {
-        peak = fmaxf(peak, __shfl_xor(peak, o));
-        squares += __shfl_xor(squares, o);
-        b = fmaxf(b, __shfl_xor(b, o));
-    }
-    if constexpr (G > 64) {
-        __shared__ float s_peak[G / 64], s_bad[G / 64];
-        __shared__ double s_squares[G / 64];
-        if ((threadIdx.x & 63) == 0) {
-            s_peak[threadIdx.x >> 6] = peak;
-            s_bad[threadIdx.x >> 6] = b;
-            s_squares[threadIdx.x >> 6] = squares;
-        }
-        __syncthreads();
-        peak = b = 0.f;
-        squares = 0.0;
-#pragma unroll
-        for (int w = 0; w < G / 64; ++w) {
-            peak = fmaxf(peak, s_peak[w]);
-            b = fmaxf(b, s_bad[w]);
-            squares += s_squares[w];
-        }
-    }
-    bad = b != 0.f;
-}
+// What turns a row's numbers into codes.
+template <typename T, bool UNIT>
+struct Quotient {
+    double num, den;          // a code is num * x / den
+    float factor, scale;      // factor: num / den to 2^-23, or 0
+    bool none;                // all codes are 0
 
-template <bool UNIT>
-__device__ inline void take(float x, float& peak, double& squares, bool& bad) {
-    bad = bad || !(fabsf(x) <= 3.402823466e38f);
-    if constexpr (UNIT) squares = fma((double)x, (double)x, squares);
-    else peak = fmaxf(peak, fabsf(x));
-}
+    __device__ Quotient() {}
+    __device__ explicit Quotient(typename Reduced<UNIT>::type v) {
+        if constexpr (UNIT) {
+            const double norm = sqrt(v);
+            num = 127.0;
+            den = norm;
+            scale = v < __builtin_huge_val() ? (float)(norm / 127.0) : __builtin_nanf("");
+            factor = 127.f / (float)norm;
+        } else {
+            float peak;
+            if constexpr (sizeof(T) == 2) {
+                const uint16_t bits = (uint16_t)v;
+                T x;
+                __builtin_memcpy(&x, &bits, 2);
+                peak = (float)x;
+            } else {
+                peak = __uint_as_float(v);
+            }
+            scale = peak < __builtin_huge_valf() ? peak / 127.f : __builtin_nanf("");
+            num = 1.0;
+            den = scale;
+            factor = 1.f / scale;
+        }
+        none = !(den > 0.0 && scale == scale);
+    }
+    // The factor is off by at most 2^-23 and the product with it by 2^-24, of at most 127: less than 2^-15.  A product that close to a half, and all of
+    // a row whose factor is no ordinary number, are compared with the half in 64 bits instead: num * x is exact there.
+    __device__ uint64_t codes(const T (&x)[8]) const {
+        constexpr float MAGIC = 12582912.f;   // 1.5 * 2^23: a sum with it is rounded to a whole number, whose last bits it holds
+        uint32_t n[8];
+        float off = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float t = (float)x[i] * factor, m = t + MAGIC;
+            n[i] = __float_as_uint(m);
+            off = fmaxf(off, fabsf(t - (m - MAGIC)));
+        }
+        if (off > 0.5f - 0x1p-14f || !(factor < 0x1p125f && factor > 0x1p-125f)) {
+            const double wide = none ? 0.0 : num / den;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float y = (float)x[i];
+                asm volatile("" : "+v"(y));   // converted here, not kept in 64 bits since the sum of squares
+                const double a = num * (double)y, below = floor((double)y * wide);
+                const double over = fma(-(below + 0.5), den, a);   // a against the half above `below`: its sign is exact
+                const int b = (int)fmin(fmax(below, -128.0), 127.0);
+                const int q = over > 0.0 || (over == 0.0 && (b & 1)) ? b + 1 : b;
+                n[i] = none ? 0 : (uint32_t)min(max(q, -127), 127);
+            }
+        }
+        uint32_t lo = __builtin_amdgcn_perm(n[1], n[0], 0x0C0C0400) | __builtin_amdgcn_perm(n[3], n[2], 0x04000C0C);
+        uint32_t hi = __builtin_amdgcn_perm(n[5], n[4], 0x0C0C0400) | __builtin_amdgcn_perm(n[7], n[6], 0x04000C0C);
+        return (uint64_t)hi << 32 | lo;
+    }
+};
 
 // 8 elements of a row from column c on; 0 behind the end.
 template <typename T>
@@ -85,77 +130,77 @@ __device__ inline void load_eight(const T* row, uint32_t c, uint32_t cols, T (&v
         for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? row[c + i] : (T)0.f;
 }
 
-__device__ inline void store_eight(int8_t* row, uint32_t c, uint32_t cols, const int8_t (&q)[8]) {
-    if (c + 8 <= cols) __builtin_memcpy(row + c, q, 8);
+__device__ inline void store_eight(int8_t* row, uint32_t c, uint32_t cols, uint64_t q) {
+    if (c + 8 <= cols) __builtin_memcpy(row + c, &q, 8);
     else
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c + i < cols) row[c + i] = q[i];
+            if (c + i < cols) row[c + i] = (int8_t)(q >> 8 * i);
 }
 
 // G lanes a row, RUNS runs of 8 elements a lane (cols <= 8 G RUNS), ROWS rows a group of lanes one after the other, all loaded at once.
+// With several rows a lane sees to the root and the quotients of one of them (64-bit operations: a third of the time of short rows
+// when every lane formed them for every row).
 template <typename T, int G, int RUNS, int ROWS, bool UNIT>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict__ x, uint64_t rows, uint32_t cols, uint64_t stride,
                                                             int8_t* __restrict__ codes, float* __restrict__ scales) {
     static_assert(G <= 64 || ROWS == 1, "one row a workgroup where its waves share it");
     constexpr int PER = 256 / G;
     const uint32_t at = threadIdx.x % G;
+    const uint64_t first = (uint64_t)blockIdx.x * ROWS * PER + threadIdx.x / G;
     T v[ROWS][RUNS][8];
 #pragma unroll
-    for (int k = 0; k < ROWS; ++k) {
-        const uint64_t r = ((uint64_t)blockIdx.x * ROWS + k) * PER + threadIdx.x / G;
+    for (int k = 0; k < ROWS; ++k)
 #pragma unroll
-        for (int j = 0; j < RUNS; ++j) load_eight(x + min(r, rows - 1) * stride, (j * G + at) * 8, cols, v[k][j]);
+        for (int j = 0; j < RUNS; ++j) load_eight(x + min(first + k * PER, rows - 1) * stride, (j * G + at) * 8, cols, v[k][j]);
+    Reduced<UNIT> reduced[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+#pragma unroll
+        for (int j = 0; j < RUNS; ++j) reduced[k].take(v[k][j]);
+        reduced[k].template join_lanes<G>();
     }
+    typename Reduced<UNIT>::type own = reduced[0].v;
+#pragma unroll
+    for (int k = 1; k < ROWS; ++k)
+        if (at % ROWS == k) own = reduced[k].v;
+    const Quotient<T, UNIT> mine(own);
 #pragma unroll
     for (int k = 0; k < ROWS; ++k) {
-        const uint64_t r = ((uint64_t)blockIdx.x * ROWS + k) * PER + threadIdx.x / G;
-        float peak = 0.f, scale;
-        double squares = 0.0;
-        bool bad = false;
-#pragma unroll
-        for (int j = 0; j < RUNS; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) take<UNIT>((float)v[k][j][i], peak, squares, bad);
-        reduce_row<G>(peak, squares, bad);
-        const Quotient quotient(peak, squares, bad, UNIT, scale);
-        if (r >= rows) continue;
-        if (at == 0) scales[r] = scale;
-#pragma unroll
-        for (int j = 0; j < RUNS; ++j) {
-            int8_t q[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = (int8_t)quotient.code((float)v[k][j][i]);
-            store_eight(codes + r * cols, (j * G + at) * 8, cols, q);
+        Quotient<T, UNIT> quotient = mine;
+        if constexpr (ROWS > 1) {
+            const int from = (int)((threadIdx.x & 63) / G * G) + k;
+            quotient.den = __shfl(mine.den, from);
+            quotient.factor = __shfl(mine.factor, from);
+            quotient.none = __shfl((int)mine.none, from);
         }
+        const uint64_t r = first + k * PER;
+        if (r >= rows) continue;
+        if (at == k) scales[r] = mine.scale;
+#pragma unroll
+        for (int j = 0; j < RUNS; ++j) store_eight(codes + r * cols, (j * G + at) * 8, cols, quotient.codes(v[k][j]));
     }
 }
 
 // Longer rows: a workgroup a row, read twice (the second time from the caches).
 template <typename T, bool UNIT>
-__global__ __launch_bounds__(256) void quantize_long_rows_kernel(const T* __restrict__ x, uint32_t cols, uint64_t stride,
-                                                                 int8_t* __restrict__ codes, float* __restrict__ scales) {
+__global__ __launch_bounds__(1024) void quantize_long_rows_kernel(const T* __restrict__ x, uint32_t cols, uint64_t stride,
+                                                                  int8_t* __restrict__ codes, float* __restrict__ scales) {
     const uint64_t r = blockIdx.x;
     const T* row = x + r * stride;
-    float peak = 0.f, scale;
-    double squares = 0.0;
-    bool bad = false;
-    for (uint32_t c = threadIdx.x * 8; c < cols; c += 2048) {
+    Reduced<UNIT> reduced;
+    for (uint32_t c = threadIdx.x * 8; c < cols; c += 8192) {
         T v[8];
         load_eight(row, c, cols, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) take<UNIT>((float)v[i], peak, squares, bad);
+        reduced.take(v);
     }
-    reduce_row<256>(peak, squares, bad);
-    const Quotient quotient(peak, squares, bad, UNIT, scale);
-    if (threadIdx.x == 0) scales[r] = scale;
-    for (uint32_t c = threadIdx.x * 8; c < cols; c += 2048) {
+    reduced.template join_lanes<1024>();
+    const Quotient<T, UNIT> quotient(reduced.v);
+    if (threadIdx.x == 0) scales[r] = quotient.scale;
+    for (uint32_t c = threadIdx.x * 8; c < cols; c += 8192) {
         T v[8];
         load_eight(row, c, cols, v);
-        int8_t q[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = (int8_t)quotient.code((float)v[i]);
-        store_eight(codes + r * cols, c, cols, q);
+        store_eight(codes + r * cols, c, cols, quotient.codes(v));
     }
 }
 
@@ -179,7 +224,7 @@ hipError_t launch_type(const void* data, uint64_t rows, uint32_t cols, uint64_t 
     else if (cols <= 2048) launch_shape<T, 256, 1, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
     else if (cols <= 4096) launch_shape<T, 256, 2, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
     else if (cols <= 8192) launch_shape<T, 256, 4, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
-    else quantize_long_rows_kernel<T, UNIT><<<dim3((uint32_t)rows), dim3(256), 0, stream>>>(x, cols, stride, codes, scales);
+    else quantize_long_rows_kernel<T, UNIT><<<dim3((uint32_t)rows), dim3(1024), 0, stream>>>(x, cols, stride, codes, scales);
     return hipGetLastError();
 }
 
