@@ -7,6 +7,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -1420,9 +1421,9 @@ dessert_status_t dessert_token_logprobs(const dessert_index_t* ix, const void* l
 }
 
 namespace {
-// The head form goes through the rows in turns whose 32-bit logits fit this much: they then stay in the 256 MB cache
-// between the product that writes them and the pass that reads them.
-constexpr size_t HEAD_LOGITS_BYTES = 96u << 20;
+// The head form goes through the rows in turns: a product that writes the turn's 32-bit logits, a pass that reads them while they still
+// lie in the 256 MB cache (4096 x 32000 x 2048 with 64 / 128 / 256 / 600 MB of logits a turn: 511 / 416 / 419 / 456 us).
+constexpr size_t HEAD_LOGITS_BYTES = 256u << 20;
 struct HeadPlan {
     uint64_t rows;     // of a turn
     uint64_t stride;   // floats from row to row
@@ -1432,8 +1433,19 @@ struct HeadPlan {
 HeadPlan head_plan(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
     HeadPlan h{};
     h.stride = ((uint64_t)vocab + 31) / 32 * 32;
-    h.rows = HEAD_LOGITS_BYTES / 4 / h.stride;
-    h.rows = h.rows < 256 ? 256 : h.rows / 256 * 256;
+    // Of the numbers of rows that fit, the one with the least time a row: whole rounds of 256 x 256 tiles over the 256 CUs, a third of a
+    // round's time for each 256 tiles' worth of logits to read, and a seventh for two launches.
+    const uint64_t across = (vocab + 255) / 256, most = std::min<uint64_t>((rows + 255) / 256, HEAD_LOGITS_BYTES / (1024 * h.stride));
+    double best = 1e30;
+    h.rows = 256;
+    for (uint64_t n = 1; n <= most && n <= 4096; ++n) {
+        const uint64_t tiles = n * across, rounds = (tiles + 255) / 256;
+        const double cost = (rounds + 0.35 * tiles / 256 + 0.15) / n;
+        if (cost < best * 0.999) {
+            best = cost;
+            h.rows = n * 256;
+        }
+    }
     if (h.rows > rows) h.rows = rows;
     h.pass = logprob_plan(h.rows, vocab, n_top);
     h.logits_bytes = align_up((size_t)h.rows * h.stride * 4, 256);

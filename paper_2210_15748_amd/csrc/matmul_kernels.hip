@@ -11,44 +11,57 @@ namespace dessert {
 
 namespace {
 
-constexpr int STEP = 128;   // columns (bytes) of a row per round of the tile kernel: one line of 128 bytes
+constexpr int LINE = 128;   // bytes
 
 // ---- tiles ------------------------------------------------------------------------------------------------------------------
-// A workgroup of WM x WN waves goes through tiles of TM tokens x TN channels, 128 columns a step.  A step's rows lie in LDS, 128
-// bytes each, double-buffered: while the waves multiply one step, the next one is on its way, across the border between two tiles
+// A workgroup of WM x WN waves goes through tiles of TM tokens x TN channels, STEP columns a step.  A step's rows lie in LDS,
+// double-buffered: while the waves multiply one step, the next one is on its way, across the border between two tiles
 // too, so that a tile's results leave while the next tile's first columns arrive.  Rows whose bytes are 16-byte aligned (ALIGNED)
 // go from memory to LDS directly; others through registers.
 //
 // The buffers are four arrays by name and the two steps of a round stand one after the other in the code: the compiler then knows
 // that reads of one buffer do not wait for what is arriving in the other.  The products appear once per buffer and nowhere else
 // (no tail outside the loop): a second copy of the accumulators would not fit the registers.
-template <int TM_, int TN_, int WM_, int WN_, bool ALIGNED_>
+template <int TM_, int TN_, int WM_, int WN_, int STEP_, bool ALIGNED_>
 struct Tile {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_;
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, STEP = STEP_;
     static constexpr bool ALIGNED = ALIGNED_;
     static constexpr int W = WM * WN;
     static constexpr int FM = TM / WM / 16, FQ = TN / WN / 64;   // a wave's fragments: of 16 tokens, and 4 x 16 channels
-    static constexpr int LA = TM / 8 / W, LB = TN / 8 / W;       // 1 KB pieces (8 rows) that a wave fetches per step
+    static constexpr int PARTS = STEP / 16, ROWS = 64 / PARTS;   // 16-byte parts of a row; rows in a piece of 1 KB, which a wave fetches at a time
+    static constexpr int LA = TM / ROWS / W, LB = TN / ROWS / W; // pieces that a wave fetches per step
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
 // 16 bytes of a row from column c on; columns from k on read as zero.
 __device__ inline v4i load_chunk(const int8_t* row, uint32_t c, uint32_t k) {
-    v4i v = {0, 0, 0, 0};
-    if (c + 16 <= k) {
-        __builtin_memcpy(&v, row + c, 16);
+    uint64_t lo = 0, hi = 0;
+    if (c < k && k >= 16) {   // where the row ends within them: its last 16 bytes, the first ones shifted out
+        const uint32_t at = min(c, k - 16), out = (c - at) * 8;   // bits, 0 to 120
+        __builtin_memcpy(&lo, row + at, 8);
+        __builtin_memcpy(&hi, row + at + 8, 8);
+        if (out >= 64) {
+            lo = hi >> (out - 64);
+            hi = 0;
+        } else if (out) {
+            lo = lo >> out | hi << (64 - out);
+            hi >>= out;
+        }
     } else if (c < k) {
-        int8_t bytes[16];
-#pragma unroll
-        for (uint32_t i = 0; i < 16; ++i) bytes[i] = c + i < k ? row[c + i] : (int8_t)0;
-        __builtin_memcpy(&v, bytes, 16);
+#pragma unroll 1
+        for (uint32_t i = 0; i < k - c; ++i) {
+            const uint64_t byte = (uint8_t)row[c + i];
+            if (i < 8) lo |= byte << 8 * i;
+            else hi |= byte << 8 * (i - 8);
+        }
     }
+    const v4i v = {(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
     return v;
 }
 
 __device__ inline v4i mfma(v4i x, v4i y, v4i acc) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, acc, 0, 0, 0); }
 
-// In LDS the 16-byte parts of a row's 128 bytes are permuted by a key of the row (part ^ key), so that the 8 lanes that read
+// In LDS the 16-byte parts of each 128 bytes of a row are permuted by a key of the row (part ^ key), so that the 8 lanes that read
 // together, same part of 8 rows, meet 8 different groups of banks (SQ_LDS_BANK_CONFLICT 0).
 __device__ inline uint32_t row_key(uint32_t row) { return row & 7; }
 // Workgroups go to the 8 dies in turn, each of which has an L2 of its own: a die takes tiles side by side, in bands of 4 rows of tiles.
@@ -75,8 +88,8 @@ struct Source {
     offset oa[G::LA], ob[G::LB];          // a lane's 16 bytes within the tile's rows, of step 0
     v4i va[G::ALIGNED ? 1 : G::LA], vb[G::ALIGNED ? 1 : G::LB];
 
-    __device__ uint32_t row_of(int j) const { return (j * G::W + wave) * 8 + lane / 8; }
-    __device__ uint32_t part() const { return (lane & 7) ^ row_key(lane / 8); }   // of any j: rows of a piece begin at a multiple of 8
+    __device__ uint32_t row_of(int j) const { return (j * G::W + wave) * G::ROWS + lane / G::PARTS; }
+    __device__ uint32_t part(int j) const { return lane % G::PARTS ^ row_key(row_of(j)); }
 
     __device__ void aim() {
         uint32_t tm, tn;
@@ -87,9 +100,9 @@ struct Source {
         pb = g.b + n0 * g.ldb;
         // rows past the last one: the last one again (their results are not stored)
 #pragma unroll
-        for (int j = 0; j < G::LA; ++j) oa[j] = min(row_of(j), last_a) * (offset)g.lda + part() * 16;
+        for (int j = 0; j < G::LA; ++j) oa[j] = min(row_of(j), last_a) * (offset)g.lda + part(j) * 16;
 #pragma unroll
-        for (int j = 0; j < G::LB; ++j) ob[j] = min(row_of(j), last_b) * (offset)g.ldb + part() * 16;
+        for (int j = 0; j < G::LB; ++j) ob[j] = min(row_of(j), last_b) * (offset)g.ldb + part(j) * 16;
         if constexpr (G::ALIGNED) {
             ra = __builtin_amdgcn_make_buffer_rsrc((void*)pa, 0, last_a * (uint32_t)g.lda + g.k, 0x00020000);
             rb = __builtin_amdgcn_make_buffer_rsrc((void*)pb, 0, last_b * (uint32_t)g.ldb + g.k, 0x00020000);
@@ -98,30 +111,37 @@ struct Source {
     }
     // The last step, if the columns end within it: lanes whose part lies behind the end read the step's first part instead.
     __device__ void fold() {
-        const uint32_t left = g.k - (steps - 1) * STEP;
-        if (left == STEP) return;
+        const uint32_t left = g.k - (steps - 1) * G::STEP;
+        if (left == G::STEP) return;
 #pragma unroll
         for (int j = 0; j < G::LA; ++j)
-            if (part() * 16 >= left) oa[j] -= part() * 16;
+            if (part(j) * 16 >= left) oa[j] -= part(j) * 16;
 #pragma unroll
         for (int j = 0; j < G::LB; ++j)
-            if (part() * 16 >= left) ob[j] -= part() * 16;
+            if (part(j) * 16 >= left) ob[j] -= part(j) * 16;
     }
     // Start the transfer of a step (ALIGNED: to LDS; otherwise into registers, for land()).
     __device__ void fetch(int8_t* a, int8_t* b) {
         if constexpr (G::ALIGNED) {
 #pragma unroll
             for (int j = 0; j < G::LA; ++j)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte*)(a + (j * G::W + wave) * 1024), 16, oa[j], step * STEP, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte*)(a + (j * G::W + wave) * 1024), 16, oa[j], step * G::STEP, 0, 0);
 #pragma unroll
             for (int j = 0; j < G::LB; ++j)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte*)(b + (j * G::W + wave) * 1024), 16, ob[j], step * STEP, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_byte*)(b + (j * G::W + wave) * 1024), 16, ob[j], step * G::STEP, 0, 0);
         } else {
-            const uint32_t c = step * STEP;
+            const uint32_t c = step * G::STEP;
+            if (c + G::STEP <= g.k) {   // one branch for all of a step's loads, which then are on their way together
 #pragma unroll
-            for (int j = 0; j < G::LA; ++j) va[j] = load_chunk(pa + (oa[j] - part() * 16), c + part() * 16, g.k);
+                for (int j = 0; j < G::LA; ++j) __builtin_memcpy(&va[j], pa + oa[j] + c, 16);
 #pragma unroll
-            for (int j = 0; j < G::LB; ++j) vb[j] = load_chunk(pb + (ob[j] - part() * 16), c + part() * 16, g.k);
+                for (int j = 0; j < G::LB; ++j) __builtin_memcpy(&vb[j], pb + ob[j] + c, 16);
+            } else {
+#pragma unroll
+                for (int j = 0; j < G::LA; ++j) va[j] = load_chunk(pa + (oa[j] - part(j) * 16), c + part(j) * 16, g.k);
+#pragma unroll
+                for (int j = 0; j < G::LB; ++j) vb[j] = load_chunk(pb + (ob[j] - part(j) * 16), c + part(j) * 16, g.k);
+            }
         }
     }
     __device__ void land(int8_t* a, int8_t* b) {
@@ -145,33 +165,33 @@ struct Source {
     // Before a step is multiplied, where the columns end within it: zeros for the tokens' parts behind the end, by the wave that
     // fetched them (the channels' may hold anything then).
     __device__ void clear_tail(int8_t* a) const {
-        const uint32_t left = g.k - (steps - 1) * STEP;
+        const uint32_t left = g.k - (steps - 1) * G::STEP;
         __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): the transfers to LDS have landed
 #pragma unroll
         for (int j = 0; j < G::LA; ++j)
-            if (part() * 16 >= left) *(v4i*)(a + (j * G::W + wave) * 1024 + lane * 16) = v4i{0, 0, 0, 0};
+            if (part(j) * 16 >= left) *(v4i*)(a + (j * G::W + wave) * 1024 + lane * 16) = v4i{0, 0, 0, 0};
     }
 };
 
 // The products of one step.
 template <typename G>
 __device__ inline void multiply_step(v4i (&acc)[G::FM][G::FQ][4], const int8_t* a, const int8_t* b, uint32_t wm, uint32_t wn, uint32_t lane) {
-    constexpr int R = G::FM + G::FQ * 4, M = G::FM * G::FQ * 4, V = G::LA + G::LB;
+    constexpr int R = G::FM + G::FQ * 4, M = G::FM * G::FQ * 4, V = G::LA + G::LB, PIECES = G::STEP / 64;
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
+    for (int kk = 0; kk < PIECES; ++kk) {
         v4i tok[G::FM], ch[G::FQ][4];
 #pragma unroll
         for (int f = 0; f < G::FM; ++f) {
             const uint32_t row = wm + f * 16 + lane % 16;
-            tok[f] = *(const v4i*)(a + row * STEP + ((kk * 4 + lane / 16) ^ row_key(row)) * 16);
+            tok[f] = *(const v4i*)(a + row * G::STEP + ((kk * 4 + lane / 16) ^ row_key(row)) * 16);
         }
 #pragma unroll
         for (int q = 0; q < G::FQ; ++q)
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
                 const uint32_t row = wn + q * 64 + f * 16 + lane % 16;
-                ch[q][f] = *(const v4i*)(b + row * STEP + ((kk * 4 + lane / 16) ^ row_key(row)) * 16);
+                ch[q][f] = *(const v4i*)(b + row * G::STEP + ((kk * 4 + lane / 16) ^ row_key(row)) * 16);
             }
 #pragma unroll
         for (int fm = 0; fm < G::FM; ++fm)
@@ -181,17 +201,19 @@ __device__ inline void multiply_step(v4i (&acc)[G::FM][G::FQ][4], const int8_t* 
                 for (int f = 0; f < 4; ++f) acc[fm][q][f] = mfma(ch[q][f], tok[fm], acc[fm][q][f]);
     }
     if constexpr (G::ALIGNED) {
-        // Order: the first half's reads; its products with the second half's reads and the next step's transfers between them (a
-        // burst of transfers at the step's start held the products up: 8192^3 486 -> 427 us with this and the rounds over tiles);
-        // the second half's products.
-        constexpr int N = M < 8 ? M : 8;
+        // Order: the reads of the first 64 columns; products with the next columns' reads between them, and in the first half of
+        // the step the next step's transfers (a burst of transfers at the step's start held the products up: 8192^3 486 -> 427 us
+        // with this and the rounds over tiles).
+        constexpr int N = M < 8 ? M : 8, SPREAD = (PIECES / 2) * N;
         __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, M / N, 0);
-            __builtin_amdgcn_sched_group_barrier(0x020, (V + N - 1) / N, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, (R + N - 1) / N, 0);
-        }
+        for (int kk = 0; kk < PIECES - 1; ++kk)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, M / N, 0);
+                if (kk < PIECES / 2) __builtin_amdgcn_sched_group_barrier(0x020, (V + SPREAD - 1) / SPREAD, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, (R + N - 1) / N, 0);
+            }
         __builtin_amdgcn_sched_group_barrier(0x008, M, 0);
     }
     __builtin_amdgcn_s_setprio(0);
@@ -257,12 +279,12 @@ __device__ inline void store_tile(const MatmulArgs& g, v4i (&acc)[G::FM][G::FQ][
 template <typename T, typename G>
 __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __shared__ __align__(16) int8_t a0[G::TM * STEP], b0[G::TN * STEP], a1[G::TM * STEP], b1[G::TN * STEP];
+    __shared__ __align__(16) int8_t a0[G::TM * G::STEP], b0[G::TN * G::STEP], a1[G::TM * G::STEP], b1[G::TN * G::STEP];
     __shared__ __align__(16) float turns[G::W][16 * 64];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave % G::WM * (G::TM / G::WM), wn = wave / G::WM * (G::TN / G::WN);
-    const uint32_t tiles = g.tiles_m * g.tiles_n, steps = (g.k + STEP - 1) / STEP;
-    const bool partial = G::ALIGNED && g.k % STEP != 0;
+    const uint32_t tiles = g.tiles_m * g.tiles_n, steps = (g.k + G::STEP - 1) / G::STEP;
+    const bool partial = G::ALIGNED && g.k % G::STEP != 0;
     Source<G> src{g, tiles, steps, lane, wave, blockIdx.x};
     src.aim();
     v4i acc[G::FM][G::FQ][4] = {};
@@ -320,13 +342,13 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 #pragma unroll
     for (int f = 0; f < MT; ++f) row_a[f] = g.a + min((uint64_t)(f * 16 + lane % 16), g.m - 1) * g.lda;
     v4i acc[MT] = {};
-    for (uint32_t c0 = wave % KS * STEP; c0 < g.k; c0 += KS * STEP * AHEAD) {
+    for (uint32_t c0 = wave % KS * LINE; c0 < g.k; c0 += KS * LINE * AHEAD) {
         v4i ch[AHEAD][2], tok[AHEAD][2][MT];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint32_t c = c0 + u * KS * STEP + h * 64 + lane / 16 * 16;
+                const uint32_t c = c0 + u * KS * LINE + h * 64 + lane / 16 * 16;
                 if constexpr (ALIGNED) {   // columns behind the end: any channels' bytes, times zeros
                     const bool in = c < g.k;
                     const uint32_t at = in ? c : 0;
@@ -336,6 +358,10 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
                         const v4i v = *(const v4i*)(row_a[f] + at);
                         tok[u][h][f] = in ? v : v4i{0, 0, 0, 0};
                     }
+                } else if (c0 + (AHEAD - 1) * KS * LINE + LINE <= g.k) {
+                    __builtin_memcpy(&ch[u][h], row_b + c, 16);
+#pragma unroll
+                    for (int f = 0; f < MT; ++f) __builtin_memcpy(&tok[u][h][f], row_a[f] + c, 16);
                 } else {
                     ch[u][h] = load_chunk(row_b, c, g.k);
 #pragma unroll
@@ -386,7 +412,7 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 
 template <typename T, int MT, bool ALIGNED>
 hipError_t launch_few(const MatmulArgs& g, hipStream_t stream) {
-    const uint32_t steps = (g.k + STEP - 1) / STEP;
+    const uint32_t steps = (g.k + LINE - 1) / LINE;
     const uint64_t groups = (g.n + 15) / 16;
     const auto grid = [&](int ks) { return dim3((uint32_t)((groups + 8 / ks - 1) / (8 / ks))); };
     if (steps >= 16 || (steps >= 8 && groups < 512)) scaled_matmul_few_kernel<T, MT, 8, ALIGNED><<<grid(8), dim3(512), 0, stream>>>(g);
@@ -401,7 +427,7 @@ hipError_t launch_tile_shape(MatmulArgs g, hipStream_t stream) {
     g.tiles_m = (uint32_t)tm;
     g.tiles_n = (uint32_t)tn;
     // as many workgroups as the 256 CUs, with 160 KB of LDS each, hold at once
-    const uint64_t most = 256 * (163840 / (2 * (G::TM + G::TN) * STEP + G::W * 4096));
+    const uint64_t most = 256 * (163840 / (2 * (G::TM + G::TN) * G::STEP + G::W * 4096));
     const uint64_t tiles = tm * tn;
     scaled_matmul_kernel<T, G><<<dim3((uint32_t)(tiles < most ? tiles : most)), dim3(64 * G::W), 0, stream>>>(g);
     return hipGetLastError();
@@ -411,9 +437,17 @@ template <typename T, bool ALIGNED>
 hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
     const uint64_t large = ((g.m + 255) / 256) * ((g.n + 255) / 256), middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
     if constexpr (ALIGNED)
-        if (large >= 128) return launch_tile_shape<T, Tile<256, 256, 4, 2, true>>(g, stream);
-    if (middle >= 192) return launch_tile_shape<T, Tile<128, 128, 2, 2, ALIGNED>>(g, stream);
-    return launch_tile_shape<T, Tile<64, 64, 4, 1, ALIGNED>>(g, stream);
+        if (large >= 128) return launch_tile_shape<T, Tile<256, 256, 4, 2, 128, true>>(g, stream);
+    if (middle >= 192) return launch_tile_shape<T, Tile<128, 128, 2, 2, 128, ALIGNED>>(g, stream);
+    // Small tiles wait for memory once a step: longer steps where there are columns for them, the longest (a workgroup a CU) where there
+    // are no more tiles than CUs.  128 / 256 / 512 columns: 128 x 4096 x 4096 24.8 / 16.6 / 14.3 us, 256 x 8192 x 8192 50.6 / 40.0 / 47.6,
+    // 256 x 1024 x 1024 6.8 / 6.1 / 6.5.  Through registers they pay no more: 1111 x 1003 x 1029 15.6 / 17.4.
+    if constexpr (ALIGNED) {
+        const uint64_t small = ((g.m + 63) / 64) * ((g.n + 63) / 64);
+        if (g.k >= 2048 && small <= 256) return launch_tile_shape<T, Tile<64, 64, 4, 1, 512, true>>(g, stream);
+        if (g.k > 256) return launch_tile_shape<T, Tile<64, 64, 4, 1, 256, true>>(g, stream);
+    }
+    return launch_tile_shape<T, Tile<64, 64, 4, 1, 128, ALIGNED>>(g, stream);
 }
 
 template <typename T>

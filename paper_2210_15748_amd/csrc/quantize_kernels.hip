@@ -216,9 +216,9 @@ template <typename T, bool UNIT>
 hipError_t launch_type(const void* data, uint64_t rows, uint32_t cols, uint64_t stride, int8_t* codes, float* scales, hipStream_t stream) {
     const T* x = (const T*)data;
     const bool many = rows >= 65536;
-    if (cols <= 128 && many) launch_shape<T, 16, 1, 4, UNIT>(x, rows, cols, stride, codes, scales, stream);
+    if (cols <= 128 && many) launch_shape<T, 16, 1, UNIT ? 2 : 4, UNIT>(x, rows, cols, stride, codes, scales, stream);
     else if (cols <= 128) launch_shape<T, 16, 1, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
-    else if (cols <= 512 && many) launch_shape<T, 64, 1, 4, UNIT>(x, rows, cols, stride, codes, scales, stream);
+    else if (cols <= 512 && many) launch_shape<T, 64, 1, UNIT ? 2 : 4, UNIT>(x, rows, cols, stride, codes, scales, stream);
     else if (cols <= 512) launch_shape<T, 64, 1, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
     else if (cols <= 1024) launch_shape<T, 64, 2, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
     else if (cols <= 2048) launch_shape<T, 256, 1, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
