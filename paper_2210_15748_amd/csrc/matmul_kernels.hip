@@ -230,6 +230,8 @@ __device__ inline void wave_sync() {
 template <typename T, typename G>
 __device__ inline void store_tile(const MatmulArgs& g, v4i (&acc)[G::FM][G::FQ][4], float* turn, uint64_t m0, uint64_t n0, uint32_t lane) {
     constexpr int RUN = 16 / sizeof(T), PARTS = RUN / 4, LANES = 64 / RUN, ROWS = 64 / LANES;   // channels a lane, lanes a token
+    static_assert(G::FM * 16 <= 64, "a lane holds the scale of one of the wave's tokens");
+    const float own = g.sa[min(m0 + lane % (G::FM * 16), g.m - 1)];   // (read where it was used, it was waited for eight times a tile)
 #pragma unroll
     for (int q = 0; q < G::FQ; ++q) {
         const uint64_t channel = n0 + q * 64 + lane % LANES * RUN;
@@ -254,8 +256,8 @@ __device__ inline void store_tile(const MatmulArgs& g, v4i (&acc)[G::FM][G::FQ][
             for (int r = 0; r < 16; r += ROWS) {
                 const uint32_t row = r + lane / LANES;
                 const uint64_t token = m0 + fm * 16 + row;
+                const float sa = __shfl(own, fm * 16 + row);
                 if (token < g.m) {
-                    const float sa = g.sa[token];
                     float y[RUN];
 #pragma unroll
                     for (int p = 0; p < PARTS; ++p)
