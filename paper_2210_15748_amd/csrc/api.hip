@@ -1421,9 +1421,10 @@ dessert_status_t dessert_token_logprobs(const dessert_index_t* ix, const void* l
 }
 
 namespace {
-// The head form goes through the rows in turns: a product that writes the turn's 32-bit logits, a pass that reads them while they still
-// lie in the 256 MB cache (4096 x 32000 x 2048 with 64 / 128 / 256 / 600 MB of logits a turn: 511 / 416 / 419 / 456 us).
-constexpr size_t HEAD_LOGITS_BYTES = 256u << 20;
+// The head form goes through the rows in turns.  Few rows, short vocabularies and rows at odd bytes: a product that writes the turn's 32-bit
+// logits, a pass that reads them while they still lie in the 256 MB cache (4096 x 32000 x 2048 with 64 / 128 / 256 / 600 MB of logits a turn:
+// 511 / 416 / 419 / 456 us).  Otherwise by groups of the vocabulary, without the logits (kernels.hpp).
+constexpr size_t HEAD_TURN_BYTES = 256u << 20;
 struct HeadPlan {
     uint64_t rows;     // of a turn
     uint64_t stride;   // floats from row to row
@@ -1435,7 +1436,7 @@ HeadPlan head_plan(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
     h.stride = ((uint64_t)vocab + 31) / 32 * 32;
     // Of the numbers of rows that fit, the one with the least time a row: whole rounds of 256 x 256 tiles over the 256 CUs, a third of a
     // round's time for each 256 tiles' worth of logits to read, and a seventh for two launches.
-    const uint64_t across = (vocab + 255) / 256, most = std::min<uint64_t>((rows + 255) / 256, HEAD_LOGITS_BYTES / (1024 * h.stride));
+    const uint64_t across = (vocab + 255) / 256, most = std::min<uint64_t>((rows + 255) / 256, HEAD_TURN_BYTES / (1024 * h.stride));
     double best = 1e30;
     h.rows = 256;
     for (uint64_t n = 1; n <= most && n <= 4096; ++n) {
@@ -1453,11 +1454,39 @@ HeadPlan head_plan(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
     h.bytes = h.logits_bytes + h.pass_bytes + scaled_matmul_workspace(h.rows, vocab, k);
     return h;
 }
+
+struct GroupPlan {
+    uint64_t rows;     // of a turn, 0: does not pay
+    uint32_t groups;
+    size_t sums, counts, lists, picked, totals, logits, bytes;
+};
+GroupPlan group_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
+    GroupPlan p{};
+    p.groups = (vocab + HEAD_GROUP - 1) / HEAD_GROUP;
+    if (((rows + 255) / 256) * ((vocab + 255) / 256) < 128 || p.groups < 4 * n_top) return p;
+    const size_t row_bytes = (size_t)p.groups * (16 + 4) + (size_t)n_top * (4 + 4 * HEAD_GROUP) + 8;
+    p.rows = HEAD_TURN_BYTES / row_bytes / 256 * 256;
+    if (p.rows < 256) p.rows = 256;
+    if (p.rows > rows) p.rows = rows;
+    const auto place = [&](size_t bytes) {
+        const size_t at = p.bytes;
+        p.bytes += align_up(bytes, 256);
+        return at;
+    };
+    p.sums = place((size_t)p.rows * p.groups * 16);
+    p.counts = place((size_t)p.groups * 4);
+    p.lists = place(n_top ? (size_t)p.groups * p.rows * 4 : 0);
+    p.picked = place((size_t)p.rows * n_top * 4);
+    p.totals = place((size_t)p.rows * 8);
+    p.logits = place((size_t)p.rows * n_top * HEAD_GROUP * 4);
+    return p;
+}
 }  // namespace
 
 size_t dessert_head_logprobs_workspace_bytes(const dessert_index_t* ix, uint64_t n_rows, uint32_t n_vocab, uint32_t n_cols, uint32_t n_top) {
     if (!ix || n_vocab == 0 || n_vocab > MAX_COLS || n_rows == 0 || n_rows >= MAX_ROWS) return 0;
-    return head_plan(n_rows, n_vocab, n_cols, n_top).bytes;
+    // which of the two it is depends on how the rows lie
+    return std::max(head_plan(n_rows, n_vocab, n_cols, n_top).bytes, group_plan(n_rows, n_vocab, n_top).bytes);
 }
 
 dessert_status_t dessert_head_logprobs(const dessert_index_t* ix, const int8_t* a_dev, uint64_t a_stride, const float* a_scales_dev,
@@ -1469,30 +1498,52 @@ dessert_status_t dessert_head_logprobs(const dessert_index_t* ix, const int8_t* 
     if (st != DESSERT_OK) return st;
     st = check_product(a_dev, a_stride, a_scales_dev, n_rows, vocab_dev, vocab_stride, vocab_scales_dev, n_vocab, n_cols);
     if (st != DESSERT_OK) return st;
+    MatmulArgs product{};
+    product.a = a_dev; product.lda = a_stride; product.sa = a_scales_dev; product.m = n_rows;
+    product.b = vocab_dev; product.ldb = vocab_stride; product.sb = vocab_scales_dev; product.n = n_vocab;
+    product.k = n_cols;
+    LogprobArgs outputs{};
+    outputs.vocab = n_vocab; outputs.n_top = n_top;
     const HeadPlan h = head_plan(n_rows ? n_rows : 1, n_vocab, n_cols, n_top);
-    st = check_workspace(workspace_dev, workspace_bytes, n_rows ? h.bytes : 0);
+    GroupPlan gp = group_plan(n_rows ? n_rows : 1, n_vocab, n_top);
+    if (!scaled_matmul_aligned(product)) gp.rows = 0;
+    st = check_workspace(workspace_dev, workspace_bytes, n_rows == 0 ? 0 : gp.rows ? gp.bytes : h.bytes);
     if (st != DESSERT_OK) return st;
     if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
     if (n_rows == 0) return DESSERT_OK;
     DeviceGuard guard(ix->cfg.device);
     if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
     char* ws = (char*)workspace_dev;
-    for (uint64_t r = 0; r < n_rows; r += h.rows) {
-        const uint64_t rows = n_rows - r < h.rows ? n_rows - r : h.rows;
-        MatmulArgs g{};
-        g.a = a_dev + r * a_stride; g.lda = a_stride; g.sa = a_scales_dev + r; g.m = rows;
-        g.b = vocab_dev; g.ldb = vocab_stride; g.sb = vocab_scales_dev; g.n = n_vocab;
-        g.k = n_cols; g.out = ws; g.ldo = h.stride;
-        HIP_TRY(launch_scaled_matmul(g, TYPE_F32, ws + h.logits_bytes + h.pass_bytes, ix->stream));
-        LogprobArgs p{};
-        p.logits = ws; p.stride = h.stride; p.rows = rows; p.vocab = n_vocab; p.n_top = n_top;
-        p.tokens = tokens_dev ? tokens_dev + r : nullptr;
-        p.logprobs = out_logprobs_dev ? out_logprobs_dev + r : nullptr;
-        p.entropy = out_entropy_dev ? out_entropy_dev + r : nullptr;
-        p.top_ids = n_top ? out_top_ids_dev + r * n_top : nullptr;
-        p.top_logprobs = n_top ? out_top_logprobs_dev + r * n_top : nullptr;
-        // the last turn's fewer rows go by the same plan, whose parts fit
-        HIP_TRY(launch_token_logprobs(p, TYPE_F32, h.pass, ws + h.logits_bytes, ix->stream));
+    const uint64_t turn = gp.rows ? gp.rows : h.rows;
+    for (uint64_t r = 0; r < n_rows; r += turn) {
+        product.m = outputs.rows = std::min(turn, n_rows - r);
+        product.a = a_dev + r * a_stride;
+        product.sa = a_scales_dev + r;
+        outputs.tokens = tokens_dev ? tokens_dev + r : nullptr;
+        outputs.logprobs = out_logprobs_dev ? out_logprobs_dev + r : nullptr;
+        outputs.entropy = out_entropy_dev ? out_entropy_dev + r : nullptr;
+        outputs.top_ids = n_top ? out_top_ids_dev + r * n_top : nullptr;
+        outputs.top_logprobs = n_top ? out_top_logprobs_dev + r * n_top : nullptr;
+        if (gp.rows) {
+            HeadArgs a{};
+            a.product = product; a.outputs = outputs; a.groups = gp.groups; a.n_top = n_top;
+            a.sums = (float4*)(ws + gp.sums); a.counts = (uint32_t*)(ws + gp.counts); a.lists = (uint32_t*)(ws + gp.lists);
+            a.picked = (uint32_t*)(ws + gp.picked); a.totals = (float2*)(ws + gp.totals); a.logits = (float*)(ws + gp.logits);
+            HIP_TRY(launch_head_sums(a, ix->stream));
+            HIP_TRY(launch_head_rows(a, ix->stream));
+            if (n_top) {
+                HIP_TRY(launch_head_groups(a, ix->stream));
+                HIP_TRY(launch_head_best(a, ix->stream));
+            }
+        } else {
+            product.out = ws;
+            product.ldo = h.stride;
+            HIP_TRY(launch_scaled_matmul(product, TYPE_F32, ws + h.logits_bytes + h.pass_bytes, ix->stream));
+            outputs.logits = ws;
+            outputs.stride = h.stride;
+            // the last turn's fewer rows go by the same plan, whose parts fit
+            HIP_TRY(launch_token_logprobs(outputs, TYPE_F32, h.pass, ws + h.logits_bytes, ix->stream));
+        }
     }
     return DESSERT_OK;
 }

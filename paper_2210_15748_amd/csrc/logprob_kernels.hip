@@ -103,9 +103,11 @@ struct Pool {
     // largest of the peaks so far bounds the n_top-th largest entry so far from below; its upper 18 bits, by bisection, leave in little
     // more than n_top entries of the first ones and few of the later ones.  (The lanes' own peaks do for a few alternatives; of 64 they
     // would be the least.)
+    // IN_ORDER: entries come with rising columns, so that a later one that only equals the bound is out.
+    template <bool IN_ORDER>
     __device__ bool raise(const uint32_t (&now)[4], uint32_t n_top) {
         const uint32_t best = max(max(now[0], now[1]), max(now[2], now[3]));
-        const uint32_t above = __popcll(__ballot(best > bound));
+        const uint32_t above = __popcll(__ballot(IN_ORDER ? best > bound : best >= max(bound, ORDER_FLOOR + 1)));
 #pragma unroll
         for (int q = 0; q < 4; ++q) peaks[q] = max(peaks[q], now[q]);
         if (above == 0) return false;
@@ -184,42 +186,28 @@ __device__ inline Sums wave_total(Sums z) {
     return z;
 }
 
-template <typename T>
-__device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, Pool& pool, uint64_t* pools, uint64_t* finals, Totals& totals, uint64_t part) {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// The row's sums over the four waves, in all threads.
+__device__ inline Sums row_total(Sums z, const Pool& pool, Totals& totals) {
     z = wave_total(z);
-    if (lane == 0) {
-        totals.sums[wave] = z;
-        totals.bound[wave] = pool.bound;
-        if (wave == 0) totals.count = 0;
+    if ((threadIdx.x & 63) == 0) {
+        totals.sums[threadIdx.x >> 6] = z;
+        totals.bound[threadIdx.x >> 6] = pool.bound;
+        if (threadIdx.x == 0) totals.count = 0;
     }
     __syncthreads();
-    z = join(join(totals.sums[0], totals.sums[1]), join(totals.sums[2], totals.sums[3]));
-    const bool whole = part == ~0ull, nan = z.s != z.s, empty = z.s == 0.f;
-    const float log_s = logf(z.s);
-    if (threadIdx.x == 0) {
-        if (!whole) {
-            g.part_sums[3 * part] = z.m;
-            g.part_sums[3 * part + 1] = z.s;
-            g.part_sums[3 * part + 2] = z.t;
-        } else {
-            if (g.entropy) g.entropy[row] = empty ? 0.f : log_s - z.t / z.s;
-            if (g.tokens) {
-                const uint32_t token = g.tokens[row];
-                float lp = nan ? z.s : MINUS_INF;
-                if (!nan && !empty && token < g.vocab) lp = ((float)((const T*)g.logits)[row * g.stride + token] - z.m) - log_s;
-                g.logprobs[row] = token == NONE ? 0.f : lp;
-            }
-        }
-    }
-    if (!g.n_top) return;
+    return join(join(totals.sums[0], totals.sums[1]), join(totals.sums[2], totals.sums[3]));
+}
+
+// After row_total: sink(place, key) for every place < n_top, by one thread each; key 0 where there is no entry.
+template <typename Sink>
+__device__ inline void rank_best(uint32_t n_top, const Pool& pool, uint64_t* pools, uint64_t* finals, Totals& totals, Sink sink) {
     const uint32_t bound = max(max(totals.bound[0], totals.bound[1]), max(totals.bound[2], totals.bound[3]));
-    for (uint32_t i = lane; i < pool.count; i += 64)
+    for (uint32_t i = threadIdx.x & 63; i < pool.count; i += 64)
         if ((uint32_t)(pool.keys[i] >> 32) >= bound) finals[atomicAdd(&totals.count, 1u)] = pool.keys[i];
     __syncthreads();
     uint32_t count = totals.count;
-    if (count > 2 * g.n_top && count > 96) count = thin_out(finals, pools, totals, count, g.n_top);
-    for (uint32_t j = threadIdx.x; j < max(count, g.n_top); j += 256) {
+    if (count > 2 * n_top && count > 96) count = thin_out(finals, pools, totals, count, n_top);
+    for (uint32_t j = threadIdx.x; j < max(count, n_top); j += 256) {
         const uint64_t mine = j < count ? finals[j] : 0;
         uint32_t place = j;   // behind the last key: an unused slot
         if (j < count) {
@@ -232,15 +220,48 @@ __device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, Pool& 
                 for (uint32_t u = 0; u < 8; ++u) place += (uint32_t)(i + u < count) & (uint32_t)(other[u] > mine);
             }
         }
-        if (place >= g.n_top) continue;
-        if (!whole) {
-            g.part_keys[part * g.n_top + place] = mine;
+        if (place < n_top) sink(place, mine);
+    }
+}
+
+// A row's log probability and entropy, by one thread; logit: of its token, where that is in the vocabulary.
+__device__ inline void write_row(const LogprobArgs& g, uint64_t row, Sums z, float log_s, float logit) {
+    const bool nan = z.s != z.s, empty = z.s == 0.f;
+    if (g.entropy) g.entropy[row] = empty ? 0.f : log_s - z.t / z.s;
+    if (g.tokens) {
+        const uint32_t token = g.tokens[row];
+        const float lp = nan ? z.s : empty || token >= g.vocab ? MINUS_INF : (logit - z.m) - log_s;
+        g.logprobs[row] = token == NONE ? 0.f : lp;
+    }
+}
+
+__device__ inline void write_place(const LogprobArgs& g, uint64_t row, uint32_t place, uint64_t key, float m, float log_s) {
+    const bool nan = log_s != log_s, some = key && !nan;
+    g.top_ids[row * g.n_top + place] = some ? ~(uint32_t)key : NONE;
+    g.top_logprobs[row * g.n_top + place] = nan ? log_s : some ? (value_of((uint32_t)(key >> 32)) - m) - log_s : MINUS_INF;
+}
+
+// part: all ones for a whole row, else where its parts go.
+template <typename T>
+__device__ inline void finish(const LogprobArgs& g, uint64_t row, Sums z, Pool& pool, uint64_t* pools, uint64_t* finals, Totals& totals, uint64_t part) {
+    z = row_total(z, pool, totals);
+    const bool whole = part == ~0ull;
+    const float log_s = logf(z.s);
+    if (threadIdx.x == 0) {
+        if (whole) {
+            const uint32_t token = g.tokens ? g.tokens[row] : NONE;
+            write_row(g, row, z, log_s, token < g.vocab ? (float)((const T*)g.logits)[row * g.stride + token] : 0.f);
         } else {
-            const bool some = mine && !nan;
-            g.top_ids[row * g.n_top + place] = some ? ~(uint32_t)mine : NONE;
-            g.top_logprobs[row * g.n_top + place] = nan ? z.s : some ? (value_of((uint32_t)(mine >> 32)) - z.m) - log_s : MINUS_INF;
+            g.part_sums[3 * part] = z.m;
+            g.part_sums[3 * part + 1] = z.s;
+            g.part_sums[3 * part + 2] = z.t;
         }
     }
+    if (!g.n_top) return;
+    rank_best(g.n_top, pool, pools, finals, totals, [&](uint32_t place, uint64_t key) {
+        if (whole) write_place(g, row, place, key, z.m, log_s);
+        else g.part_keys[part * g.n_top + place] = key;
+    });
 }
 
 // Entries c0 + (256 j + thread) * 8 ... of a row, 8 for each j, as they lie in memory; -inf from `end` on.
@@ -316,7 +337,7 @@ __global__ __launch_bounds__(256) void token_logprobs_kernel(LogprobArgs g) {
         }
         if (!g.n_top) continue;
         const uint32_t orders[4] = {order_of(peaks[0]), order_of(peaks[1]), order_of(peaks[2]), order_of(peaks[3])};
-        if (!pool.raise(orders, g.n_top)) continue;
+        if (!pool.raise<true>(orders, g.n_top)) continue;
         const float from = value_of(max(pool.bound, ORDER_FLOOR + 1));   // floats compare as their orders do
         uint32_t n = V * __popcll(__ballot(peak >= from));   // at most, and counted where that is too many
         if (pool.count + n > POOL) {
@@ -358,12 +379,88 @@ __global__ __launch_bounds__(256) void join_logprobs_kernel(LogprobArgs g) {
     for (uint32_t i = wave * 64; i < n; i += 256) {
         const uint64_t key = i + lane < n ? keys[i + lane] : 0;
         const uint32_t order = (uint32_t)(key >> 32), orders[4] = {order, 0, 0, 0};
-        if (!pool.raise(orders, g.n_top)) continue;
+        if (!pool.raise<true>(orders, g.n_top)) continue;
         if (pool.count > POOL - 64) pool.compress(g.n_top, lane);
         pool.add(order >= max(pool.bound, ORDER_FLOOR + 1), key);
         wave_sync();
     }
     finish<T>(g, row, z, pool, pools[0], finals, totals, ~0ull);
+}
+
+// A row's sums over its groups, its outputs but for the alternatives, and the groups these are among: the n_top with the largest logits,
+// ties to the first.  (Each of those has an entry that beats whatever is in another group, or equals it and comes first.)
+__global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs h) {
+    __shared__ uint64_t pools[4][POOL], finals[4 * POOL + 8];
+    __shared__ Totals totals;
+    __shared__ int dots[4];
+    const LogprobArgs& g = h.outputs;
+    const MatmulArgs& p = h.product;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t row = blockIdx.x;
+    // the token's logit
+    const uint32_t token = g.tokens ? g.tokens[row] : NONE;
+    int dot = 0;
+    if (token < g.vocab) {
+        const int8_t *a = p.a + row * p.lda, *b = p.b + token * p.ldb;
+        for (uint32_t c = threadIdx.x * 16; c < p.k; c += 4096) {
+            const v4i x = *(const v4i*)(a + c), y = *(const v4i*)(b + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dot = __builtin_amdgcn_sdot4(x[i], y[i], dot, false);
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) dot += __shfl_xor(dot, o);
+    if (lane == 0) dots[wave] = dot;
+    Sums z{MINUS_INF, 0.f, 0.f};
+    Pool pool{pools[wave]};
+    const float4* sums = h.sums + row * h.groups;
+    for (uint32_t i = wave * 64; i < h.groups; i += 256) {
+        const bool in = i + lane < h.groups;
+        const float4 v = in ? sums[i + lane] : make_float4(MINUS_INF, 0.f, 0.f, 0.f);
+        z = join(z, Sums{v.x, v.y, v.z});
+        if (!h.n_top) continue;
+        const uint32_t order = order_of(v.x), orders[4] = {order, 0, 0, 0};
+        if (!pool.raise<true>(orders, h.n_top)) continue;
+        if (pool.count > POOL - 64) pool.compress(h.n_top, lane);
+        pool.add(order >= max(pool.bound, ORDER_FLOOR + 1), key_of(order, i + lane));
+        wave_sync();
+    }
+    z = row_total(z, pool, totals);
+    const float log_s = logf(z.s);
+    if (threadIdx.x == 0) {
+        const float logit = token < g.vocab ? (float)(dots[0] + dots[1] + dots[2] + dots[3]) * (p.sa[row] * p.sb[token]) : 0.f;
+        write_row(g, row, z, log_s, logit);
+        h.totals[row] = make_float2(z.m, log_s);
+    }
+    if (!h.n_top) return;
+    rank_best(h.n_top, pool, pools[0], finals, totals, [&](uint32_t place, uint64_t key) {
+        const uint32_t group = ~(uint32_t)key, entry = (uint32_t)(row * h.n_top + place);
+        h.picked[entry] = key ? group : NONE;
+        if (key) h.lists[(uint64_t)group * p.m + atomicAdd(h.counts + group, 1u)] = entry;
+    });
+}
+
+// The best entries of a row's picked groups.
+__global__ __launch_bounds__(256) void head_best_kernel(HeadArgs h) {
+    __shared__ uint64_t pools[4][POOL], finals[4 * POOL + 8];
+    __shared__ Totals totals;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t row = blockIdx.x;
+    Pool pool{pools[wave]};
+    for (uint32_t i = wave * 64; i < h.n_top * HEAD_GROUP; i += 256) {   // 64 entries of one group
+        const uint64_t entry = row * h.n_top + i / HEAD_GROUP;
+        const uint32_t group = h.picked[entry];
+        if (group == NONE) continue;
+        const uint32_t at = i % HEAD_GROUP + lane, order = order_of(h.logits[entry * HEAD_GROUP + at]), orders[4] = {order, 0, 0, 0};
+        if (!pool.raise<false>(orders, h.n_top)) continue;
+        if (pool.count > POOL - 64) pool.compress(h.n_top, lane);
+        pool.add(order >= max(pool.bound, ORDER_FLOOR + 1), key_of(order, group * HEAD_GROUP + at));
+        wave_sync();
+    }
+    row_total(Sums{MINUS_INF, 0.f, 0.f}, pool, totals);
+    const float2 total = h.totals[row];
+    rank_best(h.n_top, pool, pools[0], finals, totals,
+              [&](uint32_t place, uint64_t key) { write_place(h.outputs, row, place, key, total.x, total.y); });
 }
 
 template <typename T>
@@ -408,6 +505,16 @@ hipError_t launch_token_logprobs(LogprobArgs g, uint32_t dtype, const LogprobPla
     if (dtype == TYPE_F16) return launch_type<f16_t>(g, stream);
     if (dtype == TYPE_BF16) return launch_type<bf16_t>(g, stream);
     return launch_type<float>(g, stream);
+}
+
+hipError_t launch_head_rows(const HeadArgs& h, hipStream_t stream) {
+    head_rows_kernel<<<dim3((uint32_t)h.product.m), dim3(256), 0, stream>>>(h);
+    return hipGetLastError();
+}
+
+hipError_t launch_head_best(const HeadArgs& h, hipStream_t stream) {
+    head_best_kernel<<<dim3((uint32_t)h.product.m), dim3(256), 0, stream>>>(h);
+    return hipGetLastError();
 }
 
 }  // namespace dessert

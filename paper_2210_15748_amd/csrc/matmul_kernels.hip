@@ -276,15 +276,74 @@ __device__ inline void store_tile(const MatmulArgs& g, v4i (&acc)[G::FM][G::FQ][
         }
     }
 }
+// A wave's results of a tile as logits of a vocabulary: for each token their largest, and what the softmax needs of them: s = sum e^(l - m),
+// t = sum e^(l - m) (l - m).  Lane / 16 has channels 4 (lane / 16) .. + 3 of each fragment, so that a token's are in 4 lanes.
+template <typename G>
+__device__ inline void sum_tile(const MatmulArgs& g, v4i (&acc)[G::FM][G::FQ][4], uint64_t m0, uint64_t n0, uint32_t lane) {
+    static_assert(G::FQ * 64 == HEAD_GROUP, "a wave's channels are one group");
+    constexpr float LOG2E = 1.44269504088896340736f, MINUS_INF = -__builtin_huge_valf();
+    float sb[G::FQ][4][4], off[G::FQ][4][4];   // off: 0, or -inf behind the last channel
+#pragma unroll
+    for (int q = 0; q < G::FQ; ++q)
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t c = n0 + q * 64 + f * 16 + lane / 16 * 4 + i;
+                sb[q][f][i] = g.sb[min(c, g.n - 1)];
+                off[q][f][i] = c < g.n ? 0.f : MINUS_INF;
+            }
+    const float own = g.sa[min(m0 + lane % (G::FM * 16), g.m - 1)];
+#pragma unroll
+    for (int fm = 0; fm < G::FM; ++fm) {
+        const float sa = __shfl(own, fm * 16 + lane % 16);
+        float m = MINUS_INF;
+#pragma unroll
+        for (int q = 0; q < G::FQ; ++q)
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = fmaf((float)acc[fm][q][f][i], sa * sb[q][f][i], off[q][f][i]);
+                    acc[fm][q][f][i] = (int)__float_as_uint(x);
+                    m = fmaxf(m, x);
+                }
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float base = m == MINUS_INF ? 0.f : m;
+        float s = 0.f, t = 0.f;
+#pragma unroll
+        for (int q = 0; q < G::FQ; ++q)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float d = __uint_as_float((uint32_t)acc[fm][q][f][i]) - base, e = __builtin_amdgcn_exp2f(d * LOG2E);
+                    s += e;
+                    t = fmaf(e, fmaxf(d, -1000.f), t);
+                }
+                acc[fm][q][f] = v4i{0, 0, 0, 0};
+            }
+        s += __shfl_xor(s, 16);
+        t += __shfl_xor(t, 16);
+        s += __shfl_xor(s, 32);
+        t += __shfl_xor(t, 32);
+        const uint64_t token = m0 + fm * 16 + lane % 16;
+        if (lane < 16 && token < g.m && n0 < g.n) ((float4*)g.out)[token * g.ldo + n0 / HEAD_GROUP] = make_float4(m, s, t, 0.f);
+    }
+}
 #endif
 
 template <typename T, typename G>
 __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ __align__(16) int8_t a0[G::TM * G::STEP], b0[G::TN * G::STEP], a1[G::TM * G::STEP], b1[G::TN * G::STEP];
-    __shared__ __align__(16) float turns[G::W][16 * 64];
+    __shared__ __align__(16) float turns[std::is_void_v<T> ? 1 : G::W][16 * 64];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave % G::WM * (G::TM / G::WM), wn = wave / G::WM * (G::TN / G::WN);
+    if constexpr (std::is_void_v<T>)   // for the kernel after this one
+        if (blockIdx.x == 0)
+            for (uint32_t i = threadIdx.x; i < g.ldo; i += 64 * G::W) g.zero[i] = 0;
     const uint32_t tiles = g.tiles_m * g.tiles_n, steps = (g.k + G::STEP - 1) / G::STEP;
     const bool partial = G::ALIGNED && g.k % G::STEP != 0;
     Source<G> src{g, tiles, steps, lane, wave, blockIdx.x};
@@ -304,7 +363,8 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
         if (++step == steps) {
             uint32_t tm, tn;
             place_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
-            store_tile<T, G>(g, acc, turns[wave], (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            if constexpr (std::is_void_v<T>) sum_tile<G>(g, acc, (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            else store_tile<T, G>(g, acc, turns[wave], (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
             step = 0;
             tile += gridDim.x;
             if (tile >= tiles) break;
@@ -318,7 +378,8 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
         if (++step == steps) {
             uint32_t tm, tn;
             place_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
-            store_tile<T, G>(g, acc, turns[wave], (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            if constexpr (std::is_void_v<T>) sum_tile<G>(g, acc, (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            else store_tile<T, G>(g, acc, turns[wave], (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
             step = 0;
             tile += gridDim.x;
             if (tile >= tiles) break;
@@ -435,6 +496,87 @@ hipError_t launch_tile_shape(MatmulArgs g, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// The logits of the groups of channels that a row's best entries lie in (head_rows_kernel's lists): a wave takes up to 32 entries of one
+// group's list and all of its channels, straight from memory into the fragments' order.
+__global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int CH = HEAD_GROUP / 16, TOK = HEAD_LIST_STEP / 16, AHEAD = 2;
+    const MatmulArgs& g = h.product;
+    const uint32_t lane = threadIdx.x & 63, groups = h.groups;
+    // which part of which list: the lists' lengths are known on the device only
+    uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6), group = groups, count = 0;
+    for (uint32_t g0 = 0; g0 < groups; g0 += 64) {
+        const uint32_t own = g0 + lane < groups ? h.counts[g0 + lane] : 0, parts = (own + HEAD_LIST_STEP - 1) / HEAD_LIST_STEP;
+        uint32_t upto = parts;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const uint32_t left = __shfl_up(upto, o);
+            if (lane >= (uint32_t)o) upto += left;
+        }
+        const uint64_t past = __ballot(upto > item);
+        if (past) {
+            const int at = __ffsll((unsigned long long)past) - 1;
+            group = g0 + at;
+            count = __shfl(own, at);
+            item -= __shfl(upto, at) - __shfl(parts, at);
+            break;
+        }
+        item -= __shfl(upto, 63);
+    }
+    if (group == groups) return;
+    const uint32_t* list = h.lists + (uint64_t)group * g.m + item * HEAD_LIST_STEP;
+    const uint32_t here = min(count - item * HEAD_LIST_STEP, (uint32_t)HEAD_LIST_STEP);
+    const uint64_t n0 = (uint64_t)group * HEAD_GROUP;
+    uint32_t entry[TOK];
+    const int8_t* row_a[TOK];
+#pragma unroll
+    for (int f = 0; f < TOK; ++f) {
+        entry[f] = list[min(f * 16 + lane % 16, here - 1)];
+        row_a[f] = g.a + (uint64_t)(entry[f] / h.n_top) * g.lda;
+    }
+    const int8_t* row_b[CH];
+#pragma unroll
+    for (int f = 0; f < CH; ++f) row_b[f] = g.b + min(n0 + f * 16 + lane % 16, g.n - 1) * g.ldb;
+    v4i acc[TOK][CH] = {};
+    for (uint32_t c0 = 0; c0 < g.k; c0 += 64 * AHEAD) {
+        v4i ch[AHEAD][CH], tok[AHEAD][TOK];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const uint32_t c = c0 + u * 64 + lane / 16 * 16, at = c < g.k ? c : 0;   // behind the columns: any channels' bytes, times zeros
+#pragma unroll
+            for (int f = 0; f < CH; ++f) ch[u][f] = *(const v4i*)(row_b[f] + at);
+#pragma unroll
+            for (int f = 0; f < TOK; ++f) {
+                const v4i v = *(const v4i*)(row_a[f] + at);
+                tok[u][f] = c < g.k ? v : v4i{0, 0, 0, 0};
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int t = 0; t < TOK; ++t)
+#pragma unroll
+                for (int f = 0; f < CH; ++f) acc[t][f] = mfma(ch[u][f], tok[u][t], acc[t][f]);
+    }
+#pragma unroll
+    for (int t = 0; t < TOK; ++t) {
+        if (t * 16 + lane % 16 >= here) continue;
+        const float sa = g.sa[entry[t] / h.n_top];
+        float* out = h.logits + (uint64_t)entry[t] * HEAD_GROUP + lane / 16 * 4;
+#pragma unroll
+        for (int f = 0; f < CH; ++f) {
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {   // as sum_tile has them
+                const uint64_t channel = n0 + f * 16 + lane / 16 * 4 + i;
+                x[i] = fmaf((float)acc[t][f][i], sa * g.sb[min(channel, g.n - 1)], channel < g.n ? 0.f : -__builtin_huge_valf());
+            }
+            store_run<float, 4>(out + f * 16, x);
+        }
+    }
+#endif
+}
+
 template <typename T, bool ALIGNED>
 hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
     const uint64_t large = ((g.m + 255) / 256) * ((g.n + 255) / 256), middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
@@ -454,9 +596,7 @@ hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
 
 template <typename T>
 hipError_t launch_type(const MatmulArgs& g, hipStream_t stream) {
-    // ALIGNED: 16-byte parts of rows, which either lie within the columns or behind them, at 32-bit offsets within a tile
-    const bool aligned = (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.k % 16 == 0 &&
-                         g.lda < (1u << 23) && g.ldb < (1u << 23);
+    const bool aligned = scaled_matmul_aligned(g);
     if (g.m <= 16) return aligned ? launch_few<T, 1, true>(g, stream) : launch_few<T, 1, false>(g, stream);
     if (g.m <= 32) return aligned ? launch_few<T, 2, true>(g, stream) : launch_few<T, 2, false>(g, stream);
     if (g.m <= 64) return aligned ? launch_few<T, 4, true>(g, stream) : launch_few<T, 4, false>(g, stream);
@@ -464,6 +604,27 @@ hipError_t launch_type(const MatmulArgs& g, hipStream_t stream) {
 }
 
 }  // namespace
+
+bool scaled_matmul_aligned(const MatmulArgs& g) {
+    // 16-byte parts of rows, which either lie within the columns or behind them, at 32-bit offsets within a tile
+    return (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.k % 16 == 0 &&
+           g.lda < (1u << 23) && g.ldb < (1u << 23);
+}
+
+hipError_t launch_head_sums(const HeadArgs& h, hipStream_t stream) {
+    MatmulArgs g = h.product;
+    g.out = h.sums;
+    g.ldo = h.groups;
+    g.zero = h.counts;
+    return launch_tile_shape<void, Tile<256, 256, 4, 2, 128, true>>(g, stream);
+}
+
+hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream) {
+    // at most: every list has a part that is not full
+    const uint64_t items = h.groups + h.product.m * h.n_top / HEAD_LIST_STEP;
+    head_groups_kernel<<<dim3((uint32_t)((items + 3) / 4)), dim3(256), 0, stream>>>(h);
+    return hipGetLastError();
+}
 
 size_t scaled_matmul_workspace(uint64_t, uint64_t, uint32_t) { return 0; }
 

@@ -291,6 +291,71 @@ def test_head_ties_and_scales_that_are_not_finite(ix):
     plain.check_logprobs(got, plain.head_logits(a, sa, b, sb), t.numpy(), 30)
 
 
+# rows and vocabularies from which on the logits do not go through memory
+GROUPS = [(300, 20000, 128, 5), (256, 20129, 272, 33), (513, 20001, 64, 0), (1100, 7000, 96, 13), (33000, 200, 16, 0), (700, 11111, 1040, 21)]
+
+
+@pytest.mark.parametrize("shape", GROUPS, ids=str)
+def test_head_by_groups(ix, shape):
+    n, V, k, n_top = shape
+    say("head by groups", shape)
+    a, sa, b, sb, t = head_inputs(n, V, k, V)
+    pick = torch.unique(torch.cat([torch.arange(min(n, 40)), torch.randint(0, n, (60,), generator=gen(1)), torch.tensor([n - 1])]))
+    l = plain.head_logits(a[pick], sa[pick], b, sb)
+    for pad, tokens in [(0, t), (16, None), (32, t)]:
+        got = dz.head_logprobs(ix, apart(a, pad), sa.to(DEV), apart(b, 2 * pad), sb.to(DEV), None if tokens is None else tokens.to(DEV), n_top)
+        got = [None if o is None else o.view(torch.int32)[pick.to(DEV)].view(o.dtype) for o in got]
+        plain.check_logprobs(got, l, None if tokens is None else tokens[pick].numpy(), n_top)
+    # rows at odd bytes take the other way: the same alternatives, and sums that differ by their order only
+    other = dz.head_logprobs(ix, apart(a, 3, 1), sa.to(DEV), apart(b, 5, 7), sb.to(DEV), t.to(DEV), n_top)
+    other = [o.view(torch.int32)[pick.to(DEV)].view(o.dtype) for o in other]
+    plain.check_logprobs(other, l, t[pick].numpy(), n_top)
+    assert torch.equal(got[2].view(torch.int32), other[2].view(torch.int32))
+
+
+def test_head_by_groups_ties_and_numbers_that_are_not_finite(ix):
+    n, V, k, n_top = 300, 20100, 64, 30
+    a, sa, b, sb, t = head_inputs(n, V, k, 12)
+    b[300:9000] = b[50]                                 # equal columns, over many groups
+    sb[300:9000] = sb[50]
+    b[20050:] = b[20040]
+    sb[20050:] = sb[20040]
+    a[1] = 0                                            # every logit 0: the first ids
+    sa[2], sa[3], sa[4] = float("nan"), 0.0, float("inf")
+    a[5:200] = a[5]                                     # every row wants the same groups
+    sa[5:200] = sa[5]
+    a[10], sa[11] = b[50], 3.0                          # best entries are the equal ones
+    got = dz.head_logprobs(ix, *(v.to(DEV) for v in (a, sa, b, sb, t)), n_top)
+    pick = torch.arange(0, 60)
+    with np.errstate(invalid="ignore"):
+        l = plain.head_logits(a[pick], sa[pick], b, sb)
+    plain.check_logprobs([o.view(torch.int32)[pick.to(DEV)].view(o.dtype) for o in got], l, t[pick].numpy(), n_top)
+    # masked entries: scales of -inf make logits of -inf (or +inf, or NaN), whole groups of them
+    sb[128:2048] = float("-inf")
+    b[128:2048] = 1
+    a[:60] = a[:60].abs().clamp(min=1)                  # positive sums there
+    got = dz.head_logprobs(ix, *(v.to(DEV) for v in (a, sa, b, sb, t)), n_top)
+    with np.errstate(invalid="ignore"):
+        l = plain.head_logits(a[pick], sa[pick], b, sb)
+    plain.check_logprobs([o.view(torch.int32)[pick.to(DEV)].view(o.dtype) for o in got], l, t[pick].numpy(), n_top)
+
+
+def test_head_by_groups_in_turns_and_again(ix):
+    """More rows than a turn takes, twice with one workspace: the same bits, though lists are filled in no fixed order."""
+    n, V, k, n_top = 13000, 20000, 32, 39
+    a, sa, b, sb, t = head_inputs(n, V, k, 14)
+    args = [v.to(DEV) for v in (a, sa, b, sb, t.to(torch.int32))]
+    ws = torch.empty(dz.head_logprobs_workspace_bytes(ix, n, V, k, n_top), dtype=torch.uint8, device=DEV)
+    assert ws.numel() < 300 << 20
+    first = [o.clone() for o in dz.head_logprobs(ix, *args, n_top, workspace=ws)]
+    again = dz.head_logprobs(ix, *args, n_top, workspace=ws)
+    for u, v in zip(first, again):
+        assert torch.equal(u.view(torch.int32), v.view(torch.int32))
+    pick = torch.cat([torch.arange(0, 13000, 311), torch.arange(11200, 11800, 40), torch.tensor([12999])])
+    got = [o.view(torch.int32)[pick.to(DEV)].view(o.dtype) for o in first]
+    plain.check_logprobs(got, plain.head_logits(a[pick], sa[pick], b, sb), t[pick].numpy(), n_top)
+
+
 # ---- as they are used -------------------------------------------------------------------------------------------------------
 def test_from_states_to_the_index_and_from_candidates_to_likelihoods():
     """Encoder states -> int8 -> last layer -> unit vectors -> index and search, then the candidates' likelihoods: every step's outputs are
@@ -336,11 +401,12 @@ def test_from_states_to_the_index_and_from_candidates_to_likelihoods():
     assert torch.isfinite(likelihood).all()
 
 
-def test_captured_into_a_graph_and_replayed_with_new_inputs():
+@pytest.mark.parametrize("n", [37, 1024])
+def test_captured_into_a_graph_and_replayed_with_new_inputs(n):
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
         ix = dz.create(128, 32, 7, seed=3)
-        n, V, k = 37, 9001, 208
+        V, k = 9001, 208
         x = torch.empty(n, k, device=DEV)
         b = torch.empty(V, k, dtype=torch.int8, device=DEV)
         sb = torch.empty(V, device=DEV)
@@ -381,10 +447,12 @@ def test_captured_into_a_graph_and_replayed_with_new_inputs():
             graph.replay()
             side.synchronize()
             pc, ps = plain.quantize(x.cpu(), False)
-            l = plain.head_logits(torch.from_numpy(pc), torch.from_numpy(ps), b.cpu(), sb.cpu())
-            plain.check_logprobs(outs, l, t.cpu().numpy(), 7)
+            pick = torch.arange(0, n, max(1, n // 37))
+            l = plain.head_logits(torch.from_numpy(pc)[pick], torch.from_numpy(ps)[pick], b.cpu(), sb.cpu())
             replayed = [o.clone() for o in (*outs, *outs2)]
-            plain.check_logprobs(outs2, logits.cpu(), t.cpu().numpy(), 7)
+            picked = [o.view(torch.int32)[pick.to(DEV)].view(o.dtype) for o in replayed]
+            plain.check_logprobs(picked[:4], l, t.cpu()[pick].numpy(), 7)
+            plain.check_logprobs(picked[4:], logits.cpu()[pick], t.cpu()[pick].numpy(), 7)
             go()
             side.synchronize()
             for u, v in zip(replayed, (*outs, *outs2)):
