@@ -397,6 +397,8 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs h) {
     const MatmulArgs& p = h.product;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t row = blockIdx.x;
+    const float4* sums = h.sums + row * h.groups;
+    float4 next = threadIdx.x < h.groups ? sums[threadIdx.x] : make_float4(MINUS_INF, 0.f, 0.f, 0.f);
     // the token's logit
     const uint32_t token = g.tokens ? g.tokens[row] : NONE;
     int dot = 0;
@@ -413,10 +415,9 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs h) {
     if (lane == 0) dots[wave] = dot;
     Sums z{MINUS_INF, 0.f, 0.f};
     Pool pool{pools[wave]};
-    const float4* sums = h.sums + row * h.groups;
     for (uint32_t i = wave * 64; i < h.groups; i += 256) {
-        const bool in = i + lane < h.groups;
-        const float4 v = in ? sums[i + lane] : make_float4(MINUS_INF, 0.f, 0.f, 0.f);
+        const float4 v = next;
+        next = i + 256 + lane < h.groups ? sums[i + 256 + lane] : make_float4(MINUS_INF, 0.f, 0.f, 0.f);
         z = join(z, Sums{v.x, v.y, v.z});
         if (!h.n_top) continue;
         const uint32_t order = order_of(v.x), orders[4] = {order, 0, 0, 0};
@@ -447,15 +448,20 @@ __global__ __launch_bounds__(256) void head_best_kernel(HeadArgs h) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t row = blockIdx.x;
     Pool pool{pools[wave]};
-    for (uint32_t i = wave * 64; i < h.n_top * HEAD_GROUP; i += 256) {   // 64 entries of one group
-        const uint64_t entry = row * h.n_top + i / HEAD_GROUP;
-        const uint32_t group = h.picked[entry];
-        if (group == NONE) continue;
-        const uint32_t at = i % HEAD_GROUP + lane, order = order_of(h.logits[entry * HEAD_GROUP + at]), orders[4] = {order, 0, 0, 0};
+    const uint32_t entries = h.n_top * HEAD_GROUP;
+    for (uint32_t i = wave * 64; i < entries; i += 1024) {   // four times 64 entries of one group each
+        uint32_t group[4], orders[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) group[j] = i + 256 * j < entries ? h.picked[row * h.n_top + (i + 256 * j) / HEAD_GROUP] : NONE;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) orders[j] = group[j] != NONE ? order_of(h.logits[row * entries + i + 256 * j + lane]) : 0;
         if (!pool.raise<false>(orders, h.n_top)) continue;
-        if (pool.count > POOL - 64) pool.compress(h.n_top, lane);
-        pool.add(order >= max(pool.bound, ORDER_FLOOR + 1), key_of(order, group * HEAD_GROUP + at));
-        wave_sync();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (pool.count > POOL - 64) pool.compress(h.n_top, lane);
+            pool.add(orders[j] >= max(pool.bound, ORDER_FLOOR + 1), key_of(orders[j], group[j] * HEAD_GROUP + (i + 256 * j) % HEAD_GROUP + lane));
+            wave_sync();
+        }
     }
     row_total(Sums{MINUS_INF, 0.f, 0.f}, pool, totals);
     const float2 total = h.totals[row];

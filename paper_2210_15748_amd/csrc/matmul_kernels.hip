@@ -496,15 +496,18 @@ hipError_t launch_tile_shape(MatmulArgs g, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// The logits of the groups of channels that a row's best entries lie in (head_rows_kernel's lists): a wave takes up to 32 entries of one
-// group's list and all of its channels, straight from memory into the fragments' order.
+// The logits of the groups of channels that a row's best entries lie in (head_rows_kernel's lists): a workgroup takes up to 32 entries of
+// one group's list and all of its channels, its waves a quarter of the columns each, straight from memory into the fragments' order.  (A
+// wave for each part of a list left the chip idle: 4096 rows x 5 groups x 2048 columns 46 us.)
 __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int CH = HEAD_GROUP / 16, TOK = HEAD_LIST_STEP / 16, AHEAD = 2;
     const MatmulArgs& g = h.product;
     const uint32_t lane = threadIdx.x & 63, groups = h.groups;
+    const uint32_t wave = threadIdx.x >> 6;
+    __shared__ __align__(16) int parts_sum[TOK][CH][64][4];
     // which part of which list: the lists' lengths are known on the device only
-    uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6), group = groups, count = 0;
+    uint32_t item = blockIdx.x, group = groups, count = 0;
     for (uint32_t g0 = 0; g0 < groups; g0 += 64) {
         const uint32_t own = g0 + lane < groups ? h.counts[g0 + lane] : 0, parts = (own + HEAD_LIST_STEP - 1) / HEAD_LIST_STEP;
         uint32_t upto = parts;
@@ -523,7 +526,9 @@ __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
         }
         item -= __shfl(upto, 63);
     }
-    if (group == groups) return;
+    if (group == groups) return;   // the same in all four waves
+    for (uint32_t i = threadIdx.x; i < TOK * CH * 64; i += 256) ((v4i*)parts_sum)[i] = v4i{0, 0, 0, 0};
+    __syncthreads();
     const uint32_t* list = h.lists + (uint64_t)group * g.m + item * HEAD_LIST_STEP;
     const uint32_t here = min(count - item * HEAD_LIST_STEP, (uint32_t)HEAD_LIST_STEP);
     const uint64_t n0 = (uint64_t)group * HEAD_GROUP;
@@ -538,11 +543,11 @@ __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
 #pragma unroll
     for (int f = 0; f < CH; ++f) row_b[f] = g.b + min(n0 + f * 16 + lane % 16, g.n - 1) * g.ldb;
     v4i acc[TOK][CH] = {};
-    for (uint32_t c0 = 0; c0 < g.k; c0 += 64 * AHEAD) {
+    for (uint32_t c0 = wave * 64; c0 < g.k; c0 += 4 * 64 * AHEAD) {
         v4i ch[AHEAD][CH], tok[AHEAD][TOK];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const uint32_t c = c0 + u * 64 + lane / 16 * 16, at = c < g.k ? c : 0;   // behind the columns: any channels' bytes, times zeros
+            const uint32_t c = c0 + u * 4 * 64 + lane / 16 * 16, at = c < g.k ? c : 0;   // behind the columns: any channels' bytes, times zeros
 #pragma unroll
             for (int f = 0; f < CH; ++f) ch[u][f] = *(const v4i*)(row_b[f] + at);
 #pragma unroll
@@ -559,17 +564,23 @@ __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
                 for (int f = 0; f < CH; ++f) acc[t][f] = mfma(ch[u][f], tok[u][t], acc[t][f]);
     }
 #pragma unroll
+    for (int t = 0; t < TOK; ++t)
+#pragma unroll
+        for (int f = 0; f < CH; ++f)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) atomicAdd(&parts_sum[t][f][lane][i], acc[t][f][i]);
+    __syncthreads();
+#pragma unroll
     for (int t = 0; t < TOK; ++t) {
         if (t * 16 + lane % 16 >= here) continue;
         const float sa = g.sa[entry[t] / h.n_top];
         float* out = h.logits + (uint64_t)entry[t] * HEAD_GROUP + lane / 16 * 4;
-#pragma unroll
-        for (int f = 0; f < CH; ++f) {
+        for (uint32_t f = wave * (CH / 4); f < (wave + 1) * (CH / 4); ++f) {
             float x[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {   // as sum_tile has them
                 const uint64_t channel = n0 + f * 16 + lane / 16 * 4 + i;
-                x[i] = fmaf((float)acc[t][f][i], sa * g.sb[min(channel, g.n - 1)], channel < g.n ? 0.f : -__builtin_huge_valf());
+                x[i] = fmaf((float)parts_sum[t][f][lane][i], sa * g.sb[min(channel, g.n - 1)], channel < g.n ? 0.f : -__builtin_huge_valf());
             }
             store_run<float, 4>(out + f * 16, x);
         }
@@ -622,7 +633,7 @@ hipError_t launch_head_sums(const HeadArgs& h, hipStream_t stream) {
 hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream) {
     // at most: every list has a part that is not full
     const uint64_t items = h.groups + h.product.m * h.n_top / HEAD_LIST_STEP;
-    head_groups_kernel<<<dim3((uint32_t)((items + 3) / 4)), dim3(256), 0, stream>>>(h);
+    head_groups_kernel<<<dim3((uint32_t)items), dim3(256), 0, stream>>>(h);
     return hipGetLastError();
 }
 
