@@ -375,7 +375,8 @@ dessert_status_t dessert_probe_mix_bandwidth(const void *in_dev, void *out_dev, 
  * faster.  Results are the same bits from call to call. */
 
 /* Rows of numbers to int8 codes with one scale a row, x ~ scale * code:
- *   DESSERT_SCALE_MAXABS: scale = max |x| / 127 (32-bit float), code = x / scale, in [-127, 127]
+ *   DESSERT_SCALE_MAXABS: scale = max |x| * (1 / 127), both factors and the product rounded to 32-bit floats, code = x / scale,
+ *                         in [-127, 127]
  *   DESSERT_SCALE_UNIT:   code = 127 x / |x| with the Euclidean norm, the vectors of an int8 index; scale = |x| / 127
  * each code the integer nearest to the quotient of these numbers, ties to even.  A row of zeros (or one whose scale
  * underflows to zero) has codes 0 and scale 0; a row that holds an infinity or NaN has codes 0 and scale NaN, so that

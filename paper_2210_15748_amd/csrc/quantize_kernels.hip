@@ -1,5 +1,5 @@
 // Rows of numbers to int8 with one scale a row.
-//   largest magnitude: scale = max|x| / 127 in 32 bits, code = x / scale
+//   largest magnitude: scale = max|x| * (1 / 127), both in 32 bits, code = x / scale
 //   unit norm:         scale = |x| / 127, code = 127 x / |x|, the norm in 64 bits (the codes of a vector are whole numbers: a sum of squares
 //                      in 32 bits would move some of them over a half)
 // each code the nearest integer to the real quotient, ties to even.  Bound by memory: rows are read once and kept in registers between the
@@ -83,7 +83,7 @@ struct Quotient {
             } else {
                 peak = __uint_as_float(v);
             }
-            scale = peak < __builtin_huge_valf() ? peak / 127.f : __builtin_nanf("");
+            scale = peak < __builtin_huge_valf() ? peak * (1.f / 127.f) : __builtin_nanf("");
             num = 1.0;
             den = scale;
             factor = 1.f / scale;

@@ -10,7 +10,7 @@ NONE = 0xFFFFFFFF
 
 
 def quantize(x, unit):
-    """codes int8, scales float32 (largest magnitude: exactly rounded) or float64 (unit norm), of a CPU tensor"""
+    """codes int8, scales float32 (largest magnitude: a product of 32-bit floats) or float64 (unit norm), of a CPU tensor"""
     x = x.to(torch.float64).numpy().astype(np.longdouble)
     ok = np.isfinite(x).all(axis=1)
     x = np.where(ok[:, None], x, 0)
@@ -20,7 +20,7 @@ def quantize(x, unit):
             codes = np.where(norm[:, None] > 0, np.rint(127 * x / norm[:, None]), 0)
         scales = (norm / 127).astype(np.float64)
     else:
-        scales = (np.abs(x).max(axis=1).astype(np.float32) / np.float32(127)).astype(np.float32)
+        scales = np.abs(x).max(axis=1).astype(np.float32) * (np.float32(1) / np.float32(127))
         with np.errstate(divide="ignore", invalid="ignore"):
             codes = np.where(scales[:, None] > 0, np.rint(x / scales[:, None].astype(np.longdouble)), 0)
     return np.clip(codes, -127, 127).astype(np.int8), np.where(ok, scales, np.nan)
