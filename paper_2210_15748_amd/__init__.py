@@ -448,6 +448,7 @@ def filter_search(ix: Index, q_vectors: torch.Tensor, q_lengths, filter_probe: i
 
 # ---- beside the search ----------------------------------------------------------------------------------------------------
 _FLOAT_TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+_INT8, _FLOAT32, _TOKEN_TYPES = (torch.int8,), (torch.float32,), (torch.int32, torch.uint32)
 
 
 def _lend(ix: Index, made) -> None:
@@ -465,28 +466,28 @@ def _lend(ix: Index, made) -> None:
         t.record_stream(stream)
 
 
-def _rows(ix: Index, t: torch.Tensor, name: str, made, *dtypes) -> torch.Tensor:
-    """A matrix on the index's device as the library reads it: elements of a row side by side, rows in order."""
-    if t.dim() != 2 or t.dtype not in dtypes or t.device != ix.device:
+def _rows(ix: Index, t: torch.Tensor, name: str, made, dtypes):
+    """A matrix on the index's device as the library reads it, elements of a row side by side and rows in order: the tensor, its address,
+    rows, columns and the elements from row to row.  (The checks of a small call take longer than its kernels: each is made once.)"""
+    shape = t.shape
+    if len(shape) != 2 or t.dtype not in dtypes or t.device != ix.device:
         raise ValueError(f"{name} must be a matrix on {ix.device} of dtype " + " / ".join(str(d) for d in dtypes))
-    n_rows, n_cols = t.shape
-    if (n_cols > 1 and t.stride(1) != 1) or (n_rows > 1 and t.stride(0) < n_cols):
+    n_rows, n_cols = shape
+    apart, step = t.stride()
+    if (n_cols > 1 and step != 1) or (n_rows > 1 and apart < n_cols):
         t = t.contiguous()
         made.append(t)
-    return t
+        apart = n_cols
+    return t, t.data_ptr(), n_rows, n_cols, apart if n_rows > 1 else n_cols
 
 
-def _stride(t: torch.Tensor) -> int:
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
-
-
-def _vector(ix: Index, t: torch.Tensor, n: int, name: str, made, *dtypes) -> torch.Tensor:
-    if t.dim() != 1 or t.shape[0] != n or t.dtype not in dtypes or t.device != ix.device:
+def _vector(ix: Index, t: torch.Tensor, n: int, name: str, made, dtypes) -> int:
+    if t.shape != (n,) or t.dtype not in dtypes or t.device != ix.device:
         raise ValueError(f"{name} must be [{n}] on {ix.device} of dtype " + " / ".join(str(d) for d in dtypes))
     if n > 1 and t.stride(0) != 1:
         t = t.contiguous()
         made.append(t)
-    return t
+    return t.data_ptr()
 
 
 def _output(ix: Index, t: Optional[torch.Tensor], shape, name: str, made, dtype) -> torch.Tensor:
@@ -494,7 +495,7 @@ def _output(ix: Index, t: Optional[torch.Tensor], shape, name: str, made, dtype)
         t = torch.empty(shape, dtype=dtype, device=ix.device)
         made.append(t)
         return t
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != ix.device or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or t.device != ix.device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {list(shape)} on {ix.device} of dtype {dtype}")
     return t
 
@@ -517,13 +518,11 @@ def quantize_rows(ix: Index, x: torch.Tensor, scaling: int = SCALE_MAXABS, out: 
     """dessert_quantize_rows: x [n, c] of float16 / bfloat16 / float32 (rows may lie apart).  Returns (codes [n, c] int8,
     scales [n] float32)."""
     made = []
-    x = _rows(ix, x, "x", made, *_FLOAT_TYPES)
-    n, c = x.shape
+    x, x_ptr, n, c, apart = _rows(ix, x, "x", made, _FLOAT_TYPES)
     out = _output(ix, out, (n, c), "out", made, torch.int8)
     out_scales = _output(ix, out_scales, (n,), "out_scales", made, torch.float32)
     _lend(ix, made)
-    _check(lib().dessert_quantize_rows(ix.handle, x.data_ptr(), _FLOAT_TYPES[x.dtype], n, c, _stride(x), scaling, out.data_ptr(),
-                                       out_scales.data_ptr()))
+    _check(lib().dessert_quantize_rows(ix.handle, x_ptr, _FLOAT_TYPES[x.dtype], n, c, apart, scaling, out.data_ptr(), out_scales.data_ptr()))
     return out, out_scales
 
 
@@ -537,34 +536,33 @@ def scaled_matmul(ix: Index, a: torch.Tensor, a_scales: torch.Tensor, b: torch.T
     """dessert_scaled_matmul: a [m, k] and b [n, k] int8 (rows may lie apart), scales [m] and [n] float32, bias [n] float32
     or None.  Returns [m, n] of out_dtype; ``out`` (rows may lie apart) decides the type if given."""
     made = []
-    a, b = _rows(ix, a, "a", made, torch.int8), _rows(ix, b, "b", made, torch.int8)
-    (m, k), n = a.shape, b.shape[0]
-    if b.shape[1] != k:
-        raise ValueError(f"a has {k} columns, b has {b.shape[1]}")
-    a_scales = _vector(ix, a_scales, m, "a_scales", made, torch.float32)
-    b_scales = _vector(ix, b_scales, n, "b_scales", made, torch.float32)
-    if bias is not None:
-        bias = _vector(ix, bias, n, "bias", made, torch.float32)
+    _, a_ptr, m, k, a_apart = _rows(ix, a, "a", made, _INT8)
+    _, b_ptr, n, b_cols, b_apart = _rows(ix, b, "b", made, _INT8)
+    if b_cols != k:
+        raise ValueError(f"a has {k} columns, b has {b_cols}")
+    sa_ptr = _vector(ix, a_scales, m, "a_scales", made, _FLOAT32)
+    sb_ptr = _vector(ix, b_scales, n, "b_scales", made, _FLOAT32)
+    bias_ptr = None if bias is None else _vector(ix, bias, n, "bias", made, _FLOAT32)
     if out is None:
         if out_dtype not in _FLOAT_TYPES:
             raise ValueError("out_dtype must be float16, bfloat16 or float32")
         out = _output(ix, None, (m, n), "out", made, out_dtype)
-    elif tuple(out.shape) != (m, n) or _rows(ix, out, "out", [], *_FLOAT_TYPES) is not out:
+    kept, out_ptr, out_rows, out_cols, out_apart = _rows(ix, out, "out", [], _FLOAT_TYPES)
+    if kept is not out or out_rows != m or out_cols != n:
         raise ValueError(f"out must be [{m}, {n}] with the elements of a row side by side")
     ws_ptr, ws_bytes = _workspace(ix, workspace, made, scaled_matmul_workspace_bytes, m, n, k)
     _lend(ix, made)
-    _check(lib().dessert_scaled_matmul(ix.handle, a.data_ptr(), _stride(a), a_scales.data_ptr(), m, b.data_ptr(), _stride(b),
-                                       b_scales.data_ptr(), _ptr(bias), n, k, _FLOAT_TYPES[out.dtype], out.data_ptr(), _stride(out),
-                                       ws_ptr, ws_bytes))
+    _check(lib().dessert_scaled_matmul(ix.handle, a_ptr, a_apart, sa_ptr, m, b_ptr, b_apart, sb_ptr, bias_ptr, n, k, _FLOAT_TYPES[out.dtype],
+                                       out_ptr, out_apart, ws_ptr, ws_bytes))
     return out
 
 
-def _tokens(ix: Index, tokens: Optional[torch.Tensor], n: int, made) -> Optional[torch.Tensor]:
+def _tokens(ix: Index, tokens: Optional[torch.Tensor], n: int, made) -> Optional[int]:
     if tokens is None:
         return None
     if tokens.dtype == torch.int64:     # ids outside 32 bits are ids outside any vocabulary; -1 is the padding mark
         tokens = torch.where((tokens < -1) | (tokens > 0x7FFFFFFF), 0x7FFFFFFF, tokens).to(torch.int32)
-    return _vector(ix, tokens, n, "tokens", made, torch.int32, torch.uint32)
+    return _vector(ix, tokens, n, "tokens", made, _TOKEN_TYPES)
 
 
 def _logprob_outputs(ix: Index, n: int, n_top: int, tokens, outs, made):
@@ -585,14 +583,13 @@ def token_logprobs(ix: Index, logits: torch.Tensor, tokens: Optional[torch.Tenso
     int64 (-1: padded position) or None.  Returns (logprobs [n] or None, entropy [n], top ids [n, n_top] uint32, top logprobs
     [n, n_top]); ``outs``: the four tensors to write."""
     made = []
-    logits = _rows(ix, logits, "logits", made, *_FLOAT_TYPES)
-    n, V = logits.shape
+    logits, l_ptr, n, V, apart = _rows(ix, logits, "logits", made, _FLOAT_TYPES)
     tokens = _tokens(ix, tokens, n, made)
     o = _logprob_outputs(ix, n, n_top, tokens, outs, made)
     ws_ptr, ws_bytes = _workspace(ix, workspace, made, token_logprobs_workspace_bytes, n, V, n_top)
     _lend(ix, made)
-    _check(lib().dessert_token_logprobs(ix.handle, logits.data_ptr(), _FLOAT_TYPES[logits.dtype], n, V, _stride(logits), _ptr(tokens),
-                                        n_top, ws_ptr, ws_bytes, *map(_ptr, o)))
+    _check(lib().dessert_token_logprobs(ix.handle, l_ptr, _FLOAT_TYPES[logits.dtype], n, V, apart, tokens, n_top, ws_ptr, ws_bytes,
+                                        *map(_ptr, o)))
     return o
 
 
@@ -605,18 +602,18 @@ def head_logprobs(ix: Index, a: torch.Tensor, a_scales: torch.Tensor, vocab: tor
     """dessert_head_logprobs: states a [n, k] and vocabulary matrix [V, k] int8 with scales [n] and [V] float32; the rest as
     token_logprobs."""
     made = []
-    a, vocab = _rows(ix, a, "a", made, torch.int8), _rows(ix, vocab, "vocab", made, torch.int8)
-    (n, k), V = a.shape, vocab.shape[0]
-    if vocab.shape[1] != k:
-        raise ValueError(f"a has {k} columns, vocab has {vocab.shape[1]}")
-    a_scales = _vector(ix, a_scales, n, "a_scales", made, torch.float32)
-    vocab_scales = _vector(ix, vocab_scales, V, "vocab_scales", made, torch.float32)
+    _, a_ptr, n, k, a_apart = _rows(ix, a, "a", made, _INT8)
+    _, v_ptr, V, v_cols, v_apart = _rows(ix, vocab, "vocab", made, _INT8)
+    if v_cols != k:
+        raise ValueError(f"a has {k} columns, vocab has {v_cols}")
+    sa_ptr = _vector(ix, a_scales, n, "a_scales", made, _FLOAT32)
+    sv_ptr = _vector(ix, vocab_scales, V, "vocab_scales", made, _FLOAT32)
     tokens = _tokens(ix, tokens, n, made)
     o = _logprob_outputs(ix, n, n_top, tokens, outs, made)
     ws_ptr, ws_bytes = _workspace(ix, workspace, made, head_logprobs_workspace_bytes, n, V, k, n_top)
     _lend(ix, made)
-    _check(lib().dessert_head_logprobs(ix.handle, a.data_ptr(), _stride(a), a_scales.data_ptr(), n, vocab.data_ptr(), _stride(vocab),
-                                       vocab_scales.data_ptr(), V, k, _ptr(tokens), n_top, ws_ptr, ws_bytes, *map(_ptr, o)))
+    _check(lib().dessert_head_logprobs(ix.handle, a_ptr, a_apart, sa_ptr, n, v_ptr, v_apart, sv_ptr, V, k, tokens, n_top, ws_ptr, ws_bytes,
+                                       *map(_ptr, o)))
     return o
 
 
