@@ -562,6 +562,7 @@ def _tokens(ix: Index, tokens: Optional[torch.Tensor], n: int, made) -> Optional
         return None
     if tokens.dtype == torch.int64:     # ids outside 32 bits are ids outside any vocabulary; -1 is the padding mark
         tokens = torch.where((tokens < -1) | (tokens > 0x7FFFFFFF), 0x7FFFFFFF, tokens).to(torch.int32)
+        made.append(tokens)
     return _vector(ix, tokens, n, "tokens", made, _TOKEN_TYPES)
 
 

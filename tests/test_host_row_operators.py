@@ -170,6 +170,31 @@ def test_the_binding_refuses_shapes_types_and_devices():
         dz.head_logprobs(ix, i8, f, torch.zeros(9, 8, dtype=torch.int8), torch.zeros(8))
 
 
+def test_the_binding_keeps_what_it_converts_until_the_call(monkeypatch):
+    """Copies that the binding makes (ids of 64 bits, columns that lie apart) are alive, and right, when the library is called."""
+    seen = {}
+
+    class Library:
+        @staticmethod
+        def dessert_head_logprobs(handle, a, a_apart, sa, n, b, b_apart, sb, V, k, tokens, *rest):
+            junk = [torch.full((n,), 7, dtype=torch.int32) for _ in range(64)]        # what freed memory would be used for
+            seen["tokens"] = list((C.c_int32 * n).from_address(tokens))
+            seen["a"] = np.ctypeslib.as_array((C.c_int8 * (n * k)).from_address(a)).reshape(n, k).copy()
+            seen["scales"] = list((C.c_float * n).from_address(sa))
+            return len(junk) - 64
+
+    monkeypatch.setattr(dz, "lib", lambda: Library)
+    monkeypatch.setattr(dz, "_lend", lambda ix, made: seen.update(lent=len(made)))
+    wide = torch.arange(600, dtype=torch.int32).to(torch.int8).view(100, 6)
+    tokens = torch.arange(100) - 1
+    tokens[5], tokens[6] = 1 << 40, -2
+    dz.head_logprobs(cpu_index(), wide[:, ::2], torch.arange(200.0)[::2], torch.zeros(9, 3, dtype=torch.int8), torch.zeros(9), tokens, 2,
+                     workspace=torch.zeros(256, dtype=torch.uint8))
+    assert seen["tokens"] == [-1, 0, 1, 2, 3, 0x7FFFFFFF, 0x7FFFFFFF] + list(range(6, 99))
+    assert np.array_equal(seen["a"], wide[:, ::2].numpy()) and seen["scales"] == list(range(0, 200, 2))
+    assert seen["lent"] == 3 + 4                          # the copies and the outputs
+
+
 def test_plain_forms_against_values_worked_out_by_hand():
     c, s = plain.quantize(torch.tensor([[127.0, 0.5, 1.5, 2.5, -0.5, -3.5]]), False)
     assert s[0] == 1.0 and c.tolist() == [[127, 0, 2, 2, 0, -4]]
