@@ -11,7 +11,7 @@ namespace dessert {
 
 namespace {
 
-constexpr int LINE = 128;   // bytes
+[[maybe_unused]] constexpr int LINE = 128;   // bytes
 
 // ---- tiles ------------------------------------------------------------------------------------------------------------------
 // A workgroup of WM x WN waves goes through tiles of TM tokens x TN channels, STEP columns a step.  A step's rows lie in LDS,
@@ -390,13 +390,13 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
 }
 
 // ---- few tokens -------------------------------------------------------------------------------------------------------------
-// Up to 64 tokens: reading b is all there is, so that many waves, each with several loads on their way, matter more than the
+// Up to 32 tokens: reading b is all there is, so that many waves, each with several loads on their way, matter more than the
 // matrix cores' rate.  A wave takes 16 channels and every KS-th 128 columns, straight from memory into the fragments' order (16
 // bytes of each of 16 rows); the 8 waves of a workgroup are KS parts of 8 / KS groups of channels and are added up in LDS.
 template <typename T, int MT, int KS, bool ALIGNED>
 __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int GROUPS = 8 / KS, AHEAD = MT == 4 ? 2 : 4;   // 128-column steps loaded before they are multiplied
+    constexpr int GROUPS = 8 / KS, AHEAD = 4;   // 128-column steps loaded before they are multiplied
     __shared__ __align__(16) v4i parts[KS == 1 ? 1 : 8][MT][64];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint64_t n0 = ((uint64_t)blockIdx.x * GROUPS + wave / KS) * 16;
@@ -473,14 +473,16 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 #endif
 }
 
+// As many parts of the columns as give 2048 waves, 8 at most: one token x 32000 x 1024 with 1 / 2 / 4 / 8 parts 10.3 / 8.9 / 13.2 / 21.6 us,
+// x 4096 x 4096 20.5 / 11.8 / 7.5 / 6.1, x 8192 x 8192 39 / 22 / 15.4 / 16.0.
 template <typename T, int MT, bool ALIGNED>
 hipError_t launch_few(const MatmulArgs& g, hipStream_t stream) {
-    const uint32_t steps = (g.k + LINE - 1) / LINE;
     const uint64_t groups = (g.n + 15) / 16;
     const auto grid = [&](int ks) { return dim3((uint32_t)((groups + 8 / ks - 1) / (8 / ks))); };
-    if (steps >= 16 || (steps >= 8 && groups < 512)) scaled_matmul_few_kernel<T, MT, 8, ALIGNED><<<grid(8), dim3(512), 0, stream>>>(g);
-    else if (steps >= 4) scaled_matmul_few_kernel<T, MT, 4, ALIGNED><<<grid(4), dim3(512), 0, stream>>>(g);
-    else scaled_matmul_few_kernel<T, MT, 1, ALIGNED><<<grid(1), dim3(512), 0, stream>>>(g);
+    if (groups >= 2048) scaled_matmul_few_kernel<T, MT, 1, ALIGNED><<<grid(1), dim3(512), 0, stream>>>(g);
+    else if (groups >= 1024) scaled_matmul_few_kernel<T, MT, 2, ALIGNED><<<grid(2), dim3(512), 0, stream>>>(g);
+    else if (groups >= 512) scaled_matmul_few_kernel<T, MT, 4, ALIGNED><<<grid(4), dim3(512), 0, stream>>>(g);
+    else scaled_matmul_few_kernel<T, MT, 8, ALIGNED><<<grid(8), dim3(512), 0, stream>>>(g);
     return hipGetLastError();
 }
 
@@ -608,9 +610,11 @@ hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
 template <typename T>
 hipError_t launch_type(const MatmulArgs& g, hipStream_t stream) {
     const bool aligned = scaled_matmul_aligned(g);
-    if (g.m <= 16) return aligned ? launch_few<T, 1, true>(g, stream) : launch_few<T, 1, false>(g, stream);
-    if (g.m <= 32) return aligned ? launch_few<T, 2, true>(g, stream) : launch_few<T, 2, false>(g, stream);
-    if (g.m <= 64) return aligned ? launch_few<T, 4, true>(g, stream) : launch_few<T, 4, false>(g, stream);
+    // The tiles' waves share what they read: better from 17 tokens on where the channels are many or the columns few (32 tokens x 32000 x
+    // 1024 15.9 by columns, 14.5 us by tiles, x 1024 x 1024 7.7 / 5.8, x 4096 x 4096 9.7 / 14.0), and for few columns with any number (16
+    // tokens x 16000 x 256 6.0 / 4.4, 16 x 32000 x 1024 12.4 / 14.2).
+    if (g.m <= 16 && g.k > 256) return aligned ? launch_few<T, 1, true>(g, stream) : launch_few<T, 1, false>(g, stream);
+    if (g.m <= 32 && g.k >= 2048 && g.n <= 4096) return aligned ? launch_few<T, 2, true>(g, stream) : launch_few<T, 2, false>(g, stream);
     return aligned ? launch_tiles<T, true>(g, stream) : launch_tiles<T, false>(g, stream);
 }
 
