@@ -1532,6 +1532,7 @@ dessert_status_t dessert_head_logprobs(const dessert_index_t* ix, const int8_t* 
             HIP_TRY(launch_head_sums(a, ix->stream));
             HIP_TRY(launch_head_rows(a, ix->stream));
             if (n_top) {
+                HIP_TRY(launch_head_lists(a, ix->stream));
                 HIP_TRY(launch_head_groups(a, ix->stream));
                 HIP_TRY(launch_head_best(a, ix->stream));
             }

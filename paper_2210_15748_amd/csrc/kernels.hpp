@@ -257,7 +257,6 @@ struct MatmulArgs {
     void* out;          // [m] rows of n, ldo apart
     uint64_t ldo;
     uint32_t tiles_m, tiles_n;   // set by the launch
-    uint32_t* zero;     // of launch_head_sums: ldo words to clear
 };
 bool scaled_matmul_aligned(const MatmulArgs& g);   // rows that the fast tiles can read
 size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k);
@@ -283,10 +282,10 @@ struct LogprobPlan {
 LogprobPlan logprob_plan(uint64_t rows, uint32_t vocab, uint32_t n_top);
 hipError_t launch_token_logprobs(LogprobArgs g, uint32_t dtype, const LogprobPlan& p, void* workspace, hipStream_t stream);
 
-// Log probabilities from int8 states without all logits in memory, in four launches: the product with the sums of each row and group of
-// HEAD_GROUP channels instead of results (launch_head_sums); a row's sums joined, and the n_top groups with the largest logits, among which its
-// n_top best entries are, put on the groups' lists (launch_head_rows); those groups' logits once more, for the rows on the
-// list (launch_head_groups); the best of them (launch_head_best).  The last two with n_top > 0 only.
+// Log probabilities from int8 states without all logits in memory: the product with the sums of each row and group of HEAD_GROUP channels
+// instead of results (launch_head_sums); a row's sums joined, and the n_top groups with the largest logits picked, among which its n_top best
+// entries are (launch_head_rows).  With n_top > 0: the picks by group (launch_head_lists); those groups' logits once more, for the rows on the
+// list (launch_head_groups); the best of them (launch_head_best).
 constexpr uint32_t HEAD_GROUP = 128, HEAD_LIST_STEP = 32;
 struct HeadArgs {
     MatmulArgs product;       // a: states, b: vocabulary; out unused
@@ -301,6 +300,7 @@ struct HeadArgs {
 };
 hipError_t launch_head_sums(const HeadArgs& h, hipStream_t stream);     // scaled_matmul_aligned(h.product) only
 hipError_t launch_head_rows(const HeadArgs& h, hipStream_t stream);
+hipError_t launch_head_lists(const HeadArgs& h, hipStream_t stream);
 hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream);
 hipError_t launch_head_best(const HeadArgs& h, hipStream_t stream);
 

@@ -341,9 +341,6 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
     __shared__ __align__(16) float turns[std::is_void_v<T> ? 1 : G::W][16 * 64];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave % G::WM * (G::TM / G::WM), wn = wave / G::WM * (G::TN / G::WN);
-    if constexpr (std::is_void_v<T>)   // for the kernel after this one
-        if (blockIdx.x == 0)
-            for (uint32_t i = threadIdx.x; i < g.ldo; i += 64 * G::W) g.zero[i] = 0;
     const uint32_t tiles = g.tiles_m * g.tiles_n, steps = (g.k + G::STEP - 1) / G::STEP;
     const bool partial = G::ALIGNED && g.k % G::STEP != 0;
     Source<G> src{g, tiles, steps, lane, wave, blockIdx.x};
@@ -498,16 +495,17 @@ hipError_t launch_tile_shape(MatmulArgs g, hipStream_t stream) {
     return hipGetLastError();
 }
 
-// The logits of the groups of channels that a row's best entries lie in (head_rows_kernel's lists): a workgroup takes up to 32 entries of
+// The logits of the groups of channels that a row's best entries lie in (head_lists_kernel): a workgroup takes up to 32 entries of
 // one group's list and all of its channels, its waves a quarter of the columns each, straight from memory into the fragments' order.  (A
-// wave for each part of a list left the chip idle: 4096 rows x 5 groups x 2048 columns 46 us.)
+// wave for each part of a list: 4096 rows x 5 of 250 groups x 2048 columns 46 us, this 39.5; neighbouring parts on the same die, whose
+// L2 would then serve the channels once: 54.)
 __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int CH = HEAD_GROUP / 16, TOK = HEAD_LIST_STEP / 16, AHEAD = 2;
     const MatmulArgs& g = h.product;
     const uint32_t lane = threadIdx.x & 63, groups = h.groups;
     const uint32_t wave = threadIdx.x >> 6;
-    __shared__ __align__(16) int parts_sum[TOK][CH][64][4];
+    __shared__ __align__(16) int sums[TOK][CH][4][64];
     // which part of which list: the lists' lengths are known on the device only
     uint32_t item = blockIdx.x, group = groups, count = 0;
     for (uint32_t g0 = 0; g0 < groups; g0 += 64) {
@@ -529,7 +527,7 @@ __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
         item -= __shfl(upto, 63);
     }
     if (group == groups) return;   // the same in all four waves
-    for (uint32_t i = threadIdx.x; i < TOK * CH * 64; i += 256) ((v4i*)parts_sum)[i] = v4i{0, 0, 0, 0};
+    for (uint32_t i = threadIdx.x; i < TOK * CH * 64; i += 256) ((v4i*)sums)[i] = v4i{0, 0, 0, 0};
     __syncthreads();
     const uint32_t* list = h.lists + (uint64_t)group * g.m + item * HEAD_LIST_STEP;
     const uint32_t here = min(count - item * HEAD_LIST_STEP, (uint32_t)HEAD_LIST_STEP);
@@ -570,7 +568,7 @@ __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
 #pragma unroll
         for (int f = 0; f < CH; ++f)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) atomicAdd(&parts_sum[t][f][lane][i], acc[t][f][i]);
+            for (int i = 0; i < 4; ++i) atomicAdd(&sums[t][f][i][lane], acc[t][f][i]);
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < TOK; ++t) {
@@ -582,7 +580,7 @@ __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {   // as sum_tile has them
                 const uint64_t channel = n0 + f * 16 + lane / 16 * 4 + i;
-                x[i] = fmaf((float)parts_sum[t][f][lane][i], sa * g.sb[min(channel, g.n - 1)], channel < g.n ? 0.f : -__builtin_huge_valf());
+                x[i] = fmaf((float)sums[t][f][i][lane], sa * g.sb[min(channel, g.n - 1)], channel < g.n ? 0.f : -__builtin_huge_valf());
             }
             store_run<float, 4>(out + f * 16, x);
         }
@@ -630,7 +628,6 @@ hipError_t launch_head_sums(const HeadArgs& h, hipStream_t stream) {
     MatmulArgs g = h.product;
     g.out = h.sums;
     g.ldo = h.groups;
-    g.zero = h.counts;
     return launch_tile_shape<void, Tile<256, 256, 4, 2, 128, true>>(g, stream);
 }
 
