@@ -61,9 +61,12 @@ __device__ inline v4i load_chunk(const int8_t* row, uint32_t c, uint32_t k) {
 
 __device__ inline v4i mfma(v4i x, v4i y, v4i acc) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, acc, 0, 0, 0); }
 
-// In LDS the 16-byte parts of each 128 bytes of a row are permuted by a key of the row (part ^ key), so that the 8 lanes that read
-// together, same part of 8 rows, meet 8 different groups of banks (SQ_LDS_BANK_CONFLICT 0).
-__device__ inline uint32_t row_key(uint32_t row) { return row & 7; }
+// In LDS the 16-byte parts of a row are permuted by a key of the row (part ^ key), so that lanes that read together, the same part of
+// neighbouring rows, meet different banks: 8 parts of 128-byte rows, 16 of longer ones (SQ_LDS_BANK_CONFLICT 0; 256-byte rows with 8
+// keys had conflicts in half of the reads' cycles).
+template <typename G>
+__device__ inline uint32_t row_key(uint32_t row) { return row & (G::PARTS < 16 ? 7 : 15); }
+
 // Workgroups go to the 8 dies in turn, each of which has an L2 of its own: a die takes tiles side by side, in bands of 4 rows of tiles.
 __device__ inline void place_tile(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& tm, uint32_t& tn) {
     constexpr uint32_t DIES = 8, BAND = 4;
@@ -89,7 +92,7 @@ struct Source {
     v4i va[G::ALIGNED ? 1 : G::LA], vb[G::ALIGNED ? 1 : G::LB];
 
     __device__ uint32_t row_of(int j) const { return (j * G::W + wave) * G::ROWS + lane / G::PARTS; }
-    __device__ uint32_t part(int j) const { return lane % G::PARTS ^ row_key(row_of(j)); }
+    __device__ uint32_t part(int j) const { return lane % G::PARTS ^ row_key<G>(row_of(j)); }
 
     __device__ void aim() {
         uint32_t tm, tn;
@@ -184,14 +187,14 @@ __device__ inline void multiply_step(v4i (&acc)[G::FM][G::FQ][4], const int8_t* 
 #pragma unroll
         for (int f = 0; f < G::FM; ++f) {
             const uint32_t row = wm + f * 16 + lane % 16;
-            tok[f] = *(const v4i*)(a + row * G::STEP + ((kk * 4 + lane / 16) ^ row_key(row)) * 16);
+            tok[f] = *(const v4i*)(a + row * G::STEP + ((kk * 4 + lane / 16) ^ row_key<G>(row)) * 16);
         }
 #pragma unroll
         for (int q = 0; q < G::FQ; ++q)
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
                 const uint32_t row = wn + q * 64 + f * 16 + lane % 16;
-                ch[q][f] = *(const v4i*)(b + row * G::STEP + ((kk * 4 + lane / 16) ^ row_key(row)) * 16);
+                ch[q][f] = *(const v4i*)(b + row * G::STEP + ((kk * 4 + lane / 16) ^ row_key<G>(row)) * 16);
             }
 #pragma unroll
         for (int fm = 0; fm < G::FM; ++fm)
