@@ -356,6 +356,38 @@ def test_head_by_groups_in_turns_and_again(ix):
     plain.check_logprobs(got, plain.head_logits(a[pick], sa[pick], b, sb), t[pick].numpy(), n_top)
 
 
+@pytest.mark.parametrize("n, V", [(9, 5000), (300, 20000)])
+def test_outputs_that_nobody_asked_for(ix, n, V):
+    """The C entry points without entropy, without tokens, and with nothing but alternatives."""
+    k, n_top = 64, 6
+    a, sa, b, sb, t = head_inputs(n, V, k, 17)
+    l = plain.head_logits(a[:9], sa[:9], b, sb)
+    d = [v.to(DEV) for v in (a, sa, b, sb, t.to(torch.int32))]
+    logits = dz.scaled_matmul(ix, *d[:4])
+    ws = torch.empty(max(dz.head_logprobs_workspace_bytes(ix, n, V, k, n_top), dz.token_logprobs_workspace_bytes(ix, n, V, n_top)),
+                     dtype=torch.uint8, device=DEV)
+    lp, ids, top = torch.empty(n, device=DEV), torch.empty(n, n_top, dtype=torch.int32, device=DEV), torch.empty(n, n_top, device=DEV)
+    want = plain.logprobs(l, t[:9].numpy(), n_top)
+    for with_tokens in (True, False):
+        for call in ("head", "token"):
+            lp.fill_(5.0)
+            ids.zero_()
+            tok = d[4].data_ptr() if with_tokens else None
+            out = lp.data_ptr() if with_tokens else None
+            if call == "head":
+                st = dz.lib().dessert_head_logprobs(ix.handle, d[0].data_ptr(), k, d[1].data_ptr(), n, d[2].data_ptr(), k, d[3].data_ptr(), V, k, tok, n_top,
+                                                    ws.data_ptr(), ws.numel(), out, None, ids.data_ptr(), top.data_ptr())
+            else:
+                st = dz.lib().dessert_token_logprobs(ix.handle, logits.data_ptr(), dz.F32, n, V, V, tok, n_top, ws.data_ptr(), ws.numel(), out, None,
+                                                     ids.data_ptr(), top.data_ptr())
+            assert st == dz.OK, dz.last_error()
+            assert np.array_equal(ids[:9].cpu().numpy().view(np.uint32), want[2])
+            if with_tokens:
+                plain.close(lp[:9].cpu().numpy(), want[0], want[4] + 4 * plain.U32 * np.where(np.isfinite(want[0]), np.abs(want[0]), 0))
+            else:
+                assert (lp == 5).all()
+
+
 # ---- as they are used -------------------------------------------------------------------------------------------------------
 def test_from_states_to_the_index_and_from_candidates_to_likelihoods():
     """Encoder states -> int8 -> last layer -> unit vectors -> index and search, then the candidates' likelihoods: every step's outputs are

@@ -3,7 +3,9 @@ compiled kernels."""
 import ctypes as C
 import importlib.util
 import pathlib
+import re
 import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -221,3 +223,23 @@ def test_no_barrier_of_the_row_operators_leaves_lds_operations_behind(source, tm
     kernels = barriers.kernels_of(barriers.disassembled(obj, tmp_path))
     assert kernels
     assert not {k: n for k, v in kernels.items() if (n := barriers.unwaited_barriers(v))}
+
+
+@pytest.mark.parametrize("source", ["quantize_kernels", "matmul_kernels", "logprob_kernels"])
+def test_the_row_operators_keep_nothing_in_scratch_memory(source, tmp_path):
+    """What the compiler recorded per lane: accumulators and rows stay in registers (a second copy of a tile's accumulators would not)."""
+    if shutil.which("hipcc") is None:
+        pytest.skip("needs hipcc")
+    from paper_2210_15748_amd import build as hip_build
+    obj = hip_build.OBJ / (source + ".o")
+    if not obj.exists() or hip_build.stale():
+        hip_build.build(force=True)
+    llvm = "/opt/rocm/llvm/bin"
+    subprocess.run([f"{llvm}/llvm-objcopy", "--dump-section", f".hip_fatbin={tmp_path}/fatbin", str(obj), f"{tmp_path}/host.o"], check=True)
+    subprocess.run([f"{llvm}/clang-offload-bundler", "--unbundle", "--type=o", "--targets=hipv4-amdgcn-amd-amdhsa--gfx950",
+                    f"--input={tmp_path}/fatbin", f"--output={tmp_path}/device.co"], check=True)
+    notes = subprocess.run([f"{llvm}/llvm-readobj", "--notes", f"{tmp_path}/device.co"], check=True, capture_output=True, text=True).stdout
+    scratch = {}
+    for block in notes.split("- .agpr_count")[1:]:
+        scratch[re.search(r"\.name:\s+(\S+)", block).group(1)] = int(re.search(r"\.private_segment_fixed_size:\s+(\d+)", block).group(1))
+    assert scratch and {k: v for k, v in scratch.items() if v} == {}
