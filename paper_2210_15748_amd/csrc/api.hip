@@ -1386,7 +1386,7 @@ dessert_status_t dessert_scaled_matmul(const dessert_index_t* ix, const int8_t* 
     g.a = a_dev; g.lda = a_stride; g.sa = a_scales_dev; g.m = n_rows;
     g.b = b_dev; g.ldb = b_stride; g.sb = b_scales_dev; g.bias = bias_dev; g.n = n_channels;
     g.k = n_cols; g.out = out_dev; g.ldo = out_stride;
-    HIP_TRY(launch_scaled_matmul(g, out_dtype, workspace_dev, ix->stream));
+    HIP_TRY(launch_scaled_matmul(g, out_dtype, workspace_dev, workspace_dev ? workspace_bytes : 0, ix->stream));
     return DESSERT_OK;
 }
 
@@ -1539,7 +1539,8 @@ dessert_status_t dessert_head_logprobs(const dessert_index_t* ix, const int8_t* 
         } else {
             product.out = ws;
             product.ldo = h.stride;
-            HIP_TRY(launch_scaled_matmul(product, TYPE_F32, ws + h.logits_bytes + h.pass_bytes, ix->stream));
+            HIP_TRY(launch_scaled_matmul(product, TYPE_F32, ws + h.logits_bytes + h.pass_bytes, h.bytes - h.logits_bytes - h.pass_bytes,
+                                         ix->stream));
             outputs.logits = ws;
             outputs.stride = h.stride;
             // the last turn's fewer rows go by the same plan, whose parts fit

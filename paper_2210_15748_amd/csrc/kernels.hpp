@@ -256,11 +256,12 @@ struct MatmulArgs {
     uint32_t k;
     void* out;          // [m] rows of n, ldo apart
     uint64_t ldo;
-    uint32_t tiles_m, tiles_n;   // set by the launch
+    uint32_t tiles_m, tiles_n, part_cols;   // set by the launch
 };
 bool scaled_matmul_aligned(const MatmulArgs& g);   // rows that the fast tiles can read
+// With less than scaled_matmul_workspace bytes the columns are not split; the results are the same bits.
 size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k);
-hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void* workspace, hipStream_t stream);
+hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void* workspace, size_t workspace_bytes, hipStream_t stream);
 struct LogprobArgs {
     const void* logits;       // [rows] rows of vocab, stride apart
     uint64_t stride, rows;

@@ -279,6 +279,22 @@ __device__ inline void store_tile(const MatmulArgs& g, v4i (&acc)[G::FM][G::FQ][
         }
     }
 }
+// A wave's sums of a tile over some of the columns, as they are, 16 bytes a lane (out: rows of whole 64 channels).
+template <typename G>
+__device__ inline void store_sums(const MatmulArgs& g, v4i (&acc)[G::FM][G::FQ][4], uint64_t m0, uint64_t n0, uint32_t lane) {
+#pragma unroll
+    for (int fm = 0; fm < G::FM; ++fm) {
+        const uint64_t token = m0 + fm * 16 + lane % 16;
+#pragma unroll
+        for (int q = 0; q < G::FQ; ++q)
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                if (token < g.m) *(v4i*)((int*)g.out + token * g.ldo + n0 + q * 64 + f * 16 + lane / 16 * 4) = acc[fm][q][f];
+                acc[fm][q][f] = v4i{0, 0, 0, 0};
+            }
+    }
+}
+
 // A wave's results of a tile as logits of a vocabulary: for each token their largest, and what the softmax needs of them: s = sum e^(l - m),
 // t = sum e^(l - m) (l - m).  Lane / 16 has channels 4 (lane / 16) .. + 3 of each fragment, so that a token's are in 4 lanes.
 template <typename G>
@@ -341,9 +357,16 @@ template <typename T, typename G>
 __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) {
 #if defined(__HIP_DEVICE_COMPILE__)
     __shared__ __align__(16) int8_t a0[G::TM * G::STEP], b0[G::TN * G::STEP], a1[G::TM * G::STEP], b1[G::TN * G::STEP];
-    __shared__ __align__(16) float turns[std::is_void_v<T> ? 1 : G::W][16 * 64];
+    __shared__ __align__(16) float turns[std::is_void_v<T> || std::is_same_v<T, int> ? 1 : G::W][16 * 64];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t wm = wave % G::WM * (G::TM / G::WM), wn = wave / G::WM * (G::TN / G::WN);
+    if constexpr (std::is_same_v<T, int>) {   // the workgroup's part of the columns, and where its sums go
+        const uint32_t c0 = blockIdx.y * g.part_cols;
+        g.a += c0;
+        g.b += c0;
+        g.k = min(g.k - c0, g.part_cols);
+        g.out = (int*)g.out + blockIdx.y * g.m * g.ldo;
+    }
     const uint32_t tiles = g.tiles_m * g.tiles_n, steps = (g.k + G::STEP - 1) / G::STEP;
     const bool partial = G::ALIGNED && g.k % G::STEP != 0;
     Source<G> src{g, tiles, steps, lane, wave, blockIdx.x};
@@ -363,7 +386,8 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
         if (++step == steps) {
             uint32_t tm, tn;
             place_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
-            if constexpr (std::is_void_v<T>) sum_tile<G>(g, acc, (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            if constexpr (std::is_same_v<T, int>) store_sums<G>(g, acc, (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            else if constexpr (std::is_void_v<T>) sum_tile<G>(g, acc, (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
             else store_tile<T, G>(g, acc, turns[wave], (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
             step = 0;
             tile += gridDim.x;
@@ -378,7 +402,8 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
         if (++step == steps) {
             uint32_t tm, tn;
             place_tile(tile, g.tiles_m, g.tiles_n, tm, tn);
-            if constexpr (std::is_void_v<T>) sum_tile<G>(g, acc, (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            if constexpr (std::is_same_v<T, int>) store_sums<G>(g, acc, (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
+            else if constexpr (std::is_void_v<T>) sum_tile<G>(g, acc, (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
             else store_tile<T, G>(g, acc, turns[wave], (uint64_t)tm * G::TM + wm, (uint64_t)tn * G::TN + wn, lane);
             step = 0;
             tile += gridDim.x;
@@ -473,6 +498,11 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 #endif
 }
 
+// Which numbers of tokens.  The tiles' waves share what they read: better from 17 tokens on where the channels are many or the columns few or
+// very many (32 tokens x 32000 x 1024 15.9 by columns, 14.5 us by tiles, x 1024 x 1024 7.7 / 5.8, x 4096 x 4096 9.7 / 12.5, x 1024 x 8192 15.1 /
+// 11.9), and for few columns with any number (16 tokens x 16000 x 256 6.0 / 4.4, 16 x 32000 x 1024 12.4 / 14.2).
+bool by_columns(uint64_t m, uint64_t n, uint32_t k) { return m <= 16 ? k > 256 : m <= 32 && k >= 2048 && k < 8192 && n <= 4096; }
+
 // As many parts of the columns as give 2048 waves, 8 at most: one token x 32000 x 1024 with 1 / 2 / 4 / 8 parts 10.3 / 8.9 / 13.2 / 21.6 us,
 // x 4096 x 4096 20.5 / 11.8 / 7.5 / 6.1, x 8192 x 8192 39 / 22 / 15.4 / 16.0.
 template <typename T, int MT, bool ALIGNED>
@@ -487,14 +517,14 @@ hipError_t launch_few(const MatmulArgs& g, hipStream_t stream) {
 }
 
 template <typename T, typename G>
-hipError_t launch_tile_shape(MatmulArgs g, hipStream_t stream) {
+hipError_t launch_tile_shape(MatmulArgs g, hipStream_t stream, uint32_t parts = 1) {
     const uint64_t tm = (g.m + G::TM - 1) / G::TM, tn = (g.n + G::TN - 1) / G::TN;
     g.tiles_m = (uint32_t)tm;
     g.tiles_n = (uint32_t)tn;
     // as many workgroups as the 256 CUs, with 160 KB of LDS each, hold at once
     const uint64_t most = 256 * (163840 / (2 * (G::TM + G::TN) * G::STEP + G::W * 4096));
     const uint64_t tiles = tm * tn;
-    scaled_matmul_kernel<T, G><<<dim3((uint32_t)(tiles < most ? tiles : most)), dim3(64 * G::W), 0, stream>>>(g);
+    scaled_matmul_kernel<T, G><<<dim3((uint32_t)(tiles < most ? tiles : most), parts), dim3(64 * G::W), 0, stream>>>(g);
     return hipGetLastError();
 }
 
@@ -591,6 +621,55 @@ __global__ __launch_bounds__(256) void head_groups_kernel(HeadArgs h) {
 #endif
 }
 
+// The parts' sums added, scaled, to memory: 4 channels a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void join_parts_kernel(MatmulArgs g, const int* sums, uint64_t row, uint32_t parts) {
+    const uint64_t quads = (g.n + 3) / 4, at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= g.m * quads) return;
+    const uint64_t token = at / quads, channel = at % quads * 4;
+    v4i sum = {0, 0, 0, 0};
+    for (uint32_t p = 0; p < parts; ++p) sum += *(const v4i*)(sums + (p * g.m + token) * row + channel);
+    const float sa = g.sa[token];
+    T* out = (T*)g.out + token * g.ldo + channel;
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t c = min(channel + i, g.n - 1);
+        y[i] = fmaf((float)sum[i], sa * g.sb[c], g.bias ? g.bias[c] : 0.f);
+    }
+    if (channel + 4 <= g.n) store_run<T, 4>(out, y);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (channel + i < g.n) out[i] = (T)y[i];
+}
+
+// Into how many parts the columns of a product in small tiles go, where the tiles alone leave CUs idle for long: 1 / 2 / 4 / 8 parts
+// of 64 x 4096 x 4096 (64 tiles) 13.6 / 13.5 / 12.5 / 15.2 us, of 128 x 4096 x 4096 (128 tiles) 13.6 / 14.7 / 16.1 / 18.5, of 128 x 1024 x 8192
+// (32 tiles) 21.5 / 18.8 / 13.6 / 12.6, of 128 x 4096 x 8192 (128 tiles) 23.1 / 20.9 / 18.2 / 25.1, of 64 x 4096 x 2048 (64 tiles) 8.8 / 10.2 / 10.4.
+uint32_t column_parts(uint64_t m, uint64_t n, uint32_t k) {
+    const uint64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
+    if (by_columns(m, n, k) || k < 4096 || k < 64 * tiles) return 1;
+    return k >= 8192 && k >= 256 * tiles ? 8 : 4;
+}
+
+size_t parts_bytes(uint64_t m, uint64_t n, uint32_t parts) { return parts < 2 ? 0 : (size_t)parts * m * ((n + 63) / 64 * 64) * 4; }
+
+template <typename T>
+hipError_t launch_parts(const MatmulArgs& g, uint32_t parts, void* workspace, hipStream_t stream) {
+    using G = Tile<64, 64, 4, 1, 256, true>;
+    MatmulArgs p = g;
+    p.out = workspace;
+    p.ldo = (g.n + 63) / 64 * 64;
+    p.part_cols = (uint32_t)(((g.k + parts - 1) / parts + G::STEP - 1) / G::STEP * G::STEP);
+    parts = (g.k + p.part_cols - 1) / p.part_cols;
+    hipError_t e = launch_tile_shape<int, G>(p, stream, parts);
+    if (e != hipSuccess) return e;
+    const uint64_t threads = g.m * ((g.n + 3) / 4);
+    join_parts_kernel<T><<<dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, stream>>>(g, (const int*)workspace, p.ldo, parts);
+    return hipGetLastError();
+}
+
 template <typename T, bool ALIGNED>
 hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
     const uint64_t large = ((g.m + 255) / 256) * ((g.n + 255) / 256), middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
@@ -609,13 +688,14 @@ hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
 }
 
 template <typename T>
-hipError_t launch_type(const MatmulArgs& g, hipStream_t stream) {
+hipError_t launch_type(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     const bool aligned = scaled_matmul_aligned(g);
-    // The tiles' waves share what they read: better from 17 tokens on where the channels are many or the columns few (32 tokens x 32000 x
-    // 1024 15.9 by columns, 14.5 us by tiles, x 1024 x 1024 7.7 / 5.8, x 4096 x 4096 9.7 / 14.0), and for few columns with any number (16
-    // tokens x 16000 x 256 6.0 / 4.4, 16 x 32000 x 1024 12.4 / 14.2).
-    if (g.m <= 16 && g.k > 256) return aligned ? launch_few<T, 1, true>(g, stream) : launch_few<T, 1, false>(g, stream);
-    if (g.m <= 32 && g.k >= 2048 && g.n <= 4096) return aligned ? launch_few<T, 2, true>(g, stream) : launch_few<T, 2, false>(g, stream);
+    if (by_columns(g.m, g.n, g.k)) {
+        if (g.m <= 16) return aligned ? launch_few<T, 1, true>(g, stream) : launch_few<T, 1, false>(g, stream);
+        return aligned ? launch_few<T, 2, true>(g, stream) : launch_few<T, 2, false>(g, stream);
+    }
+    const uint32_t parts = column_parts(g.m, g.n, g.k);
+    if (aligned && parts > 1 && parts_bytes(g.m, g.n, parts) <= workspace_bytes) return launch_parts<T>(g, parts, workspace, stream);
     return aligned ? launch_tiles<T, true>(g, stream) : launch_tiles<T, false>(g, stream);
 }
 
@@ -641,13 +721,13 @@ hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream) {
     return hipGetLastError();
 }
 
-size_t scaled_matmul_workspace(uint64_t, uint64_t, uint32_t) { return 0; }
+size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k) { return parts_bytes(m, n, column_parts(m, n, k)); }
 
-hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void*, hipStream_t stream) {
+hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     if (g.m == 0 || g.n == 0) return hipSuccess;
-    if (out_dtype == TYPE_F16) return launch_type<f16_t>(g, stream);
-    if (out_dtype == TYPE_BF16) return launch_type<bf16_t>(g, stream);
-    return launch_type<float>(g, stream);
+    if (out_dtype == TYPE_F16) return launch_type<f16_t>(g, workspace, workspace_bytes, stream);
+    if (out_dtype == TYPE_BF16) return launch_type<bf16_t>(g, workspace, workspace_bytes, stream);
+    return launch_type<float>(g, workspace, workspace_bytes, stream);
 }
 
 }  // namespace dessert

@@ -88,6 +88,12 @@ def test_matmul_refusals():
     refused(matmul(sa=P + 2), "aligned")
     refused(matmul(bias=P + 2), "aligned")
     refused(matmul(a=P + 1, b=P + 3), ALL_OK)
+    big = dict(m=64, n=64, k=8192, lda=8192, ldb=8192, ldo=64)
+    refused(matmul(**big), ALL_OK)
+    refused(matmul(**big, ws=None), "workspace_dev is NULL")
+    refused(matmul(**big, ws=P + 64), "256-byte")
+    refused(matmul(**big, wsn=1000), "workspace too small")
+    refused(matmul(ws=None, wsn=0), ALL_OK)              # none needed
 
 
 def test_logprob_refusals():
