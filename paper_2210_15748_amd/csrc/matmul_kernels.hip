@@ -153,6 +153,8 @@ struct Source {
             for (int j = 0; j < G::LA; ++j) *(v4i*)(a + (j * G::W + wave) * 1024 + lane * 16) = va[j];
 #pragma unroll
             for (int j = 0; j < G::LB; ++j) *(v4i*)(b + (j * G::W + wave) * 1024 + lane * 16) = vb[j];
+            // lgkmcnt(0): the compiler left the wait out of the barrier at the loop's head, over whose back edge these stores come
+            __builtin_amdgcn_s_waitcnt(0xC07F);
         }
     }
     // After the last tile the fetches repeat its steps, which nobody reads.
@@ -500,8 +502,13 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 
 // Which numbers of tokens.  The tiles' waves share what they read: better from 17 tokens on where the channels are many or the columns few or
 // very many (32 tokens x 32000 x 1024 15.9 by columns, 14.5 us by tiles, x 1024 x 1024 7.7 / 5.8, x 4096 x 4096 9.7 / 12.5, x 1024 x 8192 15.1 /
-// 11.9), and for few columns with any number (16 tokens x 16000 x 256 6.0 / 4.4, 16 x 32000 x 1024 12.4 / 14.2).
-bool by_columns(uint64_t m, uint64_t n, uint32_t k) { return m <= 16 ? k > 256 : m <= 32 && k >= 2048 && k < 8192 && n <= 4096; }
+// 11.9), and for few columns with any number (16 tokens x 16000 x 256 6.0 / 4.4, 16 x 32000 x 1024 12.4 / 14.2).  Rows at other addresses
+// cost a wave more here, as the tiles' parts of the columns keep more of them (1 token x 1024 x 4097 10.7 / 12.8, x 8193 18.5 / 17.2;
+// 16 x 1024 x 2049 10.0 / 10.3, x 4097 17.3 / 13.5; 32 x 1024 x 8193 46.6 / 18.7).
+bool by_columns(uint64_t m, uint64_t n, uint32_t k, bool aligned) {
+    if (m <= 16) return k > 256 && (aligned || k < (m == 1 ? 8192 : 4096));
+    return aligned && m <= 32 && k >= 2048 && k < 8192 && n <= 4096;
+}
 
 // As many parts of the columns as give 2048 waves, 8 at most: one token x 32000 x 1024 with 1 / 2 / 4 / 8 parts 10.3 / 8.9 / 13.2 / 21.6 us,
 // x 4096 x 4096 20.5 / 11.8 / 7.5 / 6.1, x 8192 x 8192 39 / 22 / 15.4 / 16.0.
@@ -647,17 +654,20 @@ __global__ __launch_bounds__(256) void join_parts_kernel(MatmulArgs g, const int
 // Into how many parts the columns of a product in small tiles go, where the tiles alone leave CUs idle for long: 1 / 2 / 4 / 8 parts
 // of 64 x 4096 x 4096 (64 tiles) 13.6 / 13.5 / 12.5 / 15.2 us, of 128 x 4096 x 4096 (128 tiles) 13.6 / 14.7 / 16.1 / 18.5, of 128 x 1024 x 8192
 // (32 tiles) 21.5 / 18.8 / 13.6 / 12.6, of 128 x 4096 x 8192 (128 tiles) 23.1 / 20.9 / 18.2 / 25.1, of 64 x 4096 x 2048 (64 tiles) 8.8 / 10.2 / 10.4.
-uint32_t column_parts(uint64_t m, uint64_t n, uint32_t k) {
+// At other addresses a step takes five times as long and parts pay sooner: 1 / 4 / 8 of 64 x 4096 x 8193 78 / 28.0 / 21.6, of 128 x 4096 x 8193 (128
+// tiles) 78 / 29.7 / 35.5, of 64 x 1024 x 2049 19.4 / 11.3; 1 / 4 of 512 x 4096 x 8193 (512 tiles) 75 / 89.
+uint32_t column_parts(uint64_t m, uint64_t n, uint32_t k, bool aligned) {
     const uint64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
-    if (by_columns(m, n, k) || k < 4096 || k < 64 * tiles) return 1;
-    return k >= 8192 && k >= 256 * tiles ? 8 : 4;
+    if (by_columns(m, n, k, aligned)) return 1;
+    if (aligned) return k < 4096 || k < 64 * tiles ? 1 : k >= 8192 && k >= 256 * tiles ? 8 : 4;
+    return k < 2048 || k < 16 * tiles || tiles > 256 ? 1 : k >= 4096 && tiles <= 64 ? 8 : 4;
 }
 
 size_t parts_bytes(uint64_t m, uint64_t n, uint32_t parts) { return parts < 2 ? 0 : (size_t)parts * m * ((n + 63) / 64 * 64) * 4; }
 
-template <typename T>
+template <typename T, bool ALIGNED>
 hipError_t launch_parts(const MatmulArgs& g, uint32_t parts, void* workspace, hipStream_t stream) {
-    using G = Tile<64, 64, 4, 1, 256, true>;
+    using G = Tile<64, 64, 4, 1, ALIGNED ? 256 : 128, ALIGNED>;
     MatmulArgs p = g;
     p.out = workspace;
     p.ldo = (g.n + 63) / 64 * 64;
@@ -687,16 +697,16 @@ hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
     return launch_tile_shape<T, Tile<64, 64, 4, 1, 128, ALIGNED>>(g, stream);
 }
 
-template <typename T>
+template <typename T, bool ALIGNED>
 hipError_t launch_type(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    const bool aligned = scaled_matmul_aligned(g);
-    if (by_columns(g.m, g.n, g.k)) {
-        if (g.m <= 16) return aligned ? launch_few<T, 1, true>(g, stream) : launch_few<T, 1, false>(g, stream);
-        return aligned ? launch_few<T, 2, true>(g, stream) : launch_few<T, 2, false>(g, stream);
+    if (by_columns(g.m, g.n, g.k, ALIGNED)) {
+        if constexpr (ALIGNED)
+            if (g.m > 16) return launch_few<T, 2, true>(g, stream);
+        return launch_few<T, 1, ALIGNED>(g, stream);
     }
-    const uint32_t parts = column_parts(g.m, g.n, g.k);
-    if (aligned && parts > 1 && parts_bytes(g.m, g.n, parts) <= workspace_bytes) return launch_parts<T>(g, parts, workspace, stream);
-    return aligned ? launch_tiles<T, true>(g, stream) : launch_tiles<T, false>(g, stream);
+    uint32_t parts = column_parts(g.m, g.n, g.k, ALIGNED);
+    while (parts > 1 && parts_bytes(g.m, g.n, parts) > workspace_bytes) --parts;
+    return parts > 1 ? launch_parts<T, ALIGNED>(g, parts, workspace, stream) : launch_tiles<T, ALIGNED>(g, stream);
 }
 
 }  // namespace
@@ -721,13 +731,22 @@ hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream) {
     return hipGetLastError();
 }
 
-size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k) { return parts_bytes(m, n, column_parts(m, n, k)); }
+size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k) {
+    const uint32_t aligned = k % 16 == 0 ? column_parts(m, n, k, true) : 1, other = column_parts(m, n, k, false);
+    return parts_bytes(m, n, aligned > other ? aligned : other);
+}
+
+template <typename T>
+static hipError_t launch_aligned(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    return scaled_matmul_aligned(g) ? launch_type<T, true>(g, workspace, workspace_bytes, stream)
+                                    : launch_type<T, false>(g, workspace, workspace_bytes, stream);
+}
 
 hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     if (g.m == 0 || g.n == 0) return hipSuccess;
-    if (out_dtype == TYPE_F16) return launch_type<f16_t>(g, workspace, workspace_bytes, stream);
-    if (out_dtype == TYPE_BF16) return launch_type<bf16_t>(g, workspace, workspace_bytes, stream);
-    return launch_type<float>(g, workspace, workspace_bytes, stream);
+    if (out_dtype == TYPE_F16) return launch_aligned<f16_t>(g, workspace, workspace_bytes, stream);
+    if (out_dtype == TYPE_BF16) return launch_aligned<bf16_t>(g, workspace, workspace_bytes, stream);
+    return launch_aligned<float>(g, workspace, workspace_bytes, stream);
 }
 
 }  // namespace dessert

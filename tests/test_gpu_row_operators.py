@@ -119,7 +119,8 @@ def check_matmul(ix, m, n, k, out_dtype, bias, pads=(0, 0, 0), at=0, seed=0, ext
 SIZES = [(1, 1, 1), (1, 16, 64), (2, 15, 63), (3, 17, 65), (16, 64, 128), (17, 65, 129), (15, 130, 127), (1, 200, 1024), (5, 1000, 272), (33, 100, 640),
          (63, 257, 144), (64, 64, 2048), (65, 70, 256), (127, 129, 112), (128, 128, 128), (129, 127, 384), (200, 260, 528), (255, 513, 192),
          (256, 256, 256), (257, 255, 1040), (300, 1, 320), (1, 1, 70000), (700, 40, 96), (513, 770, 160), (64, 130, 4096), (33, 1000, 4112), (100, 66, 8192),
-         (200, 500, 5008), (18, 100, 3000), (65, 64, 20000), (31, 70, 9216)]
+         (200, 500, 5008), (18, 100, 3000), (65, 64, 20000), (31, 70, 9216), (16, 64, 4099), (2, 600, 5001), (1, 300, 8197),
+         (100, 250, 2047), (100, 250, 2051)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=str)
@@ -159,16 +160,19 @@ def test_matmul_is_the_same_bits_however_its_rows_are_grouped(ix):
 
 
 def test_matmul_over_parts_of_the_columns(ix):
-    """Few tiles and many columns: the parts' sums lie in the workspace; a call on rows at odd bytes, which goes without, has the same bits."""
-    for m, n, k in [(70, 200, 4096), (128, 1000, 8192), (64, 2000, 4864), (20, 64, 16384)]:
+    """Few tiles and many columns: the parts' sums lie in the workspace, which nothing is written behind; rows at odd bytes, which go in other
+    parts, give the same bits, and so do calls of some of the rows."""
+    for m, n, k in [(70, 200, 4096), (128, 1000, 8192), (64, 2000, 4864), (20, 64, 16384), (33, 130, 2049), (512, 1030, 4099), (5, 66, 4109), (1, 64, 9000)]:
         a, sa, b, sb, c = (t.to(DEV) for t in product_inputs(m, n, k, m))
         nbytes = dz.scaled_matmul_workspace_bytes(ix, m, n, k)
         assert nbytes >= 4 * 4 * m * n
         ws = torch.full((nbytes + 256,), 77, dtype=torch.uint8, device=DEV)
         for out_dtype in FLOATS:
             got = dz.scaled_matmul(ix, a, sa, b, sb, c, out_dtype=out_dtype, workspace=ws[:nbytes])
-            odd = dz.scaled_matmul(ix, apart(a, 1, 3), sa, apart(b, 3, 1), sb, c, out_dtype=out_dtype)
+            odd = dz.scaled_matmul(ix, apart(a, 1, 3), sa, apart(b, 3, 1), sb, c, out_dtype=out_dtype, workspace=ws[:nbytes])
             assert torch.equal(got, odd)
+            few = dz.scaled_matmul(ix, a[m // 2:], sa[m // 2:], b, sb, c, out_dtype=out_dtype)
+            assert torch.equal(got[m // 2:], few)
         assert (ws[nbytes:] == 77).all()
         with pytest.raises(dz.DessertError, match="workspace too small"):
             dz.scaled_matmul(ix, a, sa, b, sb, c, workspace=ws[:nbytes - 256])
@@ -268,7 +272,7 @@ def head_inputs(n, V, k, seed):
 
 
 @pytest.mark.parametrize("shape", [(1, 1, 1), (1, 5, 16), (1, 1000, 64), (3, 130, 77), (1, 33000, 128), (16, 5000, 256), (17, 2049, 96), (70, 6001, 200),
-                                   (130, 3000, 512), (300, 8500, 80), (1100, 600, 144), (40, 3000, 4096), (70, 1000, 8208)], ids=str)
+                                   (130, 3000, 512), (300, 8500, 80), (1100, 600, 144), (40, 3000, 4096), (70, 1000, 8208), (50, 1000, 2301)], ids=str)
 def test_head_sizes(ix, shape):
     n, V, k = shape
     a, sa, b, sb, t = head_inputs(n, V, k, V)
