@@ -2,6 +2,7 @@
 //     out[i][j] = T( float(sum_c a[i][c] * b[j][c]) * (sa[i] * sb[j]) + bias[j] )
 // The sums are exact in int32 whatever their order, so any split of the columns gives the same bits.  Both operands lie with
 // their columns side by side, which is the order that v_mfma_i32_16x16x64_i8 takes: 16 bytes of one row per lane.
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.hpp"
@@ -16,16 +17,16 @@ namespace {
 // ---- tiles ------------------------------------------------------------------------------------------------------------------
 // A workgroup of WM x WN waves goes through tiles of TM tokens x TN channels, STEP columns a step.  A step's rows lie in LDS,
 // double-buffered: while the waves multiply one step, the next one is on its way, across the border between two tiles
-// too, so that a tile's results leave while the next tile's first columns arrive.  Rows whose bytes are 16-byte aligned (ALIGNED)
-// go from memory to LDS directly; others through registers.
+// too, so that a tile's results leave while the next tile's first columns arrive.  Rows at whole 4 bytes (DIRECT) go from memory to LDS
+// directly, others through registers: 203 x 50021 x 1028 48 us through registers, 32 directly, x 1029 54.
 //
 // The buffers are four arrays by name and the two steps of a round stand one after the other in the code: the compiler then knows
 // that reads of one buffer do not wait for what is arriving in the other.  The products appear once per buffer and nowhere else
 // (no tail outside the loop): a second copy of the accumulators would not fit the registers.
-template <int TM_, int TN_, int WM_, int WN_, int STEP_, bool ALIGNED_>
+template <int TM_, int TN_, int WM_, int WN_, int STEP_, bool DIRECT_>
 struct Tile {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, STEP = STEP_;
-    static constexpr bool ALIGNED = ALIGNED_;
+    static constexpr bool DIRECT = DIRECT_;
     static constexpr int W = WM * WN;
     static constexpr int FM = TM / WM / 16, FQ = TN / WN / 64;   // a wave's fragments: of 16 tokens, and 4 x 16 channels
     static constexpr int PARTS = STEP / 16, ROWS = 64 / PARTS;   // 16-byte parts of a row; rows in a piece of 1 KB, which a wave fetches at a time
@@ -33,29 +34,27 @@ struct Tile {
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
-// 16 bytes of a row from column c on; columns from k on read as zero.
-__device__ inline v4i load_chunk(const int8_t* row, uint32_t c, uint32_t k) {
+// 16 bytes of a row from column c on; columns from k on read as zero, k < 16.
+__device__ inline v4i load_few(const int8_t* row, uint32_t c, uint32_t k) {
     uint64_t lo = 0, hi = 0;
-    if (c < k && k >= 16) {   // where the row ends within them: its last 16 bytes, the first ones shifted out
-        const uint32_t at = min(c, k - 16), out = (c - at) * 8;   // bits, 0 to 120
-        __builtin_memcpy(&lo, row + at, 8);
-        __builtin_memcpy(&hi, row + at + 8, 8);
-        if (out >= 64) {
-            lo = hi >> (out - 64);
-            hi = 0;
-        } else if (out) {
-            lo = lo >> out | hi << (64 - out);
-            hi >>= out;
-        }
-    } else if (c < k) {
 #pragma unroll 1
-        for (uint32_t i = 0; i < k - c; ++i) {
-            const uint64_t byte = (uint8_t)row[c + i];
-            if (i < 8) lo |= byte << 8 * i;
-            else hi |= byte << 8 * (i - 8);
-        }
+    for (uint32_t i = c; i < k; ++i) {
+        const uint64_t byte = (uint8_t)row[i];
+        if (i - c < 8) lo |= byte << 8 * (i - c);
+        else hi |= byte << 8 * (i - c - 8);
     }
     const v4i v = {(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
+    return v;
+}
+
+// Where a part of 16 columns from c on would pass the columns' end, the last 16 are read instead, of tokens and channels alike (the sum does not
+// mind the order); of the tokens' the first `seen`, which an earlier part has, become zeros.
+__device__ inline v4i unseen(v4i v, uint32_t seen) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int bytes = (int)seen - 4 * i;
+        v[i] = bytes <= 0 ? v[i] : bytes >= 4 ? 0 : v[i] & (int)(~0u << 8 * bytes);
+    }
     return v;
 }
 
@@ -87,9 +86,9 @@ struct Source {
     uint32_t tile, step = 0;
     __amdgpu_buffer_rsrc_t ra, rb;
     const int8_t *pa, *pb;                // of the tile's first rows
-    using offset = std::conditional_t<G::ALIGNED, uint32_t, uint64_t>;
+    using offset = std::conditional_t<G::DIRECT, uint32_t, uint64_t>;
     offset oa[G::LA], ob[G::LB];          // a lane's 16 bytes within the tile's rows, of step 0
-    v4i va[G::ALIGNED ? 1 : G::LA], vb[G::ALIGNED ? 1 : G::LB];
+    v4i va[G::DIRECT ? 1 : G::LA], vb[G::DIRECT ? 1 : G::LB];
 
     __device__ uint32_t row_of(int j) const { return (j * G::W + wave) * G::ROWS + lane / G::PARTS; }
     __device__ uint32_t part(int j) const { return lane % G::PARTS ^ row_key<G>(row_of(j)); }
@@ -106,7 +105,7 @@ struct Source {
         for (int j = 0; j < G::LA; ++j) oa[j] = min(row_of(j), last_a) * (offset)g.lda + part(j) * 16;
 #pragma unroll
         for (int j = 0; j < G::LB; ++j) ob[j] = min(row_of(j), last_b) * (offset)g.ldb + part(j) * 16;
-        if constexpr (G::ALIGNED) {
+        if constexpr (G::DIRECT) {
             ra = __builtin_amdgcn_make_buffer_rsrc((void*)pa, 0, last_a * (uint32_t)g.lda + g.k, 0x00020000);
             rb = __builtin_amdgcn_make_buffer_rsrc((void*)pb, 0, last_b * (uint32_t)g.ldb + g.k, 0x00020000);
             if (steps == 1) fold();
@@ -123,9 +122,9 @@ struct Source {
         for (int j = 0; j < G::LB; ++j)
             if (part(j) * 16 >= left) ob[j] -= part(j) * 16;
     }
-    // Start the transfer of a step (ALIGNED: to LDS; otherwise into registers, for land()).
+    // Start the transfer of a step (DIRECT: to LDS; otherwise into registers, for land()).
     __device__ void fetch(int8_t* a, int8_t* b) {
-        if constexpr (G::ALIGNED) {
+        if constexpr (G::DIRECT) {
 #pragma unroll
             for (int j = 0; j < G::LA; ++j)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_byte*)(a + (j * G::W + wave) * 1024), 16, oa[j], step * G::STEP, 0, 0);
@@ -139,16 +138,23 @@ struct Source {
                 for (int j = 0; j < G::LA; ++j) __builtin_memcpy(&va[j], pa + oa[j] + c, 16);
 #pragma unroll
                 for (int j = 0; j < G::LB; ++j) __builtin_memcpy(&vb[j], pb + ob[j] + c, 16);
+            } else if (g.k >= 16) {
+#pragma unroll
+                for (int j = 0; j < G::LA; ++j) __builtin_memcpy(&va[j], pa + (oa[j] - part(j) * 16) + min(c + part(j) * 16, g.k - 16), 16);
+#pragma unroll
+                for (int j = 0; j < G::LB; ++j) __builtin_memcpy(&vb[j], pb + (ob[j] - part(j) * 16) + min(c + part(j) * 16, g.k - 16), 16);
+#pragma unroll
+                for (int j = 0; j < G::LA; ++j) va[j] = unseen(va[j], c + part(j) * 16 - min(c + part(j) * 16, g.k - 16));
             } else {
 #pragma unroll
-                for (int j = 0; j < G::LA; ++j) va[j] = load_chunk(pa + (oa[j] - part(j) * 16), c + part(j) * 16, g.k);
+                for (int j = 0; j < G::LA; ++j) va[j] = load_few(pa + (oa[j] - part(j) * 16), part(j) * 16, g.k);
 #pragma unroll
-                for (int j = 0; j < G::LB; ++j) vb[j] = load_chunk(pb + (ob[j] - part(j) * 16), c + part(j) * 16, g.k);
+                for (int j = 0; j < G::LB; ++j) vb[j] = load_few(pb + (ob[j] - part(j) * 16), part(j) * 16, g.k);
             }
         }
     }
     __device__ void land(int8_t* a, int8_t* b) {
-        if constexpr (!G::ALIGNED) {
+        if constexpr (!G::DIRECT) {
 #pragma unroll
             for (int j = 0; j < G::LA; ++j) *(v4i*)(a + (j * G::W + wave) * 1024 + lane * 16) = va[j];
 #pragma unroll
@@ -163,18 +169,24 @@ struct Source {
             step = 0;
             if (tile + gridDim.x < tiles) tile += gridDim.x;
             aim();
-        } else if (G::ALIGNED && step == steps - 1) {
+        } else if (G::DIRECT && step == steps - 1) {
             fold();
         }
     }
-    // Before a step is multiplied, where the columns end within it: zeros for the tokens' parts behind the end, by the wave that
+    // Before a step is multiplied, where the columns end within it: zeros for the tokens' columns behind the end, by the wave that
     // fetched them (the channels' may hold anything then).
     __device__ void clear_tail(int8_t* a) const {
         const uint32_t left = g.k - (steps - 1) * G::STEP;
         __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): the transfers to LDS have landed
 #pragma unroll
         for (int j = 0; j < G::LA; ++j)
-            if (part(j) * 16 >= left) *(v4i*)(a + (j * G::W + wave) * 1024 + lane * 16) = v4i{0, 0, 0, 0};
+            if (part(j) * 16 + 16 > left) {
+                v4i* at = (v4i*)(a + (j * G::W + wave) * 1024 + lane * 16);
+                v4i v = *at;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = part(j) * 16 + i * 4 < left ? v[i] : 0;
+                *at = v;
+            }
     }
 };
 
@@ -205,7 +217,7 @@ __device__ inline void multiply_step(v4i (&acc)[G::FM][G::FQ][4], const int8_t* 
 #pragma unroll
                 for (int f = 0; f < 4; ++f) acc[fm][q][f] = mfma(ch[q][f], tok[fm], acc[fm][q][f]);
     }
-    if constexpr (G::ALIGNED) {
+    if constexpr (G::DIRECT) {
         // Order: the reads of the first 64 columns; products with the next columns' reads between them, and in the first half of
         // the step the next step's transfers (a burst of transfers at the step's start held the products up: 8192^3 486 -> 427 us
         // with this and the rounds over tiles).
@@ -370,7 +382,7 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
         g.out = (int*)g.out + blockIdx.y * g.m * g.ldo;
     }
     const uint32_t tiles = g.tiles_m * g.tiles_n, steps = (g.k + G::STEP - 1) / G::STEP;
-    const bool partial = G::ALIGNED && g.k % G::STEP != 0;
+    const bool partial = G::DIRECT && g.k % G::STEP != 0;
     Source<G> src{g, tiles, steps, lane, wave, blockIdx.x};
     src.aim();
     v4i acc[G::FM][G::FQ][4] = {};
@@ -439,23 +451,24 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint32_t c = c0 + u * KS * LINE + h * 64 + lane / 16 * 16;
-                if constexpr (ALIGNED) {   // columns behind the end: any channels' bytes, times zeros
-                    const bool in = c < g.k;
-                    const uint32_t at = in ? c : 0;
-                    ch[u][h] = *(const v4i*)(row_b + at);
+                ch[u][h] = v4i{0, 0, 0, 0};
 #pragma unroll
-                    for (int f = 0; f < MT; ++f) {
-                        const v4i v = *(const v4i*)(row_a[f] + at);
-                        tok[u][h][f] = in ? v : v4i{0, 0, 0, 0};
+                for (int f = 0; f < MT; ++f) tok[u][h][f] = v4i{0, 0, 0, 0};
+                // no loads behind the end, which would cost what others do (1 token x 1024 x 1024 4.5 us with them, 3.4 without)
+                if (c < g.k) {
+                    if constexpr (ALIGNED) {
+                        ch[u][h] = *(const v4i*)(row_b + c);
+#pragma unroll
+                        for (int f = 0; f < MT; ++f) tok[u][h][f] = *(const v4i*)(row_a[f] + c);
+                    } else {   // k >= 16: the launch's rule
+                        const uint32_t at = min(c, g.k - 16);
+                        __builtin_memcpy(&ch[u][h], row_b + at, 16);
+#pragma unroll
+                        for (int f = 0; f < MT; ++f) {
+                            __builtin_memcpy(&tok[u][h][f], row_a[f] + at, 16);
+                            tok[u][h][f] = unseen(tok[u][h][f], c - at);
+                        }
                     }
-                } else if (c0 + (AHEAD - 1) * KS * LINE + LINE <= g.k) {
-                    __builtin_memcpy(&ch[u][h], row_b + c, 16);
-#pragma unroll
-                    for (int f = 0; f < MT; ++f) __builtin_memcpy(&tok[u][h][f], row_a[f] + c, 16);
-                } else {
-                    ch[u][h] = load_chunk(row_b, c, g.k);
-#pragma unroll
-                    for (int f = 0; f < MT; ++f) tok[u][h][f] = load_chunk(row_a[f], c, g.k);
                 }
             }
 #pragma unroll
@@ -505,9 +518,9 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 // 11.9), and for few columns with any number (16 tokens x 16000 x 256 6.0 / 4.4, 16 x 32000 x 1024 12.4 / 14.2).  Rows at other addresses
 // cost a wave more here, as the tiles' parts of the columns keep more of them (1 token x 1024 x 4097 10.7 / 12.8, x 8193 18.5 / 17.2;
 // 16 x 1024 x 2049 10.0 / 10.3, x 4097 17.3 / 13.5; 32 x 1024 x 8193 46.6 / 18.7).
-bool by_columns(uint64_t m, uint64_t n, uint32_t k, bool aligned) {
-    if (m <= 16) return k > 256 && (aligned || k < (m == 1 ? 8192 : 4096));
-    return aligned && m <= 32 && k >= 2048 && k < 8192 && n <= 4096;
+bool by_columns(uint64_t m, uint64_t n, uint32_t k, int unit) {
+    if (m <= 16) return k > 256 && (unit >= 4 || k < (m == 1 ? 8192 : 4096));
+    return unit == 16 && m <= 32 && k >= 2048 && k < 8192 && n <= 4096;
 }
 
 // As many parts of the columns as give 2048 waves, 8 at most: one token x 32000 x 1024 with 1 / 2 / 4 / 8 parts 10.3 / 8.9 / 13.2 / 21.6 us,
@@ -656,18 +669,18 @@ __global__ __launch_bounds__(256) void join_parts_kernel(MatmulArgs g, const int
 // (32 tiles) 21.5 / 18.8 / 13.6 / 12.6, of 128 x 4096 x 8192 (128 tiles) 23.1 / 20.9 / 18.2 / 25.1, of 64 x 4096 x 2048 (64 tiles) 8.8 / 10.2 / 10.4.
 // At other addresses a step takes five times as long and parts pay sooner: 1 / 4 / 8 of 64 x 4096 x 8193 78 / 28.0 / 21.6, of 128 x 4096 x 8193 (128
 // tiles) 78 / 29.7 / 35.5, of 64 x 1024 x 2049 19.4 / 11.3; 1 / 4 of 512 x 4096 x 8193 (512 tiles) 75 / 89.
-uint32_t column_parts(uint64_t m, uint64_t n, uint32_t k, bool aligned) {
+uint32_t column_parts(uint64_t m, uint64_t n, uint32_t k, int unit) {
     const uint64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
-    if (by_columns(m, n, k, aligned)) return 1;
-    if (aligned) return k < 4096 || k < 64 * tiles ? 1 : k >= 8192 && k >= 256 * tiles ? 8 : 4;
+    if (by_columns(m, n, k, unit)) return 1;
+    if (unit >= 4) return k < 4096 || k < 64 * tiles ? 1 : k >= 8192 && k >= 256 * tiles ? 8 : 4;
     return k < 2048 || k < 16 * tiles || tiles > 256 ? 1 : k >= 4096 && tiles <= 64 ? 8 : 4;
 }
 
 size_t parts_bytes(uint64_t m, uint64_t n, uint32_t parts) { return parts < 2 ? 0 : (size_t)parts * m * ((n + 63) / 64 * 64) * 4; }
 
-template <typename T, bool ALIGNED>
+template <typename T, bool DIRECT>
 hipError_t launch_parts(const MatmulArgs& g, uint32_t parts, void* workspace, hipStream_t stream) {
-    using G = Tile<64, 64, 4, 1, ALIGNED ? 256 : 128, ALIGNED>;
+    using G = Tile<64, 64, 4, 1, DIRECT ? 256 : 128, DIRECT>;
     MatmulArgs p = g;
     p.out = workspace;
     p.ldo = (g.n + 63) / 64 * 64;
@@ -680,42 +693,51 @@ hipError_t launch_parts(const MatmulArgs& g, uint32_t parts, void* workspace, hi
     return hipGetLastError();
 }
 
-template <typename T, bool ALIGNED>
+template <typename T, bool DIRECT>
 hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
     const uint64_t large = ((g.m + 255) / 256) * ((g.n + 255) / 256), middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
-    if constexpr (ALIGNED)
+    if constexpr (DIRECT)
         if (large >= 128) return launch_tile_shape<T, Tile<256, 256, 4, 2, 128, true>>(g, stream);
-    if (middle >= 192) return launch_tile_shape<T, Tile<128, 128, 2, 2, 128, ALIGNED>>(g, stream);
+    if (middle >= 192) return launch_tile_shape<T, Tile<128, 128, 2, 2, 128, DIRECT>>(g, stream);
     // Small tiles wait for memory once a step: longer steps where there are columns for them, the longest (a workgroup a CU) where there
     // are no more tiles than CUs.  128 / 256 / 512 columns: 128 x 4096 x 4096 24.8 / 16.6 / 14.3 us, 256 x 8192 x 8192 50.6 / 40.0 / 47.6,
     // 256 x 1024 x 1024 6.8 / 6.1 / 6.5.  Through registers they pay no more: 1111 x 1003 x 1029 15.6 / 17.4.
-    if constexpr (ALIGNED) {
+    if constexpr (DIRECT) {
         const uint64_t small = ((g.m + 63) / 64) * ((g.n + 63) / 64);
         if (g.k >= 2048 && small <= 256) return launch_tile_shape<T, Tile<64, 64, 4, 1, 512, true>>(g, stream);
         if (g.k > 256) return launch_tile_shape<T, Tile<64, 64, 4, 1, 256, true>>(g, stream);
     }
-    return launch_tile_shape<T, Tile<64, 64, 4, 1, 128, ALIGNED>>(g, stream);
+    return launch_tile_shape<T, Tile<64, 64, 4, 1, 128, DIRECT>>(g, stream);
 }
 
-template <typename T, bool ALIGNED>
+// UNIT: the rows lie at multiples of 16 bytes, of 4, or anywhere.
+template <typename T, int UNIT>
 hipError_t launch_type(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    if (by_columns(g.m, g.n, g.k, ALIGNED)) {
-        if constexpr (ALIGNED)
+    if (by_columns(g.m, g.n, g.k, UNIT)) {
+        if constexpr (UNIT == 16)
             if (g.m > 16) return launch_few<T, 2, true>(g, stream);
-        return launch_few<T, 1, ALIGNED>(g, stream);
+        return launch_few<T, 1, UNIT == 16>(g, stream);
     }
-    uint32_t parts = column_parts(g.m, g.n, g.k, ALIGNED);
+    uint32_t parts = column_parts(g.m, g.n, g.k, UNIT);
     while (parts > 1 && parts_bytes(g.m, g.n, parts) > workspace_bytes) --parts;
-    return parts > 1 ? launch_parts<T, ALIGNED>(g, parts, workspace, stream) : launch_tiles<T, ALIGNED>(g, stream);
+    return parts > 1 ? launch_parts<T, UNIT >= 4>(g, parts, workspace, stream) : launch_tiles<T, UNIT >= 4>(g, stream);
+}
+
+bool rows_at(const MatmulArgs& g, uint32_t bytes) {
+    return (uintptr_t)g.a % bytes == 0 && (uintptr_t)g.b % bytes == 0 && g.lda % bytes == 0 && g.ldb % bytes == 0 && g.k % bytes == 0 &&
+           g.lda < (1u << 23) && g.ldb < (1u << 23);   // 32-bit offsets within a tile
+}
+
+template <typename T>
+hipError_t launch_aligned(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (rows_at(g, 16)) return launch_type<T, 16>(g, workspace, workspace_bytes, stream);
+    if (rows_at(g, 4)) return launch_type<T, 4>(g, workspace, workspace_bytes, stream);
+    return launch_type<T, 1>(g, workspace, workspace_bytes, stream);
 }
 
 }  // namespace
 
-bool scaled_matmul_aligned(const MatmulArgs& g) {
-    // 16-byte parts of rows, which either lie within the columns or behind them, at 32-bit offsets within a tile
-    return (uintptr_t)g.a % 16 == 0 && (uintptr_t)g.b % 16 == 0 && g.lda % 16 == 0 && g.ldb % 16 == 0 && g.k % 16 == 0 &&
-           g.lda < (1u << 23) && g.ldb < (1u << 23);
-}
+bool scaled_matmul_aligned(const MatmulArgs& g) { return rows_at(g, 16); }
 
 hipError_t launch_head_sums(const HeadArgs& h, hipStream_t stream) {
     MatmulArgs g = h.product;
@@ -732,14 +754,10 @@ hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream) {
 }
 
 size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k) {
-    const uint32_t aligned = k % 16 == 0 ? column_parts(m, n, k, true) : 1, other = column_parts(m, n, k, false);
-    return parts_bytes(m, n, aligned > other ? aligned : other);
-}
-
-template <typename T>
-static hipError_t launch_aligned(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-    return scaled_matmul_aligned(g) ? launch_type<T, true>(g, workspace, workspace_bytes, stream)
-                                    : launch_type<T, false>(g, workspace, workspace_bytes, stream);
+    uint32_t parts = 1;   // the most of any addresses that rows of k columns can have
+    for (int unit : {1, 4, 16})
+        if (k % unit == 0) parts = std::max(parts, column_parts(m, n, k, unit));
+    return parts_bytes(m, n, parts);
 }
 
 hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void* workspace, size_t workspace_bytes, hipStream_t stream) {
