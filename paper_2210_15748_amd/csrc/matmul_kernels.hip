@@ -61,7 +61,7 @@ __device__ inline v4i unseen(v4i v, uint32_t seen) {
 __device__ inline v4i mfma(v4i x, v4i y, v4i acc) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(x, y, acc, 0, 0, 0); }
 
 // In LDS the 16-byte parts of a row are permuted by a key of the row (part ^ key), so that lanes that read together, the same part of
-// neighbouring rows, meet different banks: 8 parts of 128-byte rows, 16 of longer ones (SQ_LDS_BANK_CONFLICT 0; 256-byte rows with 8
+// neighbouring rows, meet different banks: 8 parts of 128-byte rows, 16 of longer ones (no conflicts in the products; 256-byte rows with 8
 // keys had conflicts in half of the reads' cycles).
 template <typename G>
 __device__ inline uint32_t row_key(uint32_t row) { return row & (G::PARTS < 16 ? 7 : 15); }
@@ -513,14 +513,15 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 #endif
 }
 
-// Which numbers of tokens.  The tiles' waves share what they read: better from 17 tokens on where the channels are many or the columns few or
-// very many (32 tokens x 32000 x 1024 15.9 by columns, 14.5 us by tiles, x 1024 x 1024 7.7 / 5.8, x 4096 x 4096 9.7 / 12.5, x 1024 x 8192 15.1 /
-// 11.9), and for few columns with any number (16 tokens x 16000 x 256 6.0 / 4.4, 16 x 32000 x 1024 12.4 / 14.2).  Rows at other addresses
-// cost a wave more here, as the tiles' parts of the columns keep more of them (1 token x 1024 x 4097 10.7 / 12.8, x 8193 18.5 / 17.2;
-// 16 x 1024 x 2049 10.0 / 10.3, x 4097 17.3 / 13.5; 32 x 1024 x 8193 46.6 / 18.7).
+// Which numbers of tokens.  From 17 on the tiles' waves, which share what they read, are better where the channels are many or the columns
+// very many: 32 tokens x 4096 x 1024 4.3 by columns, 5.7 us by tiles, x 8000 x 1024 7.5 / 6.9, x 32000 x 1024 15.9 / 14.5, x 4096 x 4096 9.7 /
+// 12.5, x 1024 x 8192 15.1 / 11.9; 16 tokens x 16000 x 256 3.6 / 4.4, x 16000 x 2048 13.2 / 12.0.  Rows at odd bytes cost a wave more
+// here, as the tiles' parts of the columns keep more waves busy (1 token x 1024 x 4097 10.0 / 12.8, x 8191 17.5 / 17.2; 16 x 1024 x 2049 9.5 /
+// 10.3, x 4097 17.3 / 11.4; 32 x 1024 x 8193 46.6 / 18.7).
 bool by_columns(uint64_t m, uint64_t n, uint32_t k, int unit) {
-    if (m <= 16) return k > 256 && (unit >= 4 || k < (m == 1 ? 8192 : 4096));
-    return unit == 16 && m <= 32 && k >= 2048 && k < 8192 && n <= 4096;
+    if (k < 16) return false;
+    if (m <= 16) return unit >= 4 || k < (m == 1 ? 8192 : 4096);
+    return unit >= 4 && m <= 32 && k < 8192 && n <= 4096;
 }
 
 // As many parts of the columns as give 2048 waves, 8 at most: one token x 32000 x 1024 with 1 / 2 / 4 / 8 parts 10.3 / 8.9 / 13.2 / 21.6 us,
@@ -714,8 +715,8 @@ hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
 template <typename T, int UNIT>
 hipError_t launch_type(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     if (by_columns(g.m, g.n, g.k, UNIT)) {
-        if constexpr (UNIT == 16)
-            if (g.m > 16) return launch_few<T, 2, true>(g, stream);
+        if constexpr (UNIT >= 4)
+            if (g.m > 16) return launch_few<T, 2, UNIT == 16>(g, stream);
         return launch_few<T, 1, UNIT == 16>(g, stream);
     }
     uint32_t parts = column_parts(g.m, g.n, g.k, UNIT);
