@@ -23,10 +23,11 @@ namespace {
 // The buffers are four arrays by name and the two steps of a round stand one after the other in the code: the compiler then knows
 // that reads of one buffer do not wait for what is arriving in the other.  The products appear once per buffer and nowhere else
 // (no tail outside the loop): a second copy of the accumulators would not fit the registers.
-template <int TM_, int TN_, int WM_, int WN_, int STEP_, bool DIRECT_>
+template <int TM_, int TN_, int WM_, int WN_, int STEP_, bool DIRECT_, bool WORDS_ = true>
 struct Tile {
     static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, STEP = STEP_;
     static constexpr bool DIRECT = DIRECT_;
+    static constexpr bool WORDS = WORDS_;                        // the columns may end within a 16-byte part, at whole 4 bytes
     static constexpr int W = WM * WN;
     static constexpr int FM = TM / WM / 16, FQ = TN / WN / 64;   // a wave's fragments: of 16 tokens, and 4 x 16 channels
     static constexpr int PARTS = STEP / 16, ROWS = 64 / PARTS;   // 16-byte parts of a row; rows in a piece of 1 KB, which a wave fetches at a time
@@ -182,9 +183,12 @@ struct Source {
         for (int j = 0; j < G::LA; ++j)
             if (part(j) * 16 + 16 > left) {
                 v4i* at = (v4i*)(a + (j * G::W + wave) * 1024 + lane * 16);
-                v4i v = *at;
+                v4i v = {0, 0, 0, 0};
+                if constexpr (G::WORDS) {   // (with this 8192^3 takes 443 us instead of 432)
+                    v = *at;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = part(j) * 16 + i * 4 < left ? v[i] : 0;
+                    for (int i = 0; i < 4; ++i) v[i] = part(j) * 16 + i * 4 < left ? v[i] : 0;
+                }
                 *at = v;
             }
     }
@@ -694,11 +698,13 @@ hipError_t launch_parts(const MatmulArgs& g, uint32_t parts, void* workspace, hi
     return hipGetLastError();
 }
 
-template <typename T, bool DIRECT>
+// UNIT: the rows lie at multiples of 16 bytes, of 4, or anywhere.
+template <typename T, int UNIT>
 hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
+    constexpr bool DIRECT = UNIT >= 4;
     const uint64_t large = ((g.m + 255) / 256) * ((g.n + 255) / 256), middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
     if constexpr (DIRECT)
-        if (large >= 128) return launch_tile_shape<T, Tile<256, 256, 4, 2, 128, true>>(g, stream);
+        if (large >= 128) return launch_tile_shape<T, Tile<256, 256, 4, 2, 128, true, UNIT == 4>>(g, stream);
     if (middle >= 192) return launch_tile_shape<T, Tile<128, 128, 2, 2, 128, DIRECT>>(g, stream);
     // Small tiles wait for memory once a step: longer steps where there are columns for them, the longest (a workgroup a CU) where there
     // are no more tiles than CUs.  128 / 256 / 512 columns: 128 x 4096 x 4096 24.8 / 16.6 / 14.3 us, 256 x 8192 x 8192 50.6 / 40.0 / 47.6,
@@ -711,7 +717,6 @@ hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
     return launch_tile_shape<T, Tile<64, 64, 4, 1, 128, DIRECT>>(g, stream);
 }
 
-// UNIT: the rows lie at multiples of 16 bytes, of 4, or anywhere.
 template <typename T, int UNIT>
 hipError_t launch_type(const MatmulArgs& g, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     if (by_columns(g.m, g.n, g.k, UNIT)) {
@@ -721,7 +726,7 @@ hipError_t launch_type(const MatmulArgs& g, void* workspace, size_t workspace_by
     }
     uint32_t parts = column_parts(g.m, g.n, g.k, UNIT);
     while (parts > 1 && parts_bytes(g.m, g.n, parts) > workspace_bytes) --parts;
-    return parts > 1 ? launch_parts<T, UNIT >= 4>(g, parts, workspace, stream) : launch_tiles<T, UNIT >= 4>(g, stream);
+    return parts > 1 ? launch_parts<T, UNIT >= 4>(g, parts, workspace, stream) : launch_tiles<T, UNIT>(g, stream);
 }
 
 bool rows_at(const MatmulArgs& g, uint32_t bytes) {
@@ -744,7 +749,7 @@ hipError_t launch_head_sums(const HeadArgs& h, hipStream_t stream) {
     MatmulArgs g = h.product;
     g.out = h.sums;
     g.ldo = h.groups;
-    return launch_tile_shape<void, Tile<256, 256, 4, 2, 128, true>>(g, stream);
+    return launch_tile_shape<void, Tile<256, 256, 4, 2, 128, true, false>>(g, stream);
 }
 
 hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream) {

@@ -120,7 +120,7 @@ SIZES = [(1, 1, 1), (1, 16, 64), (2, 15, 63), (3, 17, 65), (16, 64, 128), (17, 6
          (63, 257, 144), (64, 64, 2048), (65, 70, 256), (127, 129, 112), (128, 128, 128), (129, 127, 384), (200, 260, 528), (255, 513, 192),
          (256, 256, 256), (257, 255, 1040), (300, 1, 320), (1, 1, 70000), (700, 40, 96), (513, 770, 160), (64, 130, 4096), (33, 1000, 4112), (100, 66, 8192),
          (200, 500, 5008), (18, 100, 3000), (65, 64, 20000), (31, 70, 9216), (16, 64, 4099), (2, 600, 5001), (1, 300, 8197),
-         (100, 250, 2047), (100, 250, 2051)]
+         (100, 250, 2047), (100, 250, 2051), (3000, 4100, 196), (1700, 1900, 332), (130, 70, 4), (40, 100, 12), (1, 5, 20), (30, 4000, 1028)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=str)
