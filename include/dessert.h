@@ -372,7 +372,7 @@ dessert_status_t dessert_probe_mix_bandwidth(const void *in_dev, void *out_dev, 
  * overlap (other streams, captured graphs that may replay at the same time) need one each.  Strides count elements
  * from row to row; what lies between the rows is neither used nor written.  Outputs may not overlap inputs.  Arrays
  * need the alignment of their elements, workspaces 256 bytes; rows that begin at multiples of 16 bytes are read
- * faster.  Results are the same bits from call to call. */
+ * fastest, int8 rows at multiples of 4 (addresses, strides and n_cols) nearly as fast.  Results are the same bits from call to call. */
 
 /* Rows of numbers to int8 codes with one scale a row, x ~ scale * code:
  *   DESSERT_SCALE_MAXABS: scale = max |x| * (1 / 127), both factors and the product rounded to 32-bit floats, code = x / scale,
@@ -421,7 +421,8 @@ dessert_status_t dessert_token_logprobs(const dessert_index_t *index, const void
                                         void *workspace_dev, size_t workspace_bytes, float *out_logprobs_dev,
                                         float *out_entropy_dev, uint32_t *out_top_ids_dev, float *out_top_logprobs_dev);
 
-/* The same from a model's last states and its vocabulary matrix in int8, without the logits in memory:
+/* The same from a model's last states and its vocabulary matrix in int8; the workspace holds the logits of some rows at a
+ * time, or none where there are many rows:
  *   l[i][j] = float(sum_c a[i][c] * vocab[j][c]) * (a_scales[i] * vocab_scales[j])
  * in 32-bit float, operands as in dessert_scaled_matmul, outputs and tokens as in dessert_token_logprobs. */
 size_t dessert_head_logprobs_workspace_bytes(const dessert_index_t *index, uint64_t n_rows, uint32_t n_vocab, uint32_t n_cols,
