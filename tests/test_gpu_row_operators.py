@@ -512,6 +512,37 @@ def test_captured_into_a_graph_and_replayed_with_new_inputs(n):
                 assert torch.equal(u.view(torch.int32), v.view(torch.int32))
 
 
+@pytest.mark.parametrize("m,n,k", [(64, 1024, 4096), (20, 130, 4101), (100, 300, 8196)])
+def test_parts_of_the_columns_captured_and_replayed(m, n, k):
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ix = dz.create(128, 32, 7, seed=3)
+        a, sa, b, sb, c = (t.to(DEV) for t in product_inputs(m, n, k, 1))
+        out = torch.empty(m, n, device=DEV)
+        ws = torch.empty(dz.scaled_matmul_workspace_bytes(ix, m, n, k), dtype=torch.uint8, device=DEV)
+        assert ws.numel()
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            dz.scaled_matmul(ix, a, sa, b, sb, c, out=out, workspace=ws)
+        for seed in range(2, 6):
+            for t, new in zip((a, sa, b, sb, c), product_inputs(m, n, k, seed)):
+                t.copy_(new)
+            ws.fill_(seed)
+            out.zero_()
+            graph.replay()
+            replayed = out.clone()
+            side.synchronize()
+            assert torch.equal(replayed, dz.scaled_matmul(ix, a, sa, b, sb, c))
+            assert torch.equal(replayed, torch.cat([dz.scaled_matmul(ix, a[i:i + 16], sa[i:i + 16], b, sb, c) for i in range(0, m, 16)]))
+
+
+def test_workspaces_of_sizes_that_are_refused(ix):
+    for m, n, k in [(2 ** 40, 5, 9000), (5, 2 ** 63, 9000), (5, 5, 131072), (0, 5, 9000)]:
+        assert dz.scaled_matmul_workspace_bytes(ix, m, n, k) == 0
+    assert dz.head_logprobs_workspace_bytes(ix, 5, 1000, 131072, 3) == 0
+
+
 def test_a_handle_on_another_stream_takes_tensors_made_here():
     """Copies, outputs and workspaces that the binding makes on the current stream go to work on the handle's."""
     side = torch.cuda.Stream()
