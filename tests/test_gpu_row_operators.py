@@ -57,7 +57,7 @@ def check_quantize(ix, x, unit, pad=0, at=0):
 def test_quantize_sizes(ix, dtype, unit):
     g = gen(1)
     for rows, cols in [(1, 1), (1, 2), (3, 7), (17, 8), (5, 63), (33, 127), (16, 128), (15, 129), (9, 500), (4, 1023), (6, 1024), (3, 1025), (2, 2047),
-                       (3, 4096), (2, 8200), (1, 40000)]:
+                       (3, 4096), (2, 8192), (2, 8200), (3, 16384), (2, 16385), (1, 40000)]:
         x = (torch.randn(rows, cols, generator=g) * torch.exp(torch.randn(rows, 1, generator=g))).to(dtype)
         for pad, at in [(0, 0), (1, 0), (8, 3)]:
             say("quantize", dtype, unit, rows, cols, pad, at)
@@ -208,7 +208,7 @@ def check_token(ix, x, tokens, n_top, pad=0, at=0):
 
 @pytest.mark.parametrize("dtype", FLOATS)
 @pytest.mark.parametrize("shape", [(1, 1), (1, 2), (2, 7), (3, 64), (5, 255), (4, 257), (9, 2048), (7, 2049), (3, 8191), (2, 8200), (5, 30001), (1, 131071),
-                                   (1030, 513), (1025, 8300)], ids=str)
+                                   (1030, 513), (1025, 8300), (100, 9600), (100, 9601), (24, 2300), (200, 20000)], ids=str)
 def test_logprob_sizes(ix, shape, dtype):
     g = gen(shape[1])
     x = (3 * torch.randn(*shape, generator=g)).to(dtype)
