@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "kernels.hpp"
+#include "launch_slices.hpp"
 #include "number_formats.hpp"
 
 namespace dessert {
@@ -208,9 +209,10 @@ __global__ __launch_bounds__(1024) void quantize_long_rows_kernel(const T* __res
 
 template <typename T, int G, int RUNS, int ROWS, bool UNIT>
 void launch_shape(const T* x, uint64_t rows, uint32_t cols, uint64_t stride, int8_t* codes, float* scales, hipStream_t stream) {
-    constexpr uint64_t per = 256 / G * ROWS;
-    quantize_rows_kernel<T, G, RUNS, ROWS, UNIT><<<dim3((uint32_t)((rows + per - 1) / per)), dim3(256), 0, stream>>>(x, rows, cols, stride, codes,
-                                                                                                                     scales);
+    in_launches(rows, 256 / G * ROWS, 256, [&](uint64_t first, uint64_t n, uint32_t workgroups) {
+        quantize_rows_kernel<T, G, RUNS, ROWS, UNIT><<<dim3(workgroups), dim3(256), 0, stream>>>(x + first * stride, n, cols, stride,
+                                                                                                 codes + first * cols, scales + first);
+    });
 }
 
 // As few lanes a row as hold it in 2 to 4 runs; several short rows a lane where there are enough rows to fill the chip anyway.
@@ -227,7 +229,11 @@ hipError_t launch_type(const void* data, uint64_t rows, uint32_t cols, uint64_t 
     else if (cols <= 4096) launch_shape<T, 256, 2, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
     else if (cols <= 8192) launch_shape<T, 256, 4, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
     else if (cols <= 16384) launch_shape<T, 256, 8, 1, UNIT>(x, rows, cols, stride, codes, scales, stream);
-    else quantize_long_rows_kernel<T, UNIT><<<dim3((uint32_t)rows), dim3(1024), 0, stream>>>(x, cols, stride, codes, scales);
+    else
+        in_launches(rows, 1, 1024, [&](uint64_t first, uint64_t, uint32_t workgroups) {
+            quantize_long_rows_kernel<T, UNIT><<<dim3(workgroups), dim3(1024), 0, stream>>>(x + first * stride, cols, stride, codes + first * cols,
+                                                                                            scales + first);
+        });
     return hipGetLastError();
 }
 
