@@ -4,6 +4,7 @@
 // and two parts of a row join by moving both to the larger m: s' = e^d s, t' = e^d (t + d s) with d = m - m'.
 // Entries of -inf have no probability and are never an alternative; a row with +inf or NaN has s = NaN and gives NaN.
 #include "kernels.hpp"
+#include "launch_slices.hpp"
 #include "number_formats.hpp"
 
 namespace dessert {
@@ -499,15 +500,33 @@ __global__ __launch_bounds__(256) void head_best_kernel(HeadArgs h) {
 }
 
 template <typename T>
-hipError_t launch_type(const LogprobArgs& g, hipStream_t stream) {
+hipError_t launch_rows(const LogprobArgs& g, hipStream_t stream) {
     const dim3 grid((uint32_t)(g.rows * g.splits));
     if (g.segment <= 2048) token_logprobs_kernel<T, 8><<<grid, dim3(256), 0, stream>>>(g);
     else token_logprobs_kernel<T, 16><<<grid, dim3(256), 0, stream>>>(g);
-    if (g.splits > 1) {
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        join_logprobs_kernel<T><<<dim3((uint32_t)g.rows), dim3(256), 0, stream>>>(g);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_type(const LogprobArgs& g, hipStream_t stream) {
+    hipError_t e = hipSuccess;
+    if (g.splits == 1) {   // any number of rows
+        in_launches(g.rows, 1, 256, [&](uint64_t first, uint64_t n, uint32_t) {
+            LogprobArgs part = g;
+            part.rows = n;
+            part.logits = (const T*)g.logits + first * g.stride;
+            if (g.tokens) part.tokens = g.tokens + first;
+            if (g.logprobs) part.logprobs = g.logprobs + first;
+            if (g.entropy) part.entropy = g.entropy + first;
+            if (g.n_top) part.top_ids = g.top_ids + first * g.n_top;
+            if (g.n_top) part.top_logprobs = g.top_logprobs + first * g.n_top;
+            if (e == hipSuccess) e = launch_rows<T>(part, stream);
+        });
+        return e;
     }
+    e = launch_rows<T>(g, stream);   // fewer than 1024 rows (logprob_plan)
+    if (e != hipSuccess) return e;
+    join_logprobs_kernel<T><<<dim3((uint32_t)g.rows), dim3(256), 0, stream>>>(g);
     return hipGetLastError();
 }
 

@@ -61,3 +61,34 @@ def test_quantize_more_rows_of_a_workgroup_each_than_a_launch_takes(ix):
     pick = around((1 << 24) - 1, n=n)
     few, few_scales = dz.quantize_rows(ix, x[pick].contiguous())
     assert torch.equal(codes[pick], few) and torch.equal(scales[pick], few_scales)
+
+
+@pytest.mark.parametrize("with_tokens", [True, False])
+def test_logprobs_of_more_rows_than_a_launch_takes(ix, with_tokens):
+    """Pairs of logits: p and 1 - p by the logistic function; every 11th row has one entry."""
+    n = (1 << 24) + 5
+    say("logprobs", n, 2, with_tokens)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    x = 3 * torch.randn(n, 2, generator=g, device=DEV)
+    x[::11, 1] = -float("inf")
+    tokens = torch.randint(0, 2, (n,), generator=g, device=DEV, dtype=torch.int32)
+    tokens[::7] = -1
+    outs = (torch.full((n,), 5.0, device=DEV), torch.full((n,), 5.0, device=DEV), torch.zeros(n, 1, dtype=torch.int32, device=DEV).view(torch.uint32),
+            torch.full((n, 1), 5.0, device=DEV))
+    lp, entropy, ids, top = dz.token_logprobs(ix, x, tokens if with_tokens else None, 1, outs=outs)
+    l = torch.log_softmax(x.double(), 1)
+    p = l.exp()
+    # 32-bit steps: |l - m| <= 26 (6 standard deviations of 4.25) rounds twice, as a difference and with the logarithm; the sum of at most 2 is
+    # off by at most (3 |d| + 4) e^d, below 6, and its logarithm by 1 more
+    tol = 64 * 2.0 ** -24
+    want = l.gather(1, tokens.clamp(min=0).long()[:, None])[:, 0]
+    want[tokens == -1] = 0.0
+    if with_tokens:
+        masked = want.isinf()
+        assert torch.equal(lp.isinf(), masked) and (lp[~masked].double() - want[~masked]).abs().max() <= tol
+    else:
+        assert lp is None
+    assert (entropy.double() + torch.special.xlogy(p, p).sum(1)).abs().max() <= tol
+    assert torch.equal(ids.view(torch.int32)[:, 0], (x[:, 1] > x[:, 0]).to(torch.int32))
+    assert (top[:, 0].double() - l.amax(1)).abs().max() <= tol
