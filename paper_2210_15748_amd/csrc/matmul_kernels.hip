@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "kernels.hpp"
+#include "launch_slices.hpp"
 #include "number_formats.hpp"
 
 namespace dessert {
@@ -530,15 +531,29 @@ bool by_columns(uint64_t m, uint64_t n, uint32_t k, int unit) {
 
 // As many parts of the columns as give 2048 waves, 8 at most: one token x 32000 x 1024 with 1 / 2 / 4 / 8 parts 10.3 / 8.9 / 13.2 / 21.6 us,
 // x 4096 x 4096 20.5 / 11.8 / 7.5 / 6.1, x 8192 x 8192 39 / 22 / 15.4 / 16.0.
+template <typename T, int MT, int KS, bool ALIGNED>
+hipError_t launch_few_parts(const MatmulArgs& g, hipStream_t stream) {
+    hipError_t e = hipSuccess;
+    in_launches(g.n, 16 * (8 / KS), 512, [&](uint64_t first, uint64_t n, uint32_t workgroups) {
+        MatmulArgs part = g;
+        part.b = g.b + first * g.ldb;
+        part.sb = g.sb + first;
+        if (g.bias) part.bias = g.bias + first;
+        part.out = (T*)g.out + first;
+        part.n = n;
+        scaled_matmul_few_kernel<T, MT, KS, ALIGNED><<<dim3(workgroups), dim3(512), 0, stream>>>(part);
+        if (e == hipSuccess) e = hipGetLastError();
+    });
+    return e;
+}
+
 template <typename T, int MT, bool ALIGNED>
 hipError_t launch_few(const MatmulArgs& g, hipStream_t stream) {
     const uint64_t groups = (g.n + 15) / 16;
-    const auto grid = [&](int ks) { return dim3((uint32_t)((groups + 8 / ks - 1) / (8 / ks))); };
-    if (groups >= 2048) scaled_matmul_few_kernel<T, MT, 1, ALIGNED><<<grid(1), dim3(512), 0, stream>>>(g);
-    else if (groups >= 1024) scaled_matmul_few_kernel<T, MT, 2, ALIGNED><<<grid(2), dim3(512), 0, stream>>>(g);
-    else if (groups >= 512) scaled_matmul_few_kernel<T, MT, 4, ALIGNED><<<grid(4), dim3(512), 0, stream>>>(g);
-    else scaled_matmul_few_kernel<T, MT, 8, ALIGNED><<<grid(8), dim3(512), 0, stream>>>(g);
-    return hipGetLastError();
+    if (groups >= 2048) return launch_few_parts<T, MT, 1, ALIGNED>(g, stream);
+    if (groups >= 1024) return launch_few_parts<T, MT, 2, ALIGNED>(g, stream);
+    if (groups >= 512) return launch_few_parts<T, MT, 4, ALIGNED>(g, stream);
+    return launch_few_parts<T, MT, 8, ALIGNED>(g, stream);
 }
 
 template <typename T, typename G>

@@ -92,3 +92,28 @@ def test_logprobs_of_more_rows_than_a_launch_takes(ix, with_tokens):
     assert (entropy.double() + torch.special.xlogy(p, p).sum(1)).abs().max() <= tol
     assert torch.equal(ids.view(torch.int32)[:, 0], (x[:, 1] > x[:, 0]).to(torch.int32))
     assert (top[:, 0].double() - l.amax(1)).abs().max() <= tol
+
+
+@pytest.mark.parametrize("at", [0, 1])
+def test_matmul_of_a_token_with_more_channels_than_a_launch_takes(ix, at):
+    """at: rows at whole 16 bytes, or anywhere."""
+    n, k = (1 << 30) + 100, 16                           # 128 channels a workgroup of 512
+    say("matmul", 1, n, k, at)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    a = torch.randint(-128, 128, (1, k), generator=g, device=DEV, dtype=torch.int8)
+    b = torch.empty(n * k + at, dtype=torch.int8, device=DEV)[at:].view(n, k)
+    for part in b.split(1 << 26):
+        part.random_(-128, 128, generator=g)
+    sb = torch.rand(n, generator=g, device=DEV) + 0.5
+    bias = torch.rand(n, generator=g, device=DEV)
+    sa = torch.tensor([0.01], device=DEV)
+    out = torch.full((1, n), 5.0, dtype=torch.float16, device=DEV)
+    dz.scaled_matmul(ix, a, sa, b, sb, bias, out=out)
+    step = 1 << 23
+    for lo in range(0, n, step):
+        hi = min(n, lo + step)
+        p = (b[lo:hi].float() * a.float()).sum(1).double() * sa.double() * sb[lo:hi].double()     # whole numbers below 2^24: exact sums
+        want = p + bias[lo:hi].double()
+        tol = 3.01 * 2.0 ** -24 * p.abs() + (1.01 * 2.0 ** -24 + 1.01 * 2.0 ** -11) * want.abs() + 2.0 ** -25
+        assert ((out[0, lo:hi].double() - want).abs() <= tol).all()

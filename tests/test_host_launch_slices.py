@@ -54,7 +54,8 @@ def test_slices_cover_every_item_once_and_fit_a_launch(slices, per, threads):
     assert slices(0, per, threads) == []
 
 
-@pytest.mark.parametrize("source,kernels", [("quantize_kernels", {"quantize_rows_kernel", "quantize_long_rows_kernel"})])
+@pytest.mark.parametrize("source,kernels", [("quantize_kernels", {"quantize_rows_kernel", "quantize_long_rows_kernel"}),
+                                            ("matmul_kernels", {"scaled_matmul_few_kernel"})])
 def test_what_a_call_sizes_freely_is_launched_in_slices(source, kernels):
     """Every launch of these kernels takes its number of workgroups from a slice."""
     text = (CSRC / (source + ".hip")).read_text()
