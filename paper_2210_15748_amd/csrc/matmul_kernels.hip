@@ -165,6 +165,11 @@ struct Source {
             __builtin_amdgcn_s_waitcnt(0xC07F);
         }
     }
+    // Before the barrier behind which all waves read a step: what this wave fetched of it is in LDS.  (The compiler put the same wait there by
+    // itself; with it written out the instructions are the same.)
+    __device__ void arrived() const {
+        if constexpr (G::DIRECT) __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+    }
     // After the last tile the fetches repeat its steps, which nobody reads.
     __device__ void advance() {
         if (++step == steps) {
@@ -397,6 +402,7 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
     src.advance();
     for (;;) {
         if (partial && step == steps - 1) src.clear_tail(a0);
+        src.arrived();
         __syncthreads();
         src.fetch(a1, b1);
         multiply_step<G>(acc, a0, b0, wm, wn, lane);
@@ -413,6 +419,7 @@ __global__ __launch_bounds__(64 * G::W) void scaled_matmul_kernel(MatmulArgs g) 
             if (tile >= tiles) break;
         }
         if (partial && step == steps - 1) src.clear_tail(a1);
+        src.arrived();
         __syncthreads();
         src.fetch(a0, b0);
         multiply_step<G>(acc, a1, b1, wm, wn, lane);
