@@ -1420,69 +1420,6 @@ dessert_status_t dessert_token_logprobs(const dessert_index_t* ix, const void* l
     return DESSERT_OK;
 }
 
-namespace {
-// The head form goes through the rows in turns.  Few rows, short vocabularies and rows at odd bytes: a product that writes the turn's 32-bit
-// logits, a pass that reads them while they still lie in the 256 MB cache (4096 x 32000 x 2048 with 64 / 128 / 256 / 600 MB of logits a turn:
-// 511 / 416 / 419 / 456 us).  Otherwise by groups of the vocabulary, without the logits (kernels.hpp).
-constexpr size_t HEAD_TURN_BYTES = 256u << 20;
-struct HeadPlan {
-    uint64_t rows;     // of a turn
-    uint64_t stride;   // floats from row to row
-    LogprobPlan pass;
-    size_t logits_bytes, pass_bytes, bytes;
-};
-HeadPlan head_plan(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
-    HeadPlan h{};
-    h.stride = ((uint64_t)vocab + 31) / 32 * 32;
-    // Of the numbers of rows that fit, the one with the least time a row: whole rounds of 256 x 256 tiles over the 256 CUs, a third of a
-    // round's time for each 256 tiles' worth of logits to read, and a seventh for two launches.
-    const uint64_t across = (vocab + 255) / 256, most = std::min<uint64_t>((rows + 255) / 256, HEAD_TURN_BYTES / (1024 * h.stride));
-    double best = 1e30;
-    h.rows = 256;
-    for (uint64_t n = 1; n <= most && n <= 4096; ++n) {
-        const uint64_t tiles = n * across, rounds = (tiles + 255) / 256;
-        const double cost = (rounds + 0.35 * tiles / 256 + 0.15) / n;
-        if (cost < best * 0.999) {
-            best = cost;
-            h.rows = n * 256;
-        }
-    }
-    if (h.rows > rows) h.rows = rows;
-    h.pass = logprob_plan(h.rows, vocab, n_top);
-    h.logits_bytes = align_up((size_t)h.rows * h.stride * 4, 256);
-    h.pass_bytes = align_up(h.pass.bytes, 256);
-    h.bytes = h.logits_bytes + h.pass_bytes + scaled_matmul_workspace(h.rows, vocab, k);
-    return h;
-}
-
-struct GroupPlan {
-    uint64_t rows;     // of a turn, 0: does not pay
-    uint32_t groups;
-    size_t sums, counts, lists, picked, totals, logits, bytes;
-};
-GroupPlan group_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
-    GroupPlan p{};
-    p.groups = (vocab + HEAD_GROUP - 1) / HEAD_GROUP;
-    if (((rows + 255) / 256) * ((vocab + 255) / 256) < 128 || p.groups < 4 * n_top) return p;
-    const size_t row_bytes = (size_t)p.groups * (16 + 4) + (size_t)n_top * (4 + 4 * HEAD_GROUP) + 8;
-    p.rows = HEAD_TURN_BYTES / row_bytes / 256 * 256;
-    if (p.rows < 256) p.rows = 256;
-    if (p.rows > rows) p.rows = rows;
-    const auto place = [&](size_t bytes) {
-        const size_t at = p.bytes;
-        p.bytes += align_up(bytes, 256);
-        return at;
-    };
-    p.sums = place((size_t)p.rows * p.groups * 16);
-    p.counts = place((size_t)p.groups * 4);
-    p.lists = place(n_top ? (size_t)p.groups * p.rows * 4 : 0);
-    p.picked = place((size_t)p.rows * n_top * 4);
-    p.totals = place((size_t)p.rows * 8);
-    p.logits = place((size_t)p.rows * n_top * HEAD_GROUP * 4);
-    return p;
-}
-}  // namespace
-
 size_t dessert_head_logprobs_workspace_bytes(const dessert_index_t* ix, uint64_t n_rows, uint32_t n_vocab, uint32_t n_cols, uint32_t n_top) {
     if (!ix || n_vocab == 0 || n_vocab > MAX_COLS || n_rows == 0 || n_rows >= MAX_ROWS || n_cols > MAX_PRODUCT_COLS) return 0;
     // which of the two it is depends on how the rows lie

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "hash_riders.hpp"
+#include "row_plans.hpp"
 
 namespace dessert {
 
@@ -259,8 +260,7 @@ struct MatmulArgs {
     uint32_t tiles_m, tiles_n, part_cols;   // set by the launch
 };
 bool scaled_matmul_aligned(const MatmulArgs& g);   // rows that the fast tiles can read
-// With less than scaled_matmul_workspace bytes the columns are not split; the results are the same bits.
-size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k);
+// With less than scaled_matmul_workspace bytes the columns are split less or not; the results are the same bits.
 hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void* workspace, size_t workspace_bytes, hipStream_t stream);
 struct LogprobArgs {
     const void* logits;       // [rows] rows of vocab, stride apart
@@ -275,19 +275,13 @@ struct LogprobArgs {
     float* part_sums;
     uint64_t* part_keys;
 };
-constexpr uint32_t LOGPROB_MAX_TOP = 64;   // one entry of the list a lane
-struct LogprobPlan {
-    uint32_t splits, segment;
-    size_t sums_bytes, bytes;   // workspace: of the sums, and altogether
-};
-LogprobPlan logprob_plan(uint64_t rows, uint32_t vocab, uint32_t n_top);
 hipError_t launch_token_logprobs(LogprobArgs g, uint32_t dtype, const LogprobPlan& p, void* workspace, hipStream_t stream);
 
 // Log probabilities from int8 states without all logits in memory: the product with the sums of each row and group of HEAD_GROUP channels
 // instead of results (launch_head_sums); a row's sums joined, and the n_top groups with the largest logits picked, among which its n_top best
 // entries are (launch_head_rows).  With n_top > 0: the picks by group (launch_head_lists); those groups' logits once more, for the rows on the
 // list (launch_head_groups); the best of them (launch_head_best).
-constexpr uint32_t HEAD_GROUP = 128, HEAD_LIST_STEP = 32;
+constexpr uint32_t HEAD_LIST_STEP = 32;
 struct HeadArgs {
     MatmulArgs product;       // a: states, b: vocabulary; out unused
     LogprobArgs outputs;      // tokens and outputs; logits unused

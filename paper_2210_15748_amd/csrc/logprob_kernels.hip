@@ -532,26 +532,6 @@ hipError_t launch_type(const LogprobArgs& g, hipStream_t stream) {
 
 }  // namespace
 
-// A row to a workgroup, or to several and a second launch that joins them: 1 workgroup / several for 384 rows x 4000 7.9 / 12.4 us, x 32000
-// 20.2 / 24.1, x 128000 56.5 / 43.5, for 700 rows x 128000 65.1 / 60.4, for 1023 x 32000 27.5 / 33.3, x 128000 73.8 / 75.1 (bf16, 10 alternatives).
-LogprobPlan logprob_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
-    LogprobPlan p{};
-    if (rows >= 1024 || vocab <= 2048 || vocab <= 96 * rows) {
-        p.segment = (vocab + 8191) / 8192 * 8192;
-    } else {
-        // a few workgroups a CU
-        uint64_t splits = (2048 + rows - 1) / rows, most = (vocab + 2047) / 2048;
-        if (splits > most) splits = most;
-        p.segment = (uint32_t)(((vocab + splits - 1) / splits + 2047) / 2048 * 2048);
-    }
-    p.splits = (vocab + p.segment - 1) / p.segment;
-    if (p.splits > 1) {
-        p.sums_bytes = ((size_t)rows * p.splits * 12 + 255) / 256 * 256;
-        p.bytes = p.sums_bytes + ((size_t)rows * p.splits * n_top * 8 + 255) / 256 * 256;
-    }
-    return p;
-}
-
 hipError_t launch_token_logprobs(LogprobArgs g, uint32_t dtype, const LogprobPlan& p, void* workspace, hipStream_t stream) {
     if (g.rows == 0) return hipSuccess;
     g.splits = p.splits;

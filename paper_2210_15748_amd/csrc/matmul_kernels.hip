@@ -525,17 +525,6 @@ __global__ __launch_bounds__(512) void scaled_matmul_few_kernel(MatmulArgs g) {
 #endif
 }
 
-// Which numbers of tokens.  From 17 on the tiles' waves, which share what they read, are better where the channels are many or the columns
-// very many: 32 tokens x 4096 x 1024 4.3 by columns, 5.7 us by tiles, x 8000 x 1024 7.5 / 6.9, x 32000 x 1024 15.9 / 14.5, x 4096 x 4096 9.7 /
-// 12.5, x 1024 x 8192 15.1 / 11.9; 16 tokens x 16000 x 256 3.6 / 4.4, x 16000 x 2048 13.2 / 12.0.  Rows at odd bytes cost a wave more
-// here, as the tiles' parts of the columns keep more waves busy (1 token x 1024 x 4097 10.0 / 12.8, x 8191 17.5 / 17.2; 16 x 1024 x 2049 9.5 /
-// 10.3, x 4097 17.3 / 11.4; 32 x 1024 x 8193 46.6 / 18.7).
-bool by_columns(uint64_t m, uint64_t n, uint32_t k, int unit) {
-    if (k < 16) return false;
-    if (m <= 16) return unit >= 4 || k < (m == 1 ? 8192 : 4096);
-    return unit >= 4 && m <= 32 && k < 8192 && n <= 4096;
-}
-
 // As many parts of the columns as give 2048 waves, 8 at most: one token x 32000 x 1024 with 1 / 2 / 4 / 8 parts 10.3 / 8.9 / 13.2 / 21.6 us,
 // x 4096 x 4096 20.5 / 11.8 / 7.5 / 6.1, x 8192 x 8192 39 / 22 / 15.4 / 16.0.
 template <typename T, int MT, int KS, bool ALIGNED>
@@ -691,20 +680,6 @@ __global__ __launch_bounds__(256) void join_parts_kernel(MatmulArgs g, const int
             if (channel + i < g.n) out[i] = (T)y[i];
 }
 
-// Into how many parts the columns of a product in small tiles go, where the tiles alone leave CUs idle for long: 1 / 2 / 4 / 8 parts
-// of 64 x 4096 x 4096 (64 tiles) 13.6 / 13.5 / 12.5 / 15.2 us, of 128 x 4096 x 4096 (128 tiles) 13.6 / 14.7 / 16.1 / 18.5, of 128 x 1024 x 8192
-// (32 tiles) 21.5 / 18.8 / 13.6 / 12.6, of 128 x 4096 x 8192 (128 tiles) 23.1 / 20.9 / 18.2 / 25.1, of 64 x 4096 x 2048 (64 tiles) 8.8 / 10.2 / 10.4.
-// At other addresses a step takes five times as long and parts pay sooner: 1 / 4 / 8 of 64 x 4096 x 8193 78 / 28.0 / 21.6, of 128 x 4096 x 8193 (128
-// tiles) 78 / 29.7 / 35.5, of 64 x 1024 x 2049 19.4 / 11.3; 1 / 4 of 512 x 4096 x 8193 (512 tiles) 75 / 89.
-uint32_t column_parts(uint64_t m, uint64_t n, uint32_t k, int unit) {
-    const uint64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
-    if (by_columns(m, n, k, unit)) return 1;
-    if (unit >= 4) return k < 4096 || k < 64 * tiles ? 1 : k >= 8192 && k >= 256 * tiles ? 8 : 4;
-    return k < 2048 || k < 16 * tiles || tiles > 256 ? 1 : k >= 4096 && tiles <= 64 ? 8 : 4;
-}
-
-size_t parts_bytes(uint64_t m, uint64_t n, uint32_t parts) { return parts < 2 ? 0 : (size_t)parts * m * ((n + 63) / 64 * 64) * 4; }
-
 template <typename T, bool DIRECT>
 hipError_t launch_parts(const MatmulArgs& g, uint32_t parts, void* workspace, hipStream_t stream) {
     using G = Tile<64, 64, 4, 1, DIRECT ? 256 : 128, DIRECT>;
@@ -779,13 +754,6 @@ hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream) {
     const uint64_t items = h.groups + h.product.m * h.n_top / HEAD_LIST_STEP;
     head_groups_kernel<<<dim3((uint32_t)items), dim3(256), 0, stream>>>(h);
     return hipGetLastError();
-}
-
-size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k) {
-    uint32_t parts = 1;   // the most of any addresses that rows of k columns can have
-    for (int unit : {1, 4, 16})
-        if (k % unit == 0) parts = std::max(parts, column_parts(m, n, k, unit));
-    return parts_bytes(m, n, parts);
 }
 
 hipError_t launch_scaled_matmul(const MatmulArgs& g, uint32_t out_dtype, void* workspace, size_t workspace_bytes, hipStream_t stream) {

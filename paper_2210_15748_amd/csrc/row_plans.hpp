@@ -1,0 +1,136 @@
+// How the row operators go about a call of given sizes, and the scratch memory that takes (host code, no HIP).
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace dessert {
+
+constexpr uint32_t LOGPROB_MAX_TOP = 64;   // one entry of the list a lane
+constexpr uint32_t HEAD_GROUP = 128;       // channels of the vocabulary to a group
+
+inline size_t align_bytes(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+// ---- scaled products --------------------------------------------------------------------------------------------------------
+// unit: the rows lie at multiples of 16 bytes, of 4, or of 1.
+// Which numbers of tokens.  From 17 on the tiles' waves, which share what they read, are better where the channels are many or the columns
+// very many: 32 tokens x 4096 x 1024 4.3 by columns, 5.7 us by tiles, x 8000 x 1024 7.5 / 6.9, x 32000 x 1024 15.9 / 14.5, x 4096 x 4096 9.7 /
+// 12.5, x 1024 x 8192 15.1 / 11.9; 16 tokens x 16000 x 256 3.6 / 4.4, x 16000 x 2048 13.2 / 12.0.  Rows at odd bytes cost a wave more
+// here, as the tiles' parts of the columns keep more waves busy (1 token x 1024 x 4097 10.0 / 12.8, x 8191 17.5 / 17.2; 16 x 1024 x 2049 9.5 /
+// 10.3, x 4097 17.3 / 11.4; 32 x 1024 x 8193 46.6 / 18.7).
+inline bool by_columns(uint64_t m, uint64_t n, uint32_t k, int unit) {
+    if (k < 16) return false;
+    if (m <= 16) return unit >= 4 || k < (m == 1 ? 8192 : 4096);
+    return unit >= 4 && m <= 32 && k < 8192 && n <= 4096;
+}
+
+// Into how many parts the columns of a product in small tiles go, where the tiles alone leave CUs idle for long: 1 / 2 / 4 / 8 parts
+// of 64 x 4096 x 4096 (64 tiles) 13.6 / 13.5 / 12.5 / 15.2 us, of 128 x 4096 x 4096 (128 tiles) 13.6 / 14.7 / 16.1 / 18.5, of 128 x 1024 x 8192
+// (32 tiles) 21.5 / 18.8 / 13.6 / 12.6, of 128 x 4096 x 8192 (128 tiles) 23.1 / 20.9 / 18.2 / 25.1, of 64 x 4096 x 2048 (64 tiles) 8.8 / 10.2 / 10.4.
+// At other addresses a step takes five times as long and parts pay sooner: 1 / 4 / 8 of 64 x 4096 x 8193 78 / 28.0 / 21.6, of 128 x 4096 x 8193 (128
+// tiles) 78 / 29.7 / 35.5, of 64 x 1024 x 2049 19.4 / 11.3; 1 / 4 of 512 x 4096 x 8193 (512 tiles) 75 / 89.
+inline uint32_t column_parts(uint64_t m, uint64_t n, uint32_t k, int unit) {
+    const uint64_t tiles = ((m + 63) / 64) * ((n + 63) / 64);
+    if (by_columns(m, n, k, unit)) return 1;
+    if (unit >= 4) return k < 4096 || k < 64 * tiles ? 1 : k >= 8192 && k >= 256 * tiles ? 8 : 4;
+    return k < 2048 || k < 16 * tiles || tiles > 256 ? 1 : k >= 4096 && tiles <= 64 ? 8 : 4;
+}
+
+inline size_t parts_bytes(uint64_t m, uint64_t n, uint32_t parts) { return parts < 2 ? 0 : (size_t)parts * m * ((n + 63) / 64 * 64) * 4; }
+
+inline size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k) {
+    uint32_t parts = 1;   // the most of any addresses that rows of k columns can have
+    for (int unit : {1, 4, 16})
+        if (k % unit == 0) parts = std::max(parts, column_parts(m, n, k, unit));
+    return parts_bytes(m, n, parts);
+}
+
+// ---- log probabilities ------------------------------------------------------------------------------------------------------
+struct LogprobPlan {
+    uint32_t splits, segment;   // of a row over workgroups
+    size_t sums_bytes, bytes;   // workspace: of the sums, and altogether
+};
+// A row to a workgroup, or to several and a second launch that joins them: 1 workgroup / several for 384 rows x 4000 7.9 / 12.4 us, x 32000
+// 20.2 / 24.1, x 128000 56.5 / 43.5, for 700 rows x 128000 65.1 / 60.4, for 1023 x 32000 27.5 / 33.3, x 128000 73.8 / 75.1 (bf16, 10 alternatives).
+inline LogprobPlan logprob_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
+    LogprobPlan p{};
+    if (rows >= 1024 || vocab <= 2048 || vocab <= 96 * rows) {
+        p.segment = (vocab + 8191) / 8192 * 8192;
+    } else {
+        // a few workgroups a CU
+        uint64_t splits = (2048 + rows - 1) / rows, most = (vocab + 2047) / 2048;
+        if (splits > most) splits = most;
+        p.segment = (uint32_t)(((vocab + splits - 1) / splits + 2047) / 2048 * 2048);
+    }
+    p.splits = (vocab + p.segment - 1) / p.segment;
+    if (p.splits > 1) {
+        p.sums_bytes = ((size_t)rows * p.splits * 12 + 255) / 256 * 256;
+        p.bytes = p.sums_bytes + ((size_t)rows * p.splits * n_top * 8 + 255) / 256 * 256;
+    }
+    return p;
+}
+
+// ---- log probabilities from states ------------------------------------------------------------------------------------------
+// The head form goes through the rows in turns.  Few rows, short vocabularies and rows at odd bytes: a product that writes the turn's 32-bit
+// logits, a pass that reads them while they still lie in the 256 MB cache (4096 x 32000 x 2048 with 64 / 128 / 256 / 600 MB of logits a turn:
+// 511 / 416 / 419 / 456 us).  Otherwise by groups of the vocabulary, without the logits (kernels.hpp).
+constexpr size_t HEAD_TURN_BYTES = 256u << 20;
+struct HeadPlan {
+    uint64_t rows;     // of a turn
+    uint64_t stride;   // floats from row to row
+    LogprobPlan pass;
+    size_t logits_bytes, pass_bytes, bytes;
+};
+inline HeadPlan head_plan(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
+    HeadPlan h{};
+    h.stride = ((uint64_t)vocab + 31) / 32 * 32;
+    // Of the numbers of rows that fit, the one with the least time a row: whole rounds of 256 x 256 tiles over the 256 CUs, a third of a
+    // round's time for each 256 tiles' worth of logits to read, and a seventh for two launches.
+    const uint64_t across = (vocab + 255) / 256, most = std::min<uint64_t>((rows + 255) / 256, HEAD_TURN_BYTES / (1024 * h.stride));
+    double best = 1e30;
+    h.rows = 256;
+    for (uint64_t n = 1; n <= most && n <= 4096; ++n) {
+        const uint64_t tiles = n * across, rounds = (tiles + 255) / 256;
+        const double cost = (rounds + 0.35 * tiles / 256 + 0.15) / n;
+        if (cost < best * 0.999) {
+            best = cost;
+            h.rows = n * 256;
+        }
+    }
+    if (h.rows > rows) h.rows = rows;
+    h.pass = logprob_plan(h.rows, vocab, n_top);
+    h.logits_bytes = align_bytes((size_t)h.rows * h.stride * 4, 256);
+    h.pass_bytes = align_bytes(h.pass.bytes, 256);
+    h.bytes = h.logits_bytes + h.pass_bytes + scaled_matmul_workspace(h.rows, vocab, k);
+    return h;
+}
+
+struct GroupPlan {
+    uint64_t rows;     // of a turn, 0: does not pay
+    uint32_t groups;
+    size_t sums, counts, lists, picked, totals, logits, bytes;
+};
+inline GroupPlan group_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
+    GroupPlan p{};
+    p.groups = (vocab + HEAD_GROUP - 1) / HEAD_GROUP;
+    if (((rows + 255) / 256) * ((vocab + 255) / 256) < 128 || p.groups < 4 * n_top) return p;
+    const size_t row_bytes = (size_t)p.groups * (16 + 4) + (size_t)n_top * (4 + 4 * HEAD_GROUP) + 8;
+    p.rows = HEAD_TURN_BYTES / row_bytes / 256 * 256;
+    if (p.rows < 256) p.rows = 256;
+    if (p.rows > rows) p.rows = rows;
+    const auto place = [&](size_t bytes) {
+        const size_t at = p.bytes;
+        p.bytes += align_bytes(bytes, 256);
+        return at;
+    };
+    p.sums = place((size_t)p.rows * p.groups * 16);
+    p.counts = place((size_t)p.groups * 4);
+    p.lists = place(n_top ? (size_t)p.groups * p.rows * 4 : 0);
+    p.picked = place((size_t)p.rows * n_top * 4);
+    p.totals = place((size_t)p.rows * 8);
+    p.logits = place((size_t)p.rows * n_top * HEAD_GROUP * 4);
+    return p;
+}
+
+}  // namespace dessert
