@@ -369,7 +369,8 @@ dessert_status_t dessert_probe_mix_bandwidth(const void *in_dev, void *out_dev, 
  * query's tokens, each given the document) and generated text is scored.
  * They use only the device and the stream of the index (no built index needed) and are a fixed sequence of kernel
  * launches: asynchronous, capturable, nothing allocated.  A workspace is scratch of one call at a time: calls that may
- * overlap (other streams, captured graphs that may replay at the same time) need one each.  Strides count elements
+ * overlap (other streams, captured graphs that may replay at the same time) need one each.  What a ..._workspace_bytes call gives
+ * for a number of rows serves any call of that many rows or fewer (the other sizes the same), wherever they lie.  Strides count elements
  * from row to row; what lies between the rows is neither used nor written.  Outputs may not overlap inputs.  Arrays
  * need the alignment of their elements, workspaces 256 bytes; rows that begin at multiples of 16 bytes are read
  * fastest, int8 rows at multiples of 4 (addresses, strides and n_cols) nearly as fast.  Results are the same bits from call to call. */

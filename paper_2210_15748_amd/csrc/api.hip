@@ -1360,7 +1360,7 @@ dessert_status_t dessert_quantize_rows(const dessert_index_t* ix, const void* x_
 
 size_t dessert_scaled_matmul_workspace_bytes(const dessert_index_t* ix, uint64_t n_rows, uint64_t n_channels, uint32_t n_cols) {
     if (!ix || n_rows >= MAX_ROWS || n_channels >= MAX_ROWS || n_cols > MAX_PRODUCT_COLS) return 0;   // sizes that the call refuses
-    return scaled_matmul_workspace(n_rows, n_channels, n_cols);
+    return scaled_matmul_workspace_upto(n_rows, n_channels, n_cols);
 }
 
 dessert_status_t dessert_scaled_matmul(const dessert_index_t* ix, const int8_t* a_dev, uint64_t a_stride, const float* a_scales_dev,
@@ -1392,7 +1392,7 @@ dessert_status_t dessert_scaled_matmul(const dessert_index_t* ix, const int8_t* 
 
 size_t dessert_token_logprobs_workspace_bytes(const dessert_index_t* ix, uint64_t n_rows, uint32_t n_vocab, uint32_t n_top) {
     if (!ix || n_vocab == 0 || n_vocab > MAX_COLS || n_rows == 0 || n_rows >= MAX_ROWS) return 0;
-    return logprob_plan(n_rows, n_vocab, n_top).bytes;
+    return logprob_workspace_upto(n_rows, n_vocab, n_top);
 }
 
 dessert_status_t dessert_token_logprobs(const dessert_index_t* ix, const void* logits_dev, uint32_t dtype, uint64_t n_rows,
@@ -1422,8 +1422,7 @@ dessert_status_t dessert_token_logprobs(const dessert_index_t* ix, const void* l
 
 size_t dessert_head_logprobs_workspace_bytes(const dessert_index_t* ix, uint64_t n_rows, uint32_t n_vocab, uint32_t n_cols, uint32_t n_top) {
     if (!ix || n_vocab == 0 || n_vocab > MAX_COLS || n_rows == 0 || n_rows >= MAX_ROWS || n_cols > MAX_PRODUCT_COLS) return 0;
-    // which of the two it is depends on how the rows lie
-    return std::max(head_plan(n_rows, n_vocab, n_cols, n_top).bytes, group_plan(n_rows, n_vocab, n_top).bytes);
+    return head_workspace_upto(n_rows, n_vocab, n_cols, n_top);
 }
 
 dessert_status_t dessert_head_logprobs(const dessert_index_t* ix, const int8_t* a_dev, uint64_t a_stride, const float* a_scales_dev,

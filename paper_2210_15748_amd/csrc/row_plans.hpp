@@ -46,6 +46,16 @@ inline size_t scaled_matmul_workspace(uint64_t m, uint64_t n, uint32_t k) {
     return parts_bytes(m, n, parts);
 }
 
+// The most that any number of rows up to m needs.  For one number of parts the bytes grow with the rows, and the parts end where the tiles
+// pass one of column_parts' limits (rows by columns need none): the last rows before each limit and m itself are all there is to look at.
+inline size_t scaled_matmul_workspace_upto(uint64_t m, uint64_t n, uint32_t k) {
+    const uint64_t across = std::max<uint64_t>((n + 63) / 64, 1);
+    size_t bytes = scaled_matmul_workspace(m, n, k);
+    for (uint64_t tiles : {(uint64_t)64, (uint64_t)256, (uint64_t)k / 16, (uint64_t)k / 64, (uint64_t)k / 256})
+        bytes = std::max(bytes, scaled_matmul_workspace(std::min(m, tiles / across * 64), n, k));
+    return bytes;
+}
+
 // ---- log probabilities ------------------------------------------------------------------------------------------------------
 struct LogprobPlan {
     uint32_t splits, segment;   // of a row over workgroups
@@ -69,6 +79,14 @@ inline LogprobPlan logprob_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
         p.bytes = p.sums_bytes + ((size_t)rows * p.splits * n_top * 8 + 255) / 256 * 256;
     }
     return p;
+}
+
+// Enough for any number of rows up to `rows`: their parts are at most 2047 + rows, and `most` a row.
+inline size_t logprob_workspace_upto(uint64_t rows, uint32_t vocab, uint32_t n_top) {
+    if (vocab <= 2048) return 0;
+    const uint64_t r = std::min<uint64_t>(std::min<uint64_t>(rows, 1023), (vocab - 1) / 96);
+    const uint64_t parts = std::min<uint64_t>(r * ((vocab + 2047) / 2048), 2047 + r);
+    return align_bytes(parts * 12, 256) + align_bytes(parts * n_top * 8, 256);
 }
 
 // ---- log probabilities from states ------------------------------------------------------------------------------------------
@@ -131,6 +149,14 @@ inline GroupPlan group_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
     p.totals = place((size_t)p.rows * 8);
     p.logits = place((size_t)p.rows * n_top * HEAD_GROUP * 4);
     return p;
+}
+
+// Enough for any number of rows up to `rows`, whichever of the two it is (that depends on how the rows lie).  A turn's rows do not fall as the
+// rows of the call rise.
+inline size_t head_workspace_upto(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
+    const HeadPlan h = head_plan(rows, vocab, k, n_top);
+    const size_t pass = align_bytes(logprob_workspace_upto(h.rows, vocab, n_top), 256);
+    return std::max(h.logits_bytes + pass + scaled_matmul_workspace_upto(h.rows, vocab, k), group_plan(rows, vocab, n_top).bytes);
 }
 
 }  // namespace dessert
