@@ -449,6 +449,7 @@ def filter_search(ix: Index, q_vectors: torch.Tensor, q_lengths, filter_probe: i
 # ---- beside the search ----------------------------------------------------------------------------------------------------
 _FLOAT_TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
 _INT8, _FLOAT32, _TOKEN_TYPES = (torch.int8,), (torch.float32,), (torch.int32, torch.uint32)
+_MOST = 0x7FFFFFFF
 
 
 def _lend(ix: Index, made) -> None:
@@ -473,6 +474,8 @@ def _rows(ix: Index, t: torch.Tensor, name: str, made, dtypes):
     if len(shape) != 2 or t.dtype not in dtypes or t.device != ix.device:
         raise ValueError(f"{name} must be a matrix on {ix.device} of dtype " + " / ".join(str(d) for d in dtypes))
     n_rows, n_cols = shape
+    if n_rows > _MOST or n_cols > _MOST:      # the library's limit of rows; it takes columns and vocabulary in 32 bits
+        raise ValueError(f"{name} has {n_rows} rows of {n_cols}, at most 2^31 - 1 of each are taken")
     apart, step = t.stride()
     if (n_cols > 1 and step != 1) or (n_rows > 1 and apart < n_cols):
         t = t.contiguous()
@@ -567,6 +570,8 @@ def _tokens(ix: Index, tokens: Optional[torch.Tensor], n: int, made) -> Optional
 
 
 def _logprob_outputs(ix: Index, n: int, n_top: int, tokens, outs, made):
+    if not 0 <= n_top <= _MOST:
+        raise ValueError(f"n_top is {n_top}")
     o = (None,) * 4 if outs is None else outs
     return (None if tokens is None else _output(ix, o[0], (n,), "outs[0]", made, torch.float32),
             _output(ix, o[1], (n,), "outs[1]", made, torch.float32),
