@@ -1,4 +1,4 @@
-// Element types of the row operators (dtype codes as in dessert.h) and their conversions to and from 32-bit floats.
+// Element types of the row operators (dtype codes as in dessert.h) and their conversion from 32-bit floats.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -11,17 +11,7 @@ typedef __bf16 bf16_t;
 
 constexpr uint32_t TYPE_F16 = 1, TYPE_BF16 = 2, TYPE_F32 = 3;
 
-inline uint32_t type_bytes(uint32_t dtype) { return dtype == TYPE_F32 ? 4u : 2u; }
-
-// N elements at any element's address (16-byte accesses need no alignment on this hardware)
-template <typename T, int N>
-__device__ inline void load_run(const T* p, float (&x)[N]) {
-    T v[N];
-    __builtin_memcpy(v, p, sizeof(v));
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = (float)v[i];
-}
-
+// N elements to any element's address (16-byte accesses need no alignment on this hardware)
 template <typename T, int N>
 __device__ inline void store_run(T* p, const float (&x)[N]) {
     T v[N];
