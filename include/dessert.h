@@ -379,9 +379,10 @@ dessert_status_t dessert_probe_mix_bandwidth(const void *in_dev, void *out_dev, 
  *   DESSERT_SCALE_MAXABS: scale = max |x| * (1 / 127), both factors and the product rounded to 32-bit floats, code = x / scale,
  *                         in [-127, 127]
  *   DESSERT_SCALE_UNIT:   code = 127 x / |x| with the Euclidean norm, the vectors of an int8 index; scale = |x| / 127
- * each code the integer nearest to the quotient of these numbers, ties to even.  A row of zeros (or one whose scale
- * underflows to zero) has codes 0 and scale 0; a row that holds an infinity or NaN has codes 0 and scale NaN, so that
- * its products come out as NaN.
+ * each code the integer nearest to the quotient of these numbers, ties to even.  A row of zeros has codes 0 and scale 0.
+ * A scale may underflow to zero (32-bit rows below 2^-143): DESSERT_SCALE_MAXABS then has codes 0, DESSERT_SCALE_UNIT the
+ * direction's codes all the same.  A row that holds an infinity or NaN has codes 0 and scale NaN, so that its products
+ * come out as NaN.
  *   x_dev           dev, [n_rows][n_cols] of dtype (DESSERT_F16, DESSERT_BF16, DESSERT_F32), rows row_stride apart
  *   out_codes_dev   dev, out, [n_rows][n_cols], no padding
  *   out_scales_dev  dev, out, [n_rows] */

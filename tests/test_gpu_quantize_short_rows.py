@@ -80,3 +80,14 @@ def test_short_rows_are_the_same_bits_however_many_there_are(ix, cols, unit):
     for lo in (0, 30000):
         c, s = dz.quantize_rows(ix, x[lo:lo + 35541], scaling)
         assert torch.equal(c, codes[lo:lo + 35541]) and torch.equal(s.view(torch.int32), scales[lo:lo + 35541].view(torch.int32))
+
+
+def test_scales_that_underflow(ix):
+    """The smallest 32-bit numbers: by the largest magnitude there is no scale to divide by; to unit norm the direction is there all the same."""
+    x = torch.zeros(3, 4)
+    x[0, 1], x[1, 1] = 2.0 ** -149, -63 * 2.0 ** -149               # 63 / 127 of the smallest number is below half of it
+    x[2] = torch.tensor([3.0, 0.0, -4.0, 0.0]) * 2.0 ** -147        # norm 5 * 2^-147
+    codes, scales = dz.quantize_rows(ix, x.to(DEV))
+    assert not codes[:2].any() and not scales.any()
+    codes, scales = dz.quantize_rows(ix, x.to(DEV), dz.SCALE_UNIT)
+    assert codes.tolist() == [[0, 127, 0, 0], [0, -127, 0, 0], [76, 0, -102, 0]] and not scales.any()
