@@ -1441,7 +1441,7 @@ dessert_status_t dessert_head_logprobs(const dessert_index_t* ix, const int8_t* 
     LogprobArgs outputs{};
     outputs.vocab = n_vocab; outputs.n_top = n_top;
     const HeadPlan h = head_plan(n_rows ? n_rows : 1, n_vocab, n_cols, n_top);
-    GroupPlan gp = group_plan(n_rows ? n_rows : 1, n_vocab, n_top);
+    GroupPlan gp = group_plan(n_rows ? n_rows : 1, n_vocab, n_cols, n_top);
     if (!scaled_matmul_aligned(product)) gp.rows = 0;
     st = check_workspace(workspace_dev, workspace_bytes, n_rows == 0 ? 0 : gp.rows ? gp.bytes : h.bytes);
     if (st != DESSERT_OK) return st;

@@ -90,9 +90,10 @@ inline size_t logprob_workspace_upto(uint64_t rows, uint32_t vocab, uint32_t n_t
 }
 
 // ---- log probabilities from states ------------------------------------------------------------------------------------------
-// The head form goes through the rows in turns.  Few rows, short vocabularies and rows at odd bytes: a product that writes the turn's 32-bit
-// logits, a pass that reads them while they still lie in the 256 MB cache (4096 x 32000 x 2048 with 64 / 128 / 256 / 600 MB of logits a turn:
-// 511 / 416 / 419 / 456 us).  Otherwise by groups of the vocabulary, without the logits (kernels.hpp).
+// The head form goes through the rows in turns: by a product that writes the turn's 32-bit logits and a pass that reads them while they still lie in
+// the 256 MB cache, or by groups of the vocabulary, without most of the logits (kernels.hpp).
+// Of 16 calls that go by logits (1024 to 16384 rows, vocabularies of 4000 to 128000, 130 to 4096 columns, rows at 16, 4 and odd bytes) turns of at most
+// 128 / 200 / 400 MB take 1.06 / 0.99 / 1.02 times what 256 MB take on average, and 0.87 to 1.67 / 0.89 to 1.20 / 0.90 to 1.13 times.
 constexpr size_t HEAD_TURN_BYTES = 256u << 20;
 struct HeadPlan {
     uint64_t rows;     // of a turn
@@ -104,7 +105,8 @@ inline HeadPlan head_plan(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_
     HeadPlan h{};
     h.stride = ((uint64_t)vocab + 31) / 32 * 32;
     // Of the numbers of rows that fit, the one with the least time a row: whole rounds of 256 x 256 tiles over the 256 CUs, a third of a
-    // round's time for each 256 tiles' worth of logits to read, and a seventh for two launches.
+    // round's time for each 256 tiles' worth of logits to read, and a seventh for two launches.  (The 16 calls above with every number of rows: this
+    // choice takes 1.04 times the best one's time on average; 1.07 to 1.15 times where rows at odd bytes go in tiles of 128 x 128.)
     const uint64_t across = (vocab + 255) / 256, most = std::min<uint64_t>((rows + 255) / 256, HEAD_TURN_BYTES / (1024 * h.stride));
     double best = 1e30;
     h.rows = 256;
@@ -129,10 +131,23 @@ struct GroupPlan {
     uint32_t groups;
     size_t sums, counts, lists, picked, totals, logits, bytes;
 };
-inline GroupPlan group_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
+// Where groups pay, in us: they save a logit's way to memory and back, 1.1 us for 10^6 of them, and spend three launches and, for each row and
+// alternative, its picking and the products of a group.  Logits / groups: 4096 x 32000 x 2048 with 5, 10, 20, 33, 64 alternatives 423 / 308, 418 / 354,
+// 427 / 431, 434 / 528, 448 / 764; x 128 columns 223 / 110, 227 / 132, 233 / 183, 242 / 242, 268 / 383; 1024 x 32000 x 1024 with 0, 5, 10, 20 77 / 46,
+// 79 / 68, 80 / 76, 87 / 95; 300 x 128000 x 1024 with 5, 33, 64 130 / 114, 149 / 143, 155 / 168; 16384 x 4000 x 512 with 0, 1, 5 131 / 82, 134 / 130, 139 / 207;
+// 128 x 50000 x 1024 with 0, 1 38 / 27, 41 / 45.  220 calls drawn apart from those that the numbers were fitted to (64 to 16384 rows, vocabularies of 2048
+// to 150000, 32 to 4096 columns, 0 to 64 alternatives): 1.004 times the better one's time on average, 1.38 at most.
+// The tiles of 256 x 256 that groups are formed in have to fill half of the 256 CUs: 512 x 4000 x 2048 (32 tiles) without alternatives
+// 19 / 34, 64 x 32000 x 1024 (125) 23 / 25, 512 x 16000 x 1024 (126) 29 / 26.
+inline bool groups_pay(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
+    if (((rows + 255) / 256) * ((vocab + 255) / 256) < 128) return false;
+    return n_top == 0 || 1.1e-6 * rows * vocab > 9 + 1e-3 * rows * n_top * (0.9 + 0.0005 * k);
+}
+
+inline GroupPlan group_plan(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
     GroupPlan p{};
     p.groups = (vocab + HEAD_GROUP - 1) / HEAD_GROUP;
-    if (((rows + 255) / 256) * ((vocab + 255) / 256) < 128 || p.groups < 4 * n_top) return p;
+    if (!groups_pay(rows, vocab, k, n_top)) return p;
     const size_t row_bytes = (size_t)p.groups * (16 + 4) + (size_t)n_top * (4 + 4 * HEAD_GROUP) + 8;
     p.rows = HEAD_TURN_BYTES / row_bytes / 256 * 256;
     if (p.rows < 256) p.rows = 256;
@@ -156,7 +171,7 @@ inline GroupPlan group_plan(uint64_t rows, uint32_t vocab, uint32_t n_top) {
 inline size_t head_workspace_upto(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) {
     const HeadPlan h = head_plan(rows, vocab, k, n_top);
     const size_t pass = align_bytes(logprob_workspace_upto(h.rows, vocab, n_top), 256);
-    return std::max(h.logits_bytes + pass + scaled_matmul_workspace_upto(h.rows, vocab, k), group_plan(rows, vocab, n_top).bytes);
+    return std::max(h.logits_bytes + pass + scaled_matmul_workspace_upto(h.rows, vocab, k), group_plan(rows, vocab, k, n_top).bytes);
 }
 
 }  // namespace dessert

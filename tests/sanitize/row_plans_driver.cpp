@@ -30,7 +30,7 @@ int main() {
                     expect(h.logits_bytes >= h.rows * h.stride * 4 && h.pass_bytes >= h.pass.bytes && h.bytes >= h.logits_bytes + h.pass_bytes, "turn's workspace",
                            rows, vocab, k, n_top);
                     expect(h.logits_bytes <= HEAD_TURN_BYTES || h.rows <= 256, "turn's size", rows, vocab, k, n_top);
-                    const GroupPlan g = group_plan(rows, vocab, n_top);
+                    const GroupPlan g = group_plan(rows, vocab, k, n_top);
                     if (g.rows) {
                         expect(g.rows <= rows && (uint64_t)g.groups * HEAD_GROUP >= vocab, "groups", rows, vocab, k, n_top);
                         const size_t at[] = {g.sums, g.counts, g.lists, g.picked, g.totals, g.logits, g.bytes};

@@ -1,6 +1,7 @@
 """Scratch memory of the row operators by sizes: the rules of csrc/row_plans.hpp, compiled for the host.  What a caller is told for a number of rows
 serves every call of as many rows or fewer."""
 import ctypes as C
+import importlib.util
 import pathlib
 import random
 import shutil
@@ -18,8 +19,10 @@ size_t matmul_told(uint64_t m, uint64_t n, uint32_t k, uint32_t) { return scaled
 size_t token_needs(uint64_t rows, uint64_t vocab, uint32_t, uint32_t n_top) { return logprob_plan(rows, (uint32_t)vocab, n_top).bytes; }
 size_t token_told(uint64_t rows, uint64_t vocab, uint32_t, uint32_t n_top) { return logprob_workspace_upto(rows, (uint32_t)vocab, n_top); }
 size_t head_needs(uint64_t rows, uint64_t vocab, uint32_t k, uint32_t n_top) {
-    return std::max(head_plan(rows, (uint32_t)vocab, k, n_top).bytes, group_plan(rows, (uint32_t)vocab, n_top).bytes);
+    return std::max(head_plan(rows, (uint32_t)vocab, k, n_top).bytes, group_plan(rows, (uint32_t)vocab, k, n_top).bytes);
 }
+int by_groups(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) { return groups_pay(rows, vocab, k, n_top); }
+uint64_t group_turn(uint64_t rows, uint32_t vocab, uint32_t k, uint32_t n_top) { return group_plan(rows, vocab, k, n_top).rows; }
 size_t head_told(uint64_t rows, uint64_t vocab, uint32_t k, uint32_t n_top) { return head_workspace_upto(rows, (uint32_t)vocab, k, n_top); }
 }
 """
@@ -39,6 +42,8 @@ def rule(tmp_path_factory):
             f = getattr(lib, f"{call}_{what}")
             f.argtypes = [C.c_uint64, C.c_uint64, C.c_uint32, C.c_uint32]
             f.restype = C.c_size_t
+    lib.by_groups.argtypes = lib.group_turn.argtypes = [C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32]
+    lib.group_turn.restype = C.c_uint64
     return lib
 
 
@@ -86,3 +91,24 @@ def test_it_is_not_more_than_it_has_to_be(rule):
                 largest = max(needs(i, n, k, top) for i in range(1, m + 1))
                 assert told(m, n, k, top) <= 2 * largest + (1 << 17), (call, m, n, k, top)
     assert rule.matmul_told(0, 100, 9000, 0) == 0
+
+
+# rows, vocabulary, columns, alternatives, us by logits, us by groups: calls on both sides (300 x 128000 x 1024 with 64, 155 / 168, is one that the rule misses)
+@pytest.mark.parametrize("n,V,k,top,logits,groups", [
+    (4096, 32000, 2048, 5, 423, 308), (4096, 32000, 2048, 10, 418, 354), (4096, 32000, 2048, 33, 434, 528), (4096, 32000, 2048, 64, 448, 764),
+    (4096, 32000, 128, 20, 233, 183), (4096, 32000, 128, 64, 268, 383), (1024, 32000, 1024, 0, 77, 46), (1024, 32000, 1024, 10, 80, 76),
+    (1024, 32000, 1024, 20, 87, 95), (300, 128000, 1024, 5, 130, 114), (16384, 4000, 512, 0, 131, 82),
+    (16384, 4000, 512, 5, 139, 207), (128, 50000, 1024, 0, 38, 27), (128, 50000, 1024, 1, 41, 45), (4096, 4000, 1024, 5, 49, 78),
+    (512, 4000, 2048, 0, 19, 34), (64, 32000, 1024, 0, 23, 25)])
+def test_groups_where_they_were_measured_to_pay(rule, n, V, k, top, logits, groups):
+    assert bool(rule.by_groups(n, V, k, top)) == (groups < logits)
+
+
+def test_the_calls_that_are_tested_by_groups_go_that_way(rule):
+    spec = importlib.util.spec_from_file_location("head_groups", pathlib.Path(__file__).resolve().parent / "test_gpu_head_groups.py")
+    gpu = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(gpu)
+    for shape in [*gpu.SHAPES, gpu.VALUES, gpu.TURNS, gpu.PARTS, gpu.GRAPH, *((*gpu.SWITCH, top) for top in (1, 8, 20))]:
+        assert rule.by_groups(*shape), shape
+    assert not rule.by_groups(*gpu.SWITCH, 64)
+    assert rule.group_turn(*gpu.TURNS) == 46848 < gpu.TURNS[0]
