@@ -696,12 +696,17 @@ hipError_t launch_parts(const MatmulArgs& g, uint32_t parts, void* workspace, hi
 }
 
 // UNIT: the rows lie at multiples of 16 bytes, of 4, or anywhere.
+// 256^2, where 128^2, two workgroups of which a CU holds, would take more than one round (256^2 / 128^2 tiles, us: 2048 x 4096 x 2048 128 / 512 tiles 33.5 /
+// 23.4, 128 x 50000 x 1024 196 / 391 tiles 23.5 / 16.7, 3000 x 3000 x 2048 144 / 576 tiles 33.8 / 34.4, 4096 x 4096 x 4096 256 / 1024 tiles 67.8 / 70.8;
+// rows at 4 bytes 34.8 / 30.0, 22.9 / 18.9, 36.5 / 40.2, 70.9 / 91.9); through registers they gain nothing (126.3 / 118.8 for 4096^3).
+// 128^2 / 64^2: 2048 x 1024 x 1024 128 / 512 tiles 11.1 / 8.1, 1536 x 2048 x 4096 192 / 768 26.1 / 27.6, 2048 x 2048 x 1024 256 / 1024 12.3 / 13.3, 4096 x 4096 x
+// 4096 70.8 / 114; through registers 18.0 / 12.2, 56.3 / 45.7, 18.7 / 22.1, 119 / 217.
 template <typename T, int UNIT>
 hipError_t launch_tiles(const MatmulArgs& g, hipStream_t stream) {
     constexpr bool DIRECT = UNIT >= 4;
-    const uint64_t large = ((g.m + 255) / 256) * ((g.n + 255) / 256), middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
+    const uint64_t middle = ((g.m + 127) / 128) * ((g.n + 127) / 128);
     if constexpr (DIRECT)
-        if (large >= 128) return launch_tile_shape<T, Tile<256, 256, 4, 2, 128, true, UNIT == 4>>(g, stream);
+        if (middle > 512) return launch_tile_shape<T, Tile<256, 256, 4, 2, 128, true, UNIT == 4>>(g, stream);
     if (middle >= 192) return launch_tile_shape<T, Tile<128, 128, 2, 2, 128, DIRECT>>(g, stream);
     // Small tiles wait for memory once a step: longer steps where there are columns for them, the longest (a workgroup a CU) where there
     // are no more tiles than CUs.  128 / 256 / 512 columns: 128 x 4096 x 4096 24.8 / 16.6 / 14.3 us, 256 x 8192 x 8192 50.6 / 40.0 / 47.6,
