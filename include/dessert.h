@@ -424,7 +424,7 @@ dessert_status_t dessert_token_logprobs(const dessert_index_t *index, const void
                                         float *out_entropy_dev, uint32_t *out_top_ids_dev, float *out_top_logprobs_dev);
 
 /* The same from a model's last states and its vocabulary matrix in int8; the workspace holds the logits of some rows at a
- * time, or none where there are many rows:
+ * time, or only those of the parts of the vocabulary that hold a row's best entries:
  *   l[i][j] = float(sum_c a[i][c] * vocab[j][c]) * (a_scales[i] * vocab_scales[j])
  * in 32-bit float, operands as in dessert_scaled_matmul, outputs and tokens as in dessert_token_logprobs. */
 size_t dessert_head_logprobs_workspace_bytes(const dessert_index_t *index, uint64_t n_rows, uint32_t n_vocab, uint32_t n_cols,
