@@ -435,6 +435,124 @@ dessert_status_t dessert_head_logprobs(const dessert_index_t *index, const int8_
                                        uint32_t n_top, void *workspace_dev, size_t workspace_bytes, float *out_logprobs_dev,
                                        float *out_entropy_dev, uint32_t *out_top_ids_dev, float *out_top_logprobs_dev);
 
+/* ---- What a model keeps of its tokens ---------------------------------------------------------------------------
+ * A paged cache of keys and values in int8, for the model that reads what the search found: documents are taken in
+ * once and shared by the sequences that go on from them.  A page holds page_tokens consecutive tokens of a sequence, each
+ * head of it with a scale for its keys and one for its values, x ~ scale * code.  A sequence is a row of a table of page
+ * numbers (any of the pool, in any order) and a length; place j of its row holds its tokens j * page_tokens onwards.  One
+ * cache is one layer's; layers that share tables are as many caches of the same sizes.  The calls follow the rules of the
+ * operators above (streams, workspaces, alignment, the same bits from call to call), and none needs to know a length on
+ * the host.  0xFFFFFFFF, and any other number outside the pool, is no page: tokens there are not written and not seen.
+ *   page_tokens   16, 32, 64, 128 or 256
+ *   dim           of a head: a multiple of 32, at most 256
+ *   k_codes_dev   dev, 16-byte aligned, [n_pages][n_heads][page_tokens][dim]
+ *   v_codes_dev   dev, 16-byte aligned, [n_pages][n_heads][dim][page_tokens]: a channel's tokens side by side
+ *   k_scales_dev, v_scales_dev   dev, [n_pages][n_heads], not negative
+ *   bounds_dev    dev, 16-byte aligned, [n_pages][n_heads][2][dim]: the smallest and the largest key code of a channel, or
+ *                 NULL without dessert_cache_select */
+typedef struct {
+    int8_t *k_codes_dev, *v_codes_dev;
+    float *k_scales_dev, *v_scales_dev;
+    int8_t *bounds_dev;
+    uint32_t n_pages, n_heads, page_tokens, dim;
+} dessert_cache_t;
+
+/* Sequences of a call, each with some new tokens at its end: the last ones of its length.
+ *   tables_dev    dev, [n_seqs][table_pages]; table_pages * page_tokens <= 2^31 - 256
+ *   lengths_dev   dev, [n_seqs], the new tokens counted; a length of 0 is a sequence that sees nothing
+ *   starts_dev    dev, [n_seqs + 1]: the new tokens of sequence b are rows starts[b] .. starts[b + 1] of the arrays of tokens,
+ *                 in order (there may be none); or NULL: one new token each, row b
+ *   n_tokens      rows of the arrays of tokens; those from starts[n_seqs] on are neither read nor written
+ *   max_tokens    at least the largest number of new tokens of a sequence: further ones are left out
+ *   max_length    about the largest length: how work is divided goes by it, results do not depend on it but for rounding */
+typedef struct {
+    const uint32_t *tables_dev, *lengths_dev, *starts_dev;
+    uint32_t n_seqs, table_pages, n_tokens, max_tokens, max_length;
+} dessert_cache_batch_t;
+
+/* Writes new tokens' keys and values into their pages.  Where a sequence's first new token begins a page, the page is taken as
+ * empty; a page's scale is the largest magnitude among its tokens times (1 / 127), both factors and the product rounded to
+ * 32-bit floats, and never falls: where new tokens raise it, the codes of earlier ones (and their bounds) go from the old
+ * scale to the new one, code * old / new.  Codes are the nearest integers to the real quotients, ties to even; a scale of zero
+ * has codes 0.  A page that is given an infinity or NaN keeps scale NaN until it begins anew, and codes 0 of the tokens given
+ * from then on.  Slots behind a sequence's last token stay as they were.  A page may be written for one sequence of a call only.
+ *   k_dev, v_dev   dev, [n_tokens][n_heads][dim] of dtype (DESSERT_F16, DESSERT_BF16, DESSERT_F32), the heads of a token side by side,
+ *                  tokens k_stride / v_stride elements apart */
+dessert_status_t dessert_cache_append(const dessert_index_t *index, const dessert_cache_t *cache, const dessert_cache_batch_t *batch,
+                                      const void *k_dev, uint64_t k_stride, const void *v_dev, uint64_t v_stride, uint32_t dtype);
+
+/* Attention of the new tokens over their sequences in the cache (the new tokens among them, which have been appended).  Query head
+ * i goes with key head i / (n_q_heads / n_heads).  A token at position p sees the tokens j <= p of its sequence that are on a
+ * page, of those j > p - window (window = 0: all), and with pages_dev of those the ones in the listed places:
+ *   s[j] = scale * k_scale(j) * sum_d q[d] k_code[j][d]
+ *   out[d] = sum_j e^s[j] v_scale(j) v_code[j][d] / sum_j e^s[j],   out_lse = log sum_j e^s[j]
+ * A token that sees nothing has out 0 and out_lse -inf, a query that holds an infinity or NaN otherwise NaN.  Two halves of a
+ * context, each attended to by a call, are joined by their out_lse.
+ *   q_dev          dev, [n_tokens][n_q_heads][dim] of dtype (DESSERT_F16, DESSERT_BF16), the heads of a token side by side, tokens q_stride
+ *                  elements apart
+ *   pages_dev      dev, [n_tokens][n_heads][n_select] places in the sequence's table, in any order, each once; others than those
+ *                  of the table are left out; or NULL with n_select = 0
+ *   workspace_dev  dev, dessert_cache_attention_workspace_bytes(...) bytes (may be NULL where that is 0)
+ *   out_dev        dev, out, [n_tokens][n_q_heads][dim] of dtype, no padding
+ *   out_lse_dev    dev, out, [n_tokens][n_q_heads], or NULL */
+size_t dessert_cache_attention_workspace_bytes(const dessert_index_t *index, const dessert_cache_t *cache,
+                                               const dessert_cache_batch_t *batch, uint32_t n_q_heads, uint32_t n_select);
+dessert_status_t dessert_cache_attention(const dessert_index_t *index, const dessert_cache_t *cache, const dessert_cache_batch_t *batch,
+                                         const void *q_dev, uint32_t dtype, uint64_t q_stride, uint32_t n_q_heads, float scale,
+                                         uint32_t window, const uint32_t *pages_dev, uint32_t n_select, void *workspace_dev,
+                                         size_t workspace_bytes, void *out_dev, float *out_lse_dev);
+
+/* The pages that new tokens look at, chosen by what their keys can come to at most.  For a query head with codes c and scale s (of
+ * dessert_quantize_rows) and a page with bounds lo, hi:
+ *   score = float(sum_d (c[d] < 0 ? c[d] lo[d] : c[d] hi[d])) * (s * k_scale)
+ * the sum exact, the rest 32-bit float; of a page for a key head the largest over its query heads.  The n_select highest of the
+ * places up to the token's own, ties to the lower place; the n_first first and n_last last places always among them.  A score
+ * of NaN counts as +inf.
+ *   q_codes_dev    dev, [n_tokens * n_q_heads][dim], no padding; q_scales_dev dev, [n_tokens * n_q_heads]
+ *   n_select       at least 1, n_first + n_last <= n_select
+ *   workspace_dev  dev, dessert_cache_select_workspace_bytes(...) bytes
+ *   out_pages_dev  dev, out, [n_tokens][n_heads][n_select] places, ascending, behind the last one 0xFFFFFFFF */
+size_t dessert_cache_select_workspace_bytes(const dessert_index_t *index, const dessert_cache_t *cache, const dessert_cache_batch_t *batch);
+dessert_status_t dessert_cache_select(const dessert_index_t *index, const dessert_cache_t *cache, const dessert_cache_batch_t *batch,
+                                      const int8_t *q_codes_dev, const float *q_scales_dev, uint32_t n_q_heads, uint32_t n_select,
+                                      uint32_t n_first, uint32_t n_last, void *workspace_dev, size_t workspace_bytes,
+                                      uint32_t *out_pages_dev);
+
+/* Sequences go on: new sequence b from old sequence parents[b] (several from one: a fork, a beam; none: it has ended) with room for
+ * add[b] tokens more.  Its table begins with its parent's pages.  refs[p] counts the tables that hold page p (0: free); old
+ * sequences give their pages up, new ones count.  A last page that is partly filled, is to be written (add > 0) and has other
+ * holders is copied first, in all layers; where all holders are sequences that write to it, the first of them keeps it.  Pages
+ * are taken from the free ones, lowest first, in the order of the sequences.  A sequence that the free pages (counted before
+ * anything is taken) do not reach any more, or that does not fit the table, gets none: it stays as it was, its length without
+ * add[b]; so does one whose last page is still shared by such a sequence.
+ *   layers          host, [n_layers]: caches of the same sizes; pages are copied in all of them
+ *   refs_dev        dev, in and out, [n_pages]
+ *   tables_dev, lengths_dev   dev, [n_seqs][table_pages], [n_seqs] of the old sequences
+ *   parents_dev     dev, [n_new]; a number that is not below n_seqs is no parent (length 0); or NULL: each goes on, n_new = n_seqs
+ *                   (n_new = 0: all have ended)
+ *   add_dev         dev, [n_new]
+ *   workspace_dev   dev, dessert_cache_advance_workspace_bytes(...) bytes
+ *   out_tables_dev  dev, out, [n_new][table_pages], behind a sequence's pages 0xFFFFFFFF; apart from tables_dev
+ *   out_lengths_dev dev, out, [n_new]
+ *   out_status_dev  dev, out, [2]: free pages left, sequences that got no room */
+size_t dessert_cache_advance_workspace_bytes(const dessert_index_t *index, uint32_t n_pages, uint32_t n_new);
+dessert_status_t dessert_cache_advance(const dessert_index_t *index, const dessert_cache_t *layers, uint32_t n_layers, uint32_t *refs_dev,
+                                       const uint32_t *tables_dev, uint32_t table_pages, const uint32_t *lengths_dev, uint32_t n_seqs,
+                                       const uint32_t *parents_dev, const uint32_t *add_dev, uint32_t n_new, void *workspace_dev,
+                                       size_t workspace_bytes, uint32_t *out_tables_dev, uint32_t *out_lengths_dev,
+                                       uint32_t *out_status_dev);
+
+/* Brings the n pages in use (refs > 0) to the numbers 0 .. n: those at n and above move into the free ones below, lowest to
+ * lowest, in all layers, with their counts; the tables' entries follow.
+ *   refs_dev, tables_dev   dev, in and out, as above
+ *   workspace_dev          dev, dessert_cache_compact_workspace_bytes(...) bytes
+ *   out_numbers_dev        dev, out, [n_pages]: a page's new number, for tables elsewhere; 0xFFFFFFFF for a free one
+ *   out_live_dev           dev, out, [1]: n */
+size_t dessert_cache_compact_workspace_bytes(const dessert_index_t *index, uint32_t n_pages);
+dessert_status_t dessert_cache_compact(const dessert_index_t *index, const dessert_cache_t *layers, uint32_t n_layers, uint32_t *refs_dev,
+                                       uint32_t *tables_dev, uint32_t table_pages, const uint32_t *lengths_dev, uint32_t n_seqs,
+                                       void *workspace_dev, size_t workspace_bytes, uint32_t *out_numbers_dev, uint32_t *out_live_dev);
+
 const char *dessert_last_error(void);
 const char *dessert_version(void);
 

@@ -8,7 +8,9 @@ built (run ``python -m paper_2210_15748_amd.build`` or ``__graft_entry__.build()
 Function names mirror the C entry points without the ``dessert_`` prefix:
 ``create`` / ``destroy`` / ``hash`` / ``build_index`` / ``search`` / ``scores`` /
 ``set_algo`` / ``set_score_transform`` / ``get_projection`` / ``enable_timing`` / ``get_timing``, and beside the
-search ``quantize_rows`` / ``scaled_matmul`` / ``token_logprobs`` / ``head_logprobs``.
+search ``quantize_rows`` / ``scaled_matmul`` / ``token_logprobs`` / ``head_logprobs``, and on the paged cache of a reading model
+``cache`` / ``cache_batch`` (what the calls take) with ``cache_append`` / ``cache_attention`` / ``cache_select`` / ``cache_advance`` /
+``cache_compact``.
 """
 from __future__ import annotations
 
@@ -46,6 +48,9 @@ EXPORTS = [
     "dessert_quantize_rows", "dessert_scaled_matmul_workspace_bytes", "dessert_scaled_matmul",
     "dessert_token_logprobs_workspace_bytes", "dessert_token_logprobs",
     "dessert_head_logprobs_workspace_bytes", "dessert_head_logprobs",
+    "dessert_cache_append", "dessert_cache_attention_workspace_bytes", "dessert_cache_attention",
+    "dessert_cache_select_workspace_bytes", "dessert_cache_select", "dessert_cache_advance_workspace_bytes", "dessert_cache_advance",
+    "dessert_cache_compact_workspace_bytes", "dessert_cache_compact",
     "dessert_enable_timing", "dessert_get_timing", "dessert_probe_read_bandwidth", "dessert_probe_mix_bandwidth", "dessert_last_error",
     "dessert_version",
 ]
@@ -55,6 +60,16 @@ class Config(C.Structure):
     _fields_ = [("d", C.c_uint32), ("L", C.c_uint32), ("C", C.c_uint32), ("dtype", C.c_uint32),
                 ("proj_kind", C.c_uint32), ("device", C.c_int32), ("seed", C.c_uint64),
                 ("proj_dev", C.c_void_p), ("stream", C.c_void_p)]
+
+
+class _CacheStruct(C.Structure):
+    _fields_ = [("k_codes_dev", C.c_void_p), ("v_codes_dev", C.c_void_p), ("k_scales_dev", C.c_void_p), ("v_scales_dev", C.c_void_p),
+                ("bounds_dev", C.c_void_p), ("n_pages", C.c_uint32), ("n_heads", C.c_uint32), ("page_tokens", C.c_uint32), ("dim", C.c_uint32)]
+
+
+class _BatchStruct(C.Structure):
+    _fields_ = [("tables_dev", C.c_void_p), ("lengths_dev", C.c_void_p), ("starts_dev", C.c_void_p), ("n_seqs", C.c_uint32),
+                ("table_pages", C.c_uint32), ("n_tokens", C.c_uint32), ("max_tokens", C.c_uint32), ("max_length", C.c_uint32)]
 
 
 class DessertError(RuntimeError):
@@ -118,6 +133,19 @@ def lib() -> C.CDLL:
     l.dessert_head_logprobs_workspace_bytes.argtypes = [vp, u64, u32, u32, u32]
     l.dessert_head_logprobs_workspace_bytes.restype = sz
     l.dessert_head_logprobs.argtypes = [vp, vp, u64, vp, u64, vp, u64, vp, u32, u32, vp, u32, vp, sz, vp, vp, vp, vp]
+    l.dessert_cache_append.argtypes = [vp, vp, vp, vp, u64, vp, u64, u32]
+    l.dessert_cache_attention_workspace_bytes.argtypes = [vp, vp, vp, u32, u32]
+    l.dessert_cache_attention_workspace_bytes.restype = sz
+    l.dessert_cache_attention.argtypes = [vp, vp, vp, vp, u32, u64, u32, C.c_float, u32, vp, u32, vp, sz, vp, vp]
+    l.dessert_cache_select_workspace_bytes.argtypes = [vp, vp, vp]
+    l.dessert_cache_select_workspace_bytes.restype = sz
+    l.dessert_cache_select.argtypes = [vp, vp, vp, vp, vp, u32, u32, u32, u32, vp, sz, vp]
+    l.dessert_cache_advance_workspace_bytes.argtypes = [vp, u32, u32]
+    l.dessert_cache_advance_workspace_bytes.restype = sz
+    l.dessert_cache_advance.argtypes = [vp, vp, u32, vp, vp, u32, vp, u32, vp, vp, u32, vp, sz, vp, vp, vp]
+    l.dessert_cache_compact_workspace_bytes.argtypes = [vp, u32]
+    l.dessert_cache_compact_workspace_bytes.restype = sz
+    l.dessert_cache_compact.argtypes = [vp, vp, u32, vp, vp, u32, vp, u32, vp, sz, vp, vp]
     l.dessert_enable_timing.argtypes = [vp, C.c_int]
     l.dessert_get_timing.argtypes = [vp, u32, C.POINTER(C.c_float)]
     l.dessert_probe_read_bandwidth.argtypes = [vp, sz, C.c_int, vp, C.c_int, C.POINTER(C.c_float)]
@@ -448,6 +476,7 @@ def filter_search(ix: Index, q_vectors: torch.Tensor, q_lengths, filter_probe: i
 
 # ---- beside the search ----------------------------------------------------------------------------------------------------
 _FLOAT_TYPES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+_HALF_TYPES = (torch.float16, torch.bfloat16)
 _INT8, _FLOAT32, _TOKEN_TYPES = (torch.int8,), (torch.float32,), (torch.int32, torch.uint32)
 _MOST = 0x7FFFFFFF
 
@@ -620,6 +649,218 @@ def head_logprobs(ix: Index, a: torch.Tensor, a_scales: torch.Tensor, vocab: tor
     _lend(ix, made)
     _check(lib().dessert_head_logprobs(ix.handle, a_ptr, a_apart, sa_ptr, n, v_ptr, v_apart, sv_ptr, V, k, tokens, n_top, ws_ptr, ws_bytes,
                                        *map(_ptr, o)))
+    return o
+
+
+# ---- what a model keeps of its tokens ---------------------------------------------------------------------------------------
+class Cache:
+    """One layer's paged int8 cache, as the calls take it: the tensors (kept alive here) and dessert_cache_t."""
+
+    def __init__(self, tensors, struct: _CacheStruct):
+        self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.bounds = tensors
+        self.struct = struct
+        self.n_pages, self.n_heads, self.page_tokens, self.dim = struct.n_pages, struct.n_heads, struct.page_tokens, struct.dim
+        self.address = C.addressof(struct)
+
+
+class CacheBatch:
+    """The sequences of a call: the tensors (kept alive here; their contents may change from call to call) and dessert_cache_batch_t."""
+
+    def __init__(self, tensors, struct: _BatchStruct):
+        self.tables, self.lengths, self.starts = tensors
+        self.struct = struct
+        self.n_seqs, self.n_tokens = struct.n_seqs, struct.n_tokens
+        self.address = C.addressof(struct)
+
+
+def _kept(ix: Index, t: torch.Tensor, shape, name: str, dtypes) -> int:
+    """A tensor that a call reads or writes where it lies: None in a shape is any size."""
+    if (len(t.shape) != len(shape) or any(w is not None and w != n for n, w in zip(t.shape, shape)) or t.dtype not in dtypes
+            or t.device != ix.device or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {list(shape)} on {ix.device} of dtype " + " / ".join(str(d) for d in dtypes))
+    return t.data_ptr()
+
+
+def _size(n: int, name: str, most: int = _MOST) -> int:
+    if not 0 <= n <= most:
+        raise ValueError(f"{name} is {n}, 0 to {most} is taken")
+    return n
+
+
+def cache(ix: Index, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+          bounds: Optional[torch.Tensor] = None) -> Cache:
+    """dessert_cache_t: k_codes [pages, heads, page tokens, dim] int8, v_codes [pages, heads, dim, page tokens] int8, scales
+    [pages, heads] float32, bounds [pages, heads, 2, dim] int8 or None.  Nothing is copied: calls read and write these tensors."""
+    k_ptr = _kept(ix, k_codes, (None,) * 4, "k_codes", _INT8)
+    P, H, T, D = k_codes.shape
+    for n in (P, H, T, D):
+        _size(n, "a size of k_codes")
+    struct = _CacheStruct(k_ptr, _kept(ix, v_codes, (P, H, D, T), "v_codes", _INT8), _kept(ix, k_scales, (P, H), "k_scales", _FLOAT32),
+                          _kept(ix, v_scales, (P, H), "v_scales", _FLOAT32),
+                          None if bounds is None else _kept(ix, bounds, (P, H, 2, D), "bounds", _INT8), P, H, T, D)
+    return Cache((k_codes, v_codes, k_scales, v_scales, bounds), struct)
+
+
+def cache_batch(ix: Index, tables: torch.Tensor, lengths: torch.Tensor, starts: Optional[torch.Tensor] = None,
+                n_tokens: Optional[int] = None, max_tokens: Optional[int] = None, max_length: Optional[int] = None) -> CacheBatch:
+    """dessert_cache_batch_t: tables [seqs, table pages] and lengths [seqs] int32 / uint32 (-1: no page), starts [seqs + 1] or None (one new token
+    each).  With starts, n_tokens (rows of the arrays of tokens) is needed; max_tokens (new tokens of a sequence, at most)
+    is taken to be that where it is not given, max_length (which decides how work is divided) what the tables hold."""
+    t_ptr = _kept(ix, tables, (None, None), "tables", _TOKEN_TYPES)
+    n, width = tables.shape
+    l_ptr = _kept(ix, lengths, (n,), "lengths", _TOKEN_TYPES)
+    s_ptr = None if starts is None else _kept(ix, starts, (n + 1,), "starts", _TOKEN_TYPES)
+    if n_tokens is None:
+        if starts is not None:
+            raise ValueError("n_tokens is needed with starts")
+        n_tokens = n
+    if max_tokens is None:
+        max_tokens = n_tokens if starts is not None else 1
+    struct = _BatchStruct(t_ptr, l_ptr, s_ptr, _size(n, "the number of sequences"), _size(width, "the tables' width"), _size(n_tokens, "n_tokens"),
+                          _size(max_tokens, "max_tokens"), _MOST if max_length is None else _size(max_length, "max_length"))
+    return CacheBatch((tables, lengths, starts), struct)
+
+
+def _states(ix: Index, t: torch.Tensor, n: int, heads: Optional[int], dim: int, name: str, made, dtypes):
+    """[n, heads, dim], a token's heads side by side: address, heads, elements from token to token"""
+    shape = t.shape
+    if (len(shape) != 3 or shape[0] != n or shape[2] != dim or (heads is not None and shape[1] != heads) or shape[1] > _MOST
+            or t.dtype not in dtypes or t.device != ix.device):
+        raise ValueError(f"{name} must be [{n}, {'heads' if heads is None else heads}, {dim}] on {ix.device} of dtype " + " / ".join(str(d) for d in dtypes))
+    heads, wide = shape[1], shape[1] * dim
+    apart, between, step = t.stride()
+    if step != 1 or (heads > 1 and between != dim) or (n > 1 and apart < wide):
+        t = t.contiguous()
+        made.append(t)
+        apart = wide
+    return t.data_ptr(), heads, apart if n > 1 else wide
+
+
+def cache_append(ix: Index, cache: Cache, batch: CacheBatch, k: torch.Tensor, v: torch.Tensor) -> None:
+    """dessert_cache_append: k and v [tokens, heads, dim] of float16 / bfloat16 / float32 (tokens may lie apart)."""
+    made = []
+    if k.dtype != v.dtype:
+        raise ValueError("k and v must be of one dtype")
+    k_ptr, _, k_apart = _states(ix, k, batch.n_tokens, cache.n_heads, cache.dim, "k", made, _FLOAT_TYPES)
+    v_ptr, _, v_apart = _states(ix, v, batch.n_tokens, cache.n_heads, cache.dim, "v", made, _FLOAT_TYPES)
+    _lend(ix, made)
+    _check(lib().dessert_cache_append(ix.handle, cache.address, batch.address, k_ptr, k_apart, v_ptr, v_apart, _FLOAT_TYPES[k.dtype]))
+
+
+def cache_attention_workspace_bytes(ix: Index, cache: Cache, batch: CacheBatch, n_q_heads: int, n_select: int = 0) -> int:
+    return int(lib().dessert_cache_attention_workspace_bytes(ix.handle, cache.address, batch.address, n_q_heads, n_select))
+
+
+def cache_attention(ix: Index, cache: Cache, batch: CacheBatch, q: torch.Tensor, scale: Optional[float] = None, window: int = 0,
+                    pages: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, out_lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None):
+    """dessert_cache_attention: q [tokens, query heads, dim] of float16 / bfloat16 (tokens may lie apart), scale 1 / sqrt(dim) unless given, pages
+    [tokens, heads, n] int32 / uint32 as cache_select gives them, or None.  Returns (out like q without gaps, lse [tokens,
+    query heads] float32)."""
+    made = []
+    n = batch.n_tokens
+    q_ptr, heads, apart = _states(ix, q, n, None, cache.dim, "q", made, _HALF_TYPES)
+    if pages is None:
+        p_ptr, n_select = None, 0
+    else:
+        p_ptr, n_select = _kept(ix, pages, (n, cache.n_heads, None), "pages", _TOKEN_TYPES), _size(pages.shape[2], "the number of pages")
+        if n_select == 0:
+            raise ValueError("pages has no places")
+    out = _output(ix, out, (n, heads, cache.dim), "out", made, q.dtype)
+    out_lse = _output(ix, out_lse, (n, heads), "out_lse", made, torch.float32)
+    ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_attention_workspace_bytes, cache, batch, heads, n_select)
+    _lend(ix, made)
+    _check(lib().dessert_cache_attention(ix.handle, cache.address, batch.address, q_ptr, _FLOAT_TYPES[q.dtype], apart, heads,
+                                         cache.dim ** -0.5 if scale is None else scale, _size(window, "window"), p_ptr, n_select, ws_ptr, ws_bytes,
+                                         out.data_ptr(), out_lse.data_ptr()))
+    return out, out_lse
+
+
+def cache_select_workspace_bytes(ix: Index, cache: Cache, batch: CacheBatch) -> int:
+    return int(lib().dessert_cache_select_workspace_bytes(ix.handle, cache.address, batch.address))
+
+
+def cache_select(ix: Index, cache: Cache, batch: CacheBatch, q_codes: torch.Tensor, q_scales: torch.Tensor, n_select: int,
+                 n_first: int = 0, n_last: int = 0, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dessert_cache_select: q_codes [tokens * query heads, dim] int8 and q_scales [tokens * query heads] as quantize_rows gives them.
+    Returns places [tokens, heads, n_select] uint32, ascending, 0xFFFFFFFF behind the last."""
+    made = []
+    n = batch.n_tokens
+    q_ptr = _kept(ix, q_codes, (None, cache.dim), "q_codes", _INT8)
+    rows = q_codes.shape[0]
+    if n == 0 or rows % n:
+        raise ValueError(f"q_codes has {rows} rows for {n} tokens")
+    s_ptr = _vector(ix, q_scales, rows, "q_scales", made, _FLOAT32)
+    out = _output(ix, out, (n, cache.n_heads, _size(n_select, "n_select")), "out", made, torch.uint32)
+    ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_select_workspace_bytes, cache, batch)
+    _lend(ix, made)
+    _check(lib().dessert_cache_select(ix.handle, cache.address, batch.address, q_ptr, s_ptr, rows // n, n_select, _size(n_first, "n_first"),
+                                      _size(n_last, "n_last"), ws_ptr, ws_bytes, out.data_ptr()))
+    return out
+
+
+def _layers(caches):
+    """(array of dessert_cache_t, its length)"""
+    caches = [caches] if isinstance(caches, Cache) else list(caches)
+    if not caches:
+        raise ValueError("no layers")
+    return (_CacheStruct * len(caches))(*(c.struct for c in caches)), len(caches)
+
+
+def _page_outputs(ix: Index, outs, shapes, made, dtypes=_TOKEN_TYPES):
+    o = (None,) * len(shapes) if outs is None else outs
+    return tuple(_output(ix, t, shape, f"outs[{i}]", made, t.dtype if t is not None and t.dtype in dtypes else torch.int32)
+                 for i, (t, shape) in enumerate(zip(o, shapes)))
+
+
+def cache_advance_workspace_bytes(ix: Index, n_pages: int, n_new: int) -> int:
+    return int(lib().dessert_cache_advance_workspace_bytes(ix.handle, n_pages, n_new))
+
+
+def cache_advance(ix: Index, caches, refs: torch.Tensor, tables: torch.Tensor, lengths: torch.Tensor, add: torch.Tensor,
+                  parents: Optional[torch.Tensor] = None, outs=None, workspace: Optional[torch.Tensor] = None):
+    """dessert_cache_advance: caches a Cache or one for each layer, refs [pages] (changed), tables [seqs, table pages], lengths [seqs], add and parents [new
+    seqs] (-1: none) or None, all int32 / uint32.  Returns (tables [new seqs, table pages], lengths [new seqs], status [2]: free
+    pages, sequences without room); ``outs``: the three tensors to write, apart from the old ones."""
+    made = []
+    layers, n_layers = _layers(caches)
+    pages = layers[0].n_pages
+    r_ptr = _kept(ix, refs, (pages,), "refs", _TOKEN_TYPES)
+    t_ptr = _kept(ix, tables, (None, None), "tables", _TOKEN_TYPES)
+    n, width = tables.shape
+    l_ptr = _kept(ix, lengths, (n,), "lengths", _TOKEN_TYPES)
+    a_ptr = _kept(ix, add, (None,), "add", _TOKEN_TYPES)
+    new = add.shape[0]
+    p_ptr = None if parents is None else _kept(ix, parents, (new,), "parents", _TOKEN_TYPES)
+    o = _page_outputs(ix, outs, ((new, width), (new,), (2,)), made)
+    ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_advance_workspace_bytes, pages, new)
+    _lend(ix, made)
+    _check(lib().dessert_cache_advance(ix.handle, C.addressof(layers), n_layers, r_ptr, t_ptr, _size(width, "the tables' width"), l_ptr,
+                                       _size(n, "the number of sequences"), p_ptr, a_ptr, _size(new, "the number of sequences"), ws_ptr, ws_bytes,
+                                       *map(_ptr, o)))
+    return o
+
+
+def cache_compact_workspace_bytes(ix: Index, n_pages: int) -> int:
+    return int(lib().dessert_cache_compact_workspace_bytes(ix.handle, n_pages))
+
+
+def cache_compact(ix: Index, caches, refs: torch.Tensor, tables: torch.Tensor, lengths: torch.Tensor, outs=None,
+                  workspace: Optional[torch.Tensor] = None):
+    """dessert_cache_compact: caches as for cache_advance, refs [pages] and tables [seqs, table pages] (both changed), lengths [seqs], all int32 / uint32.
+    Returns (new numbers [pages], pages in use [1])."""
+    made = []
+    layers, n_layers = _layers(caches)
+    pages = layers[0].n_pages
+    r_ptr = _kept(ix, refs, (pages,), "refs", _TOKEN_TYPES)
+    t_ptr = _kept(ix, tables, (None, None), "tables", _TOKEN_TYPES)
+    n, width = tables.shape
+    l_ptr = _kept(ix, lengths, (n,), "lengths", _TOKEN_TYPES)
+    o = _page_outputs(ix, outs, ((pages,), (1,)), made)
+    ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_compact_workspace_bytes, pages)
+    _lend(ix, made)
+    _check(lib().dessert_cache_compact(ix.handle, C.addressof(layers), n_layers, r_ptr, t_ptr, _size(width, "the tables' width"), l_ptr,
+                                       _size(n, "the number of sequences"), ws_ptr, ws_bytes, *map(_ptr, o)))
     return o
 
 

@@ -10,7 +10,8 @@ CSRC = HERE / "csrc"
 OBJ = HERE / "_build"
 LIB = HERE / "libdessert_hip.so"
 SOURCES = ["api.hip", "hash_kernels.hip", "score_kernels.hip", "topk_kernels.hip", "filter_kernels.hip", "filter_groups.hip",
-           "quantize_kernels.hip", "matmul_kernels.hip", "logprob_kernels.hip"]
+           "quantize_kernels.hip", "matmul_kernels.hip", "logprob_kernels.hip", "attention_kernels.hip", "cache_kernels.hip",
+           "cache_pages_kernels.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # MFMA accumulators in ordinary VGPRs: the sign packing reads them with VALU ops, which

@@ -1486,4 +1486,256 @@ dessert_status_t dessert_head_logprobs(const dessert_index_t* ix, const int8_t* 
     return DESSERT_OK;
 }
 
+// ---- what a model keeps of its tokens --------------------------------------------------------------------------------------
+
+namespace {
+constexpr uint64_t MAX_WORKGROUPS = 0xFFFFFFFFull / 256;   // of 256 threads in a launch
+
+dessert_status_t check_cache(const dessert_cache_t* c, CachePages* out) {
+    if (!c) return fail(DESSERT_EINVAL, "cache is NULL");
+    if (c->page_tokens < CACHE_MIN_PAGE || c->page_tokens > CACHE_MAX_PAGE || (c->page_tokens & (c->page_tokens - 1)))
+        return fail(DESSERT_EINVAL, "page_tokens must be 16, 32, 64, 128 or 256");
+    if (c->dim == 0 || c->dim % 32 || c->dim > CACHE_MAX_DIM) return fail(DESSERT_EINVAL, "dim must be a multiple of 32, at most %u", CACHE_MAX_DIM);
+    if (c->n_heads == 0 || c->n_heads > 65535) return fail(DESSERT_EINVAL, "n_heads must be in 1..65535");
+    if (c->n_pages == 0 || c->n_pages > CACHE_MOST) return fail(DESSERT_EINVAL, "n_pages must be in 1..%u", CACHE_MOST);
+    if (!c->k_codes_dev || !c->v_codes_dev || !c->k_scales_dev || !c->v_scales_dev) return fail(DESSERT_EINVAL, "a cache's array is NULL");
+    if ((uintptr_t)c->k_codes_dev % 16 || (uintptr_t)c->v_codes_dev % 16 || (uintptr_t)c->bounds_dev % 16)
+        return fail(DESSERT_EINVAL, "a cache's codes and bounds must be 16-byte aligned");
+    if ((uintptr_t)c->k_scales_dev % 4 || (uintptr_t)c->v_scales_dev % 4) return fail(DESSERT_EINVAL, "a cache's scales must be 4-byte aligned");
+    out->k = c->k_codes_dev; out->v = c->v_codes_dev; out->ks = c->k_scales_dev; out->vs = c->v_scales_dev; out->bounds = c->bounds_dev;
+    out->n_pages = c->n_pages; out->heads = c->n_heads; out->page_tokens = c->page_tokens; out->dim = c->dim;
+    out->shift = (uint32_t)__builtin_ctz(c->page_tokens);
+    return DESSERT_OK;
+}
+
+dessert_status_t check_table(const uint32_t* tables, uint32_t table_pages, const uint32_t* lengths, uint32_t n_seqs, uint32_t page_tokens) {
+    if (n_seqs > CACHE_MOST) return fail(DESSERT_EINVAL, "at most %u sequences", CACHE_MOST);
+    if (table_pages == 0 || (uint64_t)table_pages * page_tokens > CACHE_MOST) return fail(DESSERT_EINVAL, "table_pages must be in 1..%u", CACHE_MOST / page_tokens);
+    if (n_seqs && (!tables || !lengths)) return fail(DESSERT_EINVAL, "tables_dev or lengths_dev is NULL");
+    if ((uintptr_t)tables % 4 || (uintptr_t)lengths % 4) return fail(DESSERT_EINVAL, "tables and lengths must be 4-byte aligned");
+    return DESSERT_OK;
+}
+
+dessert_status_t check_cache_batch(const dessert_cache_batch_t* b, const CachePages& c, CacheBatch* out) {
+    if (!b) return fail(DESSERT_EINVAL, "batch is NULL");
+    dessert_status_t st = check_table(b->tables_dev, b->table_pages, b->lengths_dev, b->n_seqs, c.page_tokens);
+    if (st != DESSERT_OK) return st;
+    if (b->n_tokens > CACHE_MOST) return fail(DESSERT_EINVAL, "at most %u tokens", CACHE_MOST);
+    if ((uintptr_t)b->starts_dev % 4) return fail(DESSERT_EINVAL, "starts_dev must be 4-byte aligned");
+    if (!b->starts_dev && (b->n_tokens != b->n_seqs || b->max_tokens != 1))
+        return fail(DESSERT_EINVAL, "without starts_dev each sequence has one new token: n_tokens = n_seqs, max_tokens = 1");
+    if (b->n_tokens && (b->max_tokens == 0 || b->max_tokens > b->n_tokens)) return fail(DESSERT_EINVAL, "max_tokens must be in 1..n_tokens");
+    out->tables = b->tables_dev; out->lengths = b->lengths_dev; out->starts = b->starts_dev;
+    out->n_seqs = b->n_seqs; out->table_pages = b->table_pages; out->n_tokens = b->n_tokens; out->max_tokens = b->max_tokens;
+    return DESSERT_OK;
+}
+
+dessert_status_t check_tokens(const void* x, uint64_t stride, uint32_t dtype, uint64_t heads, uint32_t dim, uint32_t n_tokens, const char* name) {
+    if (n_tokens && !x) return fail(DESSERT_EINVAL, "%s is NULL", name);
+    if ((uintptr_t)x % type_size(dtype)) return fail(DESSERT_EINVAL, "%s must be aligned to its elements", name);
+    if (stride < heads * dim || stride >= MAX_STRIDE) return fail(DESSERT_EINVAL, "tokens of %s need a stride of %llu to 2^31-1", name, (unsigned long long)(heads * dim));
+    return DESSERT_OK;
+}
+
+dessert_status_t check_group(uint32_t n_q_heads, const CachePages& c, uint32_t* group) {
+    if (n_q_heads == 0 || n_q_heads % c.heads || n_q_heads > (1u << 20)) return fail(DESSERT_EINVAL, "n_q_heads must be a multiple of n_heads, at most 2^20");
+    *group = n_q_heads / c.heads;
+    return DESSERT_OK;
+}
+
+// The keys that a row looks at, at most.
+uint64_t attended(const dessert_cache_batch_t& b, uint32_t page_tokens, uint32_t n_select) {
+    return n_select ? (uint64_t)n_select * page_tokens : std::min<uint64_t>(b.max_length, (uint64_t)b.table_pages * page_tokens);
+}
+
+// The caches of the layers that go on together.
+dessert_status_t check_layers(const dessert_cache_t* layers, uint32_t n_layers, std::vector<CachePages>* out) {
+    if (!layers || n_layers == 0 || n_layers > 65535) return fail(DESSERT_EINVAL, "1 to 65535 layers");
+    try {
+        out->resize(n_layers);
+    } catch (...) {
+        return fail(DESSERT_ENOMEM, "out of host memory");
+    }
+    for (uint32_t i = 0; i < n_layers; ++i) {
+        dessert_status_t st = check_cache(layers + i, &(*out)[i]);
+        if (st != DESSERT_OK) return st;
+        const CachePages &x = (*out)[i], &y = (*out)[0];
+        if (x.n_pages != y.n_pages || x.heads != y.heads || x.page_tokens != y.page_tokens || x.dim != y.dim)
+            return fail(DESSERT_EINVAL, "the layers' caches must have the same sizes");
+    }
+    return DESSERT_OK;
+}
+
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+    return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+}  // namespace
+
+dessert_status_t dessert_cache_append(const dessert_index_t* ix, const dessert_cache_t* cache, const dessert_cache_batch_t* batch,
+                                      const void* k_dev, uint64_t k_stride, const void* v_dev, uint64_t v_stride, uint32_t dtype) {
+    if (!float_type(dtype)) return fail(DESSERT_EINVAL, "dtype must be DESSERT_F16, DESSERT_BF16 or DESSERT_F32");
+    CachePages c;
+    CacheBatch b;
+    dessert_status_t st = check_cache(cache, &c);
+    if (st == DESSERT_OK) st = check_cache_batch(batch, c, &b);
+    if (st == DESSERT_OK) st = check_tokens(k_dev, k_stride, dtype, c.heads, c.dim, b.n_tokens, "k_dev");
+    if (st == DESSERT_OK) st = check_tokens(v_dev, v_stride, dtype, c.heads, c.dim, b.n_tokens, "v_dev");
+    if (st != DESSERT_OK) return st;
+    const uint64_t seq_heads = (uint64_t)b.n_seqs * c.heads, places = append_places(b.max_tokens, c.page_tokens);
+    if (seq_heads > MAX_WORKGROUPS || seq_heads * places > 1ull << 32) return fail(DESSERT_EINVAL, "too many sequences for one call");
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    if (b.n_tokens == 0 || b.n_seqs == 0) return DESSERT_OK;
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    HIP_TRY(launch_cache_append(c, b, k_dev, k_stride, v_dev, v_stride, dtype, ix->stream));
+    return DESSERT_OK;
+}
+
+size_t dessert_cache_attention_workspace_bytes(const dessert_index_t* ix, const dessert_cache_t* cache, const dessert_cache_batch_t* batch,
+                                               uint32_t n_q_heads, uint32_t n_select) {
+    CachePages c;
+    CacheBatch b;
+    uint32_t group;
+    if (!ix || check_cache(cache, &c) != DESSERT_OK || check_cache_batch(batch, c, &b) != DESSERT_OK || check_group(n_q_heads, c, &group) != DESSERT_OK) return 0;
+    return attend_workspace_upto(b.max_tokens, group, c.dim, attended(*batch, c.page_tokens, n_select), n_select != 0);
+}
+
+dessert_status_t dessert_cache_attention(const dessert_index_t* ix, const dessert_cache_t* cache, const dessert_cache_batch_t* batch,
+                                         const void* q_dev, uint32_t dtype, uint64_t q_stride, uint32_t n_q_heads, float scale,
+                                         uint32_t window, const uint32_t* pages_dev, uint32_t n_select, void* workspace_dev,
+                                         size_t workspace_bytes, void* out_dev, float* out_lse_dev) {
+    if (dtype != DESSERT_F16 && dtype != DESSERT_BF16) return fail(DESSERT_EINVAL, "dtype must be DESSERT_F16 or DESSERT_BF16");
+    AttendArgs a{};
+    dessert_status_t st = check_cache(cache, &a.cache);
+    if (st == DESSERT_OK) st = check_cache_batch(batch, a.cache, &a.batch);
+    if (st == DESSERT_OK) st = check_group(n_q_heads, a.cache, &a.group);
+    if (st == DESSERT_OK) st = check_tokens(q_dev, q_stride, dtype, n_q_heads, a.cache.dim, a.batch.n_tokens, "q_dev");
+    if (st != DESSERT_OK) return st;
+    if ((pages_dev != nullptr) != (n_select != 0)) return fail(DESSERT_EINVAL, "pages_dev and n_select go together: both or neither");
+    if ((uint64_t)n_select * a.cache.page_tokens > CACHE_MOST) return fail(DESSERT_EINVAL, "n_select is too large");
+    if (a.batch.n_tokens && !out_dev) return fail(DESSERT_EINVAL, "out_dev is NULL");
+    if ((uintptr_t)out_dev % 2 || (uintptr_t)out_lse_dev % 4 || (uintptr_t)pages_dev % 4)
+        return fail(DESSERT_EINVAL, "pages_dev and outputs must be aligned to their elements");
+    const bool none = a.batch.n_tokens == 0 || a.batch.n_seqs == 0;
+    AttendPlan p{};
+    if (!none) {
+        const uint64_t units = (uint64_t)a.batch.n_seqs * (n_select ? a.batch.max_tokens : 1);
+        if ((uint64_t)a.batch.max_tokens * a.group > CACHE_MOST || units > MAX_WORKGROUPS || units * a.cache.heads > MAX_WORKGROUPS)
+            return fail(DESSERT_EINVAL, "too many tokens for one call");
+        p = attend_plan(a.batch.n_seqs, a.batch.max_tokens, a.cache.heads, a.group, a.cache.dim, attended(*batch, a.cache.page_tokens, n_select), n_select != 0);
+        if (p.groups * p.parts > MAX_WORKGROUPS) return fail(DESSERT_EINVAL, "too many tokens for one call");
+        st = check_workspace(workspace_dev, workspace_bytes, p.bytes);
+        if (st != DESSERT_OK) return st;
+    }
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    if (none) return DESSERT_OK;
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    a.q = q_dev; a.q_stride = q_stride; a.dtype = dtype; a.window = window; a.n_select = n_select; a.pages = pages_dev;
+    a.scale = scale; a.out = out_dev; a.lse = out_lse_dev;
+    HIP_TRY(launch_cache_attention(a, p, workspace_dev, ix->stream));
+    return DESSERT_OK;
+}
+
+size_t dessert_cache_select_workspace_bytes(const dessert_index_t* ix, const dessert_cache_t* cache, const dessert_cache_batch_t* batch) {
+    CachePages c;
+    CacheBatch b;
+    if (!ix || check_cache(cache, &c) != DESSERT_OK || check_cache_batch(batch, c, &b) != DESSERT_OK) return 0;
+    const size_t need = select_workspace(b.n_tokens, c.heads, b.table_pages);
+    return need == ~(size_t)0 ? 0 : need;
+}
+
+dessert_status_t dessert_cache_select(const dessert_index_t* ix, const dessert_cache_t* cache, const dessert_cache_batch_t* batch,
+                                      const int8_t* q_codes_dev, const float* q_scales_dev, uint32_t n_q_heads, uint32_t n_select,
+                                      uint32_t n_first, uint32_t n_last, void* workspace_dev, size_t workspace_bytes, uint32_t* out_pages_dev) {
+    SelectArgs a{};
+    dessert_status_t st = check_cache(cache, &a.cache);
+    if (st == DESSERT_OK) st = check_cache_batch(batch, a.cache, &a.batch);
+    if (st == DESSERT_OK) st = check_group(n_q_heads, a.cache, &a.group);
+    if (st != DESSERT_OK) return st;
+    if (!a.cache.bounds) return fail(DESSERT_EINVAL, "the cache has no bounds");
+    if (n_select == 0 || n_select > CACHE_MOST || (uint64_t)n_first + n_last > n_select) return fail(DESSERT_EINVAL, "n_select must be at least 1 and n_first + n_last");
+    if (a.batch.n_tokens && (!q_codes_dev || !q_scales_dev || !out_pages_dev)) return fail(DESSERT_EINVAL, "NULL argument");
+    if ((uintptr_t)q_scales_dev % 4 || (uintptr_t)out_pages_dev % 4) return fail(DESSERT_EINVAL, "q_scales_dev and out_pages_dev must be 4-byte aligned");
+    const bool none = a.batch.n_tokens == 0 || a.batch.n_seqs == 0;
+    if (!none) {
+        const uint64_t seqs_tokens = (uint64_t)a.batch.n_seqs * a.batch.max_tokens;
+        if (seqs_tokens > MAX_WORKGROUPS || seqs_tokens * a.cache.heads * divided_up(a.batch.table_pages, 256) > MAX_WORKGROUPS)
+            return fail(DESSERT_EINVAL, "too many tokens for one call");
+        st = check_workspace(workspace_dev, workspace_bytes, select_workspace(a.batch.n_tokens, a.cache.heads, a.batch.table_pages));
+        if (st != DESSERT_OK) return st;
+    }
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    if (none) return DESSERT_OK;
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    a.q = q_codes_dev; a.q_scales = q_scales_dev; a.n_select = n_select; a.n_first = n_first; a.n_last = n_last;
+    a.keys = (uint32_t*)workspace_dev; a.out = out_pages_dev;
+    HIP_TRY(launch_cache_select(a, ix->stream));
+    return DESSERT_OK;
+}
+
+size_t dessert_cache_advance_workspace_bytes(const dessert_index_t* ix, uint32_t n_pages, uint32_t n_new) {
+    if (!ix || n_pages == 0 || n_pages > CACHE_MOST || n_new > CACHE_MOST) return 0;
+    return advance_plan(n_pages, n_new).bytes;
+}
+
+dessert_status_t dessert_cache_advance(const dessert_index_t* ix, const dessert_cache_t* layers, uint32_t n_layers, uint32_t* refs_dev,
+                                       const uint32_t* tables_dev, uint32_t table_pages, const uint32_t* lengths_dev, uint32_t n_seqs,
+                                       const uint32_t* parents_dev, const uint32_t* add_dev, uint32_t n_new, void* workspace_dev,
+                                       size_t workspace_bytes, uint32_t* out_tables_dev, uint32_t* out_lengths_dev, uint32_t* out_status_dev) {
+    std::vector<CachePages> pages;
+    dessert_status_t st = check_layers(layers, n_layers, &pages);
+    if (st == DESSERT_OK) st = check_table(tables_dev, table_pages, lengths_dev, n_seqs, pages[0].page_tokens);
+    if (st != DESSERT_OK) return st;
+    if (!parents_dev && n_new && n_new != n_seqs) return fail(DESSERT_EINVAL, "without parents_dev each sequence goes on: n_new = n_seqs");
+    if (!refs_dev || !out_status_dev || (n_new && (!add_dev || !out_tables_dev || !out_lengths_dev))) return fail(DESSERT_EINVAL, "NULL argument");
+    if ((uintptr_t)refs_dev % 4 || (uintptr_t)parents_dev % 4 || (uintptr_t)add_dev % 4 || (uintptr_t)out_tables_dev % 4 || (uintptr_t)out_lengths_dev % 4 ||
+        (uintptr_t)out_status_dev % 4)
+        return fail(DESSERT_EINVAL, "arrays must be 4-byte aligned");
+    if (n_new && n_seqs && (overlap(tables_dev, 4ull * n_seqs * table_pages, out_tables_dev, 4ull * n_new * table_pages) ||
+                            overlap(lengths_dev, 4ull * n_seqs, out_lengths_dev, 4ull * n_new)))
+        return fail(DESSERT_EINVAL, "out_tables_dev and out_lengths_dev must lie apart from what they are made of");
+    if (n_new > CACHE_MOST || (uint64_t)n_new * divided_up((uint64_t)pages[0].heads * pages[0].page_tokens * pages[0].dim, 8192) > MAX_WORKGROUPS)
+        return fail(DESSERT_EINVAL, "too many sequences for one call");
+    st = check_workspace(workspace_dev, workspace_bytes, advance_plan(pages[0].n_pages, n_new).bytes);
+    if (st != DESSERT_OK) return st;
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    AdvanceArgs a{};
+    a.p = {pages.data(), n_layers, refs_dev, const_cast<uint32_t*>(tables_dev), lengths_dev, n_seqs, table_pages};
+    a.parents = parents_dev; a.add = add_dev; a.n_new = n_new;
+    a.counts = parents_dev || n_new == 0;
+    a.out_tables = out_tables_dev; a.out_lengths = out_lengths_dev; a.status = out_status_dev;
+    HIP_TRY(launch_cache_advance(a, workspace_dev, ix->stream));
+    return DESSERT_OK;
+}
+
+size_t dessert_cache_compact_workspace_bytes(const dessert_index_t* ix, uint32_t n_pages) {
+    if (!ix || n_pages == 0 || n_pages > CACHE_MOST) return 0;
+    return compact_plan(n_pages).bytes;
+}
+
+dessert_status_t dessert_cache_compact(const dessert_index_t* ix, const dessert_cache_t* layers, uint32_t n_layers, uint32_t* refs_dev,
+                                       uint32_t* tables_dev, uint32_t table_pages, const uint32_t* lengths_dev, uint32_t n_seqs,
+                                       void* workspace_dev, size_t workspace_bytes, uint32_t* out_numbers_dev, uint32_t* out_live_dev) {
+    std::vector<CachePages> pages;
+    dessert_status_t st = check_layers(layers, n_layers, &pages);
+    if (st == DESSERT_OK) st = check_table(tables_dev, table_pages, lengths_dev, n_seqs, pages[0].page_tokens);
+    if (st != DESSERT_OK) return st;
+    if (!refs_dev || !out_numbers_dev || !out_live_dev) return fail(DESSERT_EINVAL, "NULL argument");
+    if ((uintptr_t)refs_dev % 4 || (uintptr_t)out_numbers_dev % 4 || (uintptr_t)out_live_dev % 4) return fail(DESSERT_EINVAL, "arrays must be 4-byte aligned");
+    st = check_workspace(workspace_dev, workspace_bytes, compact_plan(pages[0].n_pages).bytes);
+    if (st != DESSERT_OK) return st;
+    if (!ix) return fail(DESSERT_EINVAL, "index is NULL");
+    DeviceGuard guard(ix->cfg.device);
+    if (!guard.ok) return fail(DESSERT_EHIP, "hipSetDevice(%d) failed", ix->cfg.device);
+    CompactArgs a{};
+    a.p = {pages.data(), n_layers, refs_dev, tables_dev, lengths_dev, n_seqs, table_pages};
+    a.numbers = out_numbers_dev; a.live = out_live_dev;
+    HIP_TRY(launch_cache_compact(a, workspace_dev, ix->stream));
+    return DESSERT_OK;
+}
+
 }  // extern "C"

@@ -1,0 +1,588 @@
+// Attention of new tokens over a paged int8 cache: for the rows of a key head (its query heads, the new tokens)
+//   s_j = scale * k_scale(page of j) * q . k_j     over the visible j: not behind the row's position, inside the window, on a page
+//   out = sum_j e^(s_j - m) v_scale(page of j) v_j / sum_j e^(s_j - m),   lse = m + log sum_j e^(s_j - m),   m = max_j s_j
+// in one pass over the keys with a running m.  All products go to the matrix cores in fp16, which holds codes exactly; queries of bf16 are
+// first scaled by a power of two a row, which makes their 8 bits exact in fp16 (but for parts below 2^-37 of the row's largest).
+// e^s v_scale is rounded to fp16 (off by at most 2^-11 of itself: the rounding of an fp16 result), 2^12 being the largest of a row so far, which
+// keeps all down to 2^-26 of the largest a normal number however far apart the scales of pages are; sums, maxima and the outputs are held
+// in 32 bits.  Below, exponents are in powers of two: m the largest s log2(e), top the largest s log2(e) + log2(v_scale).
+// Scores are formed as K Q^T: a lane then holds consecutive tokens of one row, and these are what it has to give as its part of P for
+// O^T = V^T P^T, so P goes from one product to the next in registers.
+#include "cache_common.hpp"
+
+namespace dessert {
+
+namespace {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr float NEVER = -__builtin_huge_valf();
+constexpr float P_TOP = 12.f;      // the largest of P so far is 2^12
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What e^(s - m) is multiplied by to be a part of P.  (The exponent passes 120 only with scales that are 2^100 apart.)
+__device__ inline float p_factor(float vs, float m, float top) {
+    return vs * exp2_fast(fminf((m == NEVER ? 0.f : m) - (top == NEVER ? 0.f : top) + P_TOP, 120.f));
+}
+
+// 4 signed bytes to fp16, exactly: 1024 + (c + 128) is 0x6400 | byte.
+__device__ inline void bytes_to_half(uint32_t w, half2_t& lo, half2_t& hi) {
+    const uint32_t x = w ^ 0x80808080u;
+    const uint32_t a = __builtin_amdgcn_perm(0x64646464u, x, 0x04010400u), b = __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u);
+    const half2_t bias = {(_Float16)1152.f, (_Float16)1152.f};
+    lo = __builtin_bit_cast(half2_t, a) - bias;
+    hi = __builtin_bit_cast(half2_t, b) - bias;
+}
+
+__device__ inline half8 codes_to_half(uint32_t w0, uint32_t w1) {
+    half2_t r[4];
+    bytes_to_half(w0, r[0], r[1]);
+    bytes_to_half(w1, r[2], r[3]);
+    return __builtin_bit_cast(half8, r);
+}
+
+// 8 elements of a query row as fp16, of bf16 still to be scaled by the row.
+__device__ inline void load_query(const void* q, uint64_t at, uint32_t dtype, float (&x)[8]) {
+    if (dtype == TYPE_F16) {
+        f16_t v[8];
+        __builtin_memcpy(v, (const f16_t*)q + at, 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+    } else {
+        bf16_t v[8];
+        __builtin_memcpy(v, (const bf16_t*)q + at, 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+    }
+}
+
+// A row that holds an infinity or NaN gives NaN wherever it sees a key.
+__device__ inline float query_factor(float peak, float scale, int e) {
+    return peak < __builtin_huge_valf() ? ldexpf(scale * LOG2E, -e) : __builtin_nanf("");
+}
+
+// The power of two that brings a bf16 row's largest magnitude to [2^13, 2^14); 1 for fp16, rows of zeros, infinities and NaN.
+__device__ inline int query_exponent(float peak, uint32_t dtype) {
+    if (dtype == TYPE_F16 || !(peak > 0.f && peak < __builtin_huge_valf())) return 0;
+    int e;
+    (void)frexpf(peak, &e);
+    return 14 - e;
+}
+
+template <int N>
+__device__ inline void store_out(void* out, uint64_t at, uint32_t dtype, const float (&x)[N]) {
+    if (dtype == TYPE_F16) store_run((f16_t*)out + at, x);
+    else store_run((bf16_t*)out + at, x);
+}
+
+// A unit's rows: the query heads of key head h for tokens of one sequence (or, with lists of pages, of one token).
+struct Unit {
+    uint32_t seq, head, first_token;   // first_token: its row in q
+    uint32_t rows;                     // rows of the unit
+    int32_t begin;                     // the first token's position
+    uint32_t lo, hi;                   // keys that some row sees lie at lo .. hi of the axis (with lists: of the listed pages)
+};
+
+__device__ inline Unit unit_of(const AttendArgs& a, uint32_t index, uint32_t head) {
+    Unit u;
+    u.head = head;
+    const bool lists = a.pages != nullptr;
+    u.seq = lists ? index / a.batch.max_tokens : index;
+    const uint32_t t = lists ? index % a.batch.max_tokens : 0;
+    const NewTokens n = new_tokens(a.batch, u.seq);
+    const uint32_t tokens = lists ? (t < n.count ? 1u : 0u) : n.count;
+    u.first_token = n.first + t;
+    u.begin = n.begin + (int32_t)t;
+    u.rows = tokens * a.group;
+    const int32_t last = u.begin + (int32_t)tokens - 1;
+    u.lo = 0;
+    if (lists) {
+        u.hi = a.n_select << a.cache.shift;
+    } else {
+        u.hi = last < 0 ? 0u : min((uint32_t)last + 1u, a.batch.table_pages << a.cache.shift);
+        if (a.window && u.begin >= 0 && (uint32_t)u.begin + 1u > a.window) u.lo = (uint32_t)u.begin + 1u - a.window;
+    }
+    return u;
+}
+
+__device__ inline uint32_t unit_parts(const AttendArgs& a, const Unit& u) {
+    const uint32_t first = u.lo / ATTEND_CHUNK, end = (u.hi + ATTEND_CHUNK - 1) / ATTEND_CHUNK;
+    if (end <= first) return 1;
+    return min((end - first + a.part_chunks - 1) / a.part_chunks, a.parts);
+}
+
+// The steps of a part; the last part of a call goes on to the end, however long a sequence is.
+__device__ inline void part_range(const AttendArgs& a, const Unit& u, uint32_t part, uint32_t& begin, uint32_t& end) {
+    const uint32_t first = u.lo / ATTEND_CHUNK, last = (u.hi + ATTEND_CHUNK - 1) / ATTEND_CHUNK;
+    begin = first + part * a.part_chunks;
+    end = part + 1 == a.parts ? last : min(last, begin + a.part_chunks);
+}
+
+// Where 16 tokens of the axis lie: their page (or NO_PAGE) and the position of the first.
+struct Group16 {
+    uint32_t page, offset;
+    int32_t pos;
+};
+
+__device__ inline Group16 group_at(const AttendArgs& a, const uint32_t* table, const uint32_t* list, uint32_t token) {
+    Group16 g;
+    uint32_t place = token >> a.cache.shift;
+    g.offset = token & (a.cache.page_tokens - 1);
+    if (list) place = place < a.n_select ? list[place] : NO_PAGE;
+    g.page = page_at(a.batch, table, place, a.cache.n_pages);
+    g.pos = g.page == NO_PAGE ? 0x7FFFFFFF - 64 : (int32_t)((place << a.cache.shift) + g.offset);
+    return g;
+}
+
+// ---- few rows: 16 to a workgroup, each of its four waves takes every fourth step of 64 tokens --------------------------------
+// Keys and values come from memory straight into the layout of the products: a lane reads 16 bytes of a key (or of a value channel's
+// 16 tokens), converts them, and no LDS is used before the waves' results are joined.
+template <int ND>
+__global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
+    constexpr int D = ND * 32, NV = D / 16;
+    __shared__ float joined[4][16][D + 4];
+    __shared__ float sums[4][16][2];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    uint32_t id = blockIdx.x;
+    const uint32_t part = id % a.parts;
+    id /= a.parts;
+    const uint32_t group_index = id;
+    const uint32_t tile = id % a.tiles;
+    id /= a.tiles;
+    const Unit u = unit_of(a, id / a.cache.heads, id % a.cache.heads);
+    if (tile * 16 >= u.rows || part >= unit_parts(a, u)) return;
+    uint32_t c0, c1;
+    part_range(a, u, part, c0, c1);
+    const uint32_t* table = a.batch.tables + (uint64_t)u.seq * a.batch.table_pages;
+    const uint32_t* list = a.pages ? a.pages + ((uint64_t)u.first_token * a.cache.heads + u.head) * a.n_select : nullptr;
+    const uint32_t heads = a.cache.heads, q_heads = heads * a.group;
+
+    // the row of this lane
+    const uint32_t row = min(tile * 16 + r, u.rows - 1);
+    const uint32_t token = u.first_token + row / a.group, q_head = u.head * a.group + row % a.group;
+    const int32_t pos = u.begin + (int32_t)(row / a.group);
+    const int32_t least = a.window ? max(pos - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
+    half8 q[ND];
+    float factor;
+    {
+        float x[ND][8], peak = 0.f;
+        const uint64_t at = (uint64_t)token * a.q_stride + (uint64_t)q_head * D;
+#pragma unroll
+        for (int f = 0; f < ND; ++f) {
+            const int d = f < ND / 2 * 2 ? 64 * (f / 2) + 16 * (int)g + 8 * (f % 2) : 32 * f + 8 * (int)g;
+            load_query(a.q, at + d, a.dtype, x[f]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) peak = fmaxf(peak, x[f][i] == x[f][i] ? fabsf(x[f][i]) : __builtin_huge_valf());
+        }
+        peak = fmaxf(peak, __shfl_xor(peak, 16));
+        peak = fmaxf(peak, __shfl_xor(peak, 32));
+        const int e = query_exponent(peak, a.dtype);
+#pragma unroll
+        for (int f = 0; f < ND; ++f)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[f][i] = (f16_t)ldexpf(x[f][i], e);
+        factor = query_factor(peak, a.scale, e);
+    }
+
+    f32x4 o[NV] = {};
+    float m = NEVER, top = NEVER, l = 0.f;
+    for (uint32_t c = c0 + wave; c < c1; c += 4) {
+        const Group16 kg = group_at(a, table, list, c * 64 + 16 * (r >> 2));   // of the key this lane reads
+        const Group16 vg = group_at(a, table, list, c * 64 + 16 * g);          // of the values it reads and the scores it holds
+        const uint32_t k_page = kg.page == NO_PAGE ? 0u : kg.page, v_page = vg.page == NO_PAGE ? 0u : vg.page;
+        const int8_t* k = a.cache.k + (((uint64_t)k_page * heads + u.head) * a.cache.page_tokens + kg.offset + (r & 3)) * D;
+        const int8_t* v = a.cache.v + ((uint64_t)v_page * heads + u.head) * D * a.cache.page_tokens + (uint64_t)r * a.cache.page_tokens + vg.offset;
+        u32x4 kc[4][ND / 2 + 1], vc[NV];
+        u32x2 kt[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int f = 0; f < ND / 2; ++f) kc[t][f] = *(const u32x4*)(k + 4 * t * D + 64 * f + 16 * g);
+            if constexpr (ND % 2) kt[t] = *(const u32x2*)(k + 4 * t * D + 32 * (ND - 1) + 8 * g);
+        }
+        const float ks = a.cache.ks[(uint64_t)v_page * heads + u.head] * factor, vs = a.cache.vs[(uint64_t)v_page * heads + u.head];
+#pragma unroll
+        for (int d = 0; d < NV; ++d) vc[d] = *(const u32x4*)(v + (uint64_t)(16 * d) * a.cache.page_tokens);
+        f32x4 s[4] = {};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int f = 0; f < ND / 2; ++f) {
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(kc[t][f].x, kc[t][f].y), q[2 * f], s[t], 0, 0, 0);
+                s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(kc[t][f].z, kc[t][f].w), q[2 * f + 1], s[t], 0, 0, 0);
+            }
+            if constexpr (ND % 2) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(kt[t].x, kt[t].y), q[ND - 1], s[t], 0, 0, 0);
+        }
+        const bool whole = __all(vg.pos + 15 <= pos && vg.pos >= least);
+        float peak = NEVER;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t at = vg.pos + 4 * t + i;
+                s[t][i] = whole || (at <= pos && at >= least) ? s[t][i] * ks : NEVER;
+                peak = fmaxf(peak, s[t][i]);
+            }
+        float high = vs < __builtin_huge_valf() ? peak + __builtin_amdgcn_logf(vs) : NEVER;
+        high = fmaxf(high, __shfl_xor(high, 16));
+        high = fmaxf(high, __shfl_xor(high, 32));
+        peak = fmaxf(peak, __shfl_xor(peak, 16));
+        peak = fmaxf(peak, __shfl_xor(peak, 32));
+        if (__any(peak > m || high > top)) {
+            const float m_new = fmaxf(m, peak), top_new = fmaxf(top, high);
+            if (m_new != m) l *= exp2_fast(m - m_new);
+            if (top_new != top) {
+                const float keep = exp2_fast(top - top_new);
+#pragma unroll
+                for (int d = 0; d < NV; ++d) o[d] *= keep;
+            }
+            m = m_new;
+            top = top_new;
+        }
+        const float base = m == NEVER ? 0.f : m;
+        const float weight = p_factor(vs, m, top);
+        half8 p[2];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float e = exp2_fast(s[t][i] - base);
+                l += e;
+                p[t / 2][t % 2 * 4 + i] = (f16_t)(whole || s[t][i] != NEVER ? e * weight : 0.f);
+            }
+#pragma unroll
+        for (int d = 0; d < NV; ++d) {
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(vc[d].x, vc[d].y), p[0], o[d], 0, 0, 0);
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(vc[d].z, vc[d].w), p[1], o[d], 0, 0, 0);
+        }
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    // the four waves' results
+    if (g == 0) {
+        sums[wave][r][0] = m;
+        sums[wave][r][1] = l;
+    }
+    __syncthreads();
+    float most = sums[0][r][0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) most = fmaxf(most, sums[w][r][0]);
+    const float mine = exp2_fast(top - P_TOP - (most == NEVER ? 0.f : most));
+#pragma unroll
+    for (int d = 0; d < NV; ++d) *(f32x4*)&joined[wave][r][16 * d + 4 * g] = o[d] * mine;
+    __syncthreads();
+    constexpr int PER = D / 4;    // threads of a row, 4 channels each
+    for (uint32_t i = threadIdx.x; i < 16 * PER; i += 256) {
+        const uint32_t rr = i / PER, d = i % PER * 4;
+        if (tile * 16 + rr >= u.rows) break;
+        float mm = sums[0][rr][0], ll = 0.f;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) mm = fmaxf(mm, sums[w][rr][0]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) ll += sums[w][rr][1] * (sums[w][rr][0] == mm ? 1.f : exp2_fast(sums[w][rr][0] - mm));
+        f32x4 x = *(const f32x4*)&joined[0][rr][d];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) x += *(const f32x4*)&joined[w][rr][d];
+        if (a.parts == 1) {
+            const uint32_t full = tile * 16 + rr;
+            const uint64_t at = (uint64_t)(u.first_token + full / a.group) * q_heads + u.head * a.group + full % a.group;
+            const float by = ll == 0.f ? 0.f : 1.f / ll;
+            const float y[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
+            store_out(a.out, at * D + d, a.dtype, y);
+            if (a.lse && d == 0) a.lse[at] = ll == 0.f ? NEVER : (mm + log2f(ll)) * LN2;
+        } else {
+            const uint64_t slot = ((uint64_t)group_index * a.parts + part) * 16 + rr;
+            *(f32x4*)(a.part_out + slot * D + d) = x;
+            if (d == 0) a.part_sums[slot] = make_float2(mm, ll);
+        }
+    }
+}
+
+// ---- many rows: 128 to a workgroup, 32 to a wave, all over the same steps of 64 tokens ---------------------------------------
+// Keys and values are converted once for the workgroup's four waves on their way into LDS, two steps' worth of it: while one is computed
+// with, the next one's codes are under way from memory.  Rows in LDS are 16 bytes apart from a multiple of their length: a wave's 16-byte
+// reads then spread over all banks.
+template <int ND>
+__global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(AttendArgs a) {
+    constexpr int D = ND * 32, KS = D + 8, VS = 64 + 8, UNITS = D * 4, PER = (UNITS + 255) / 256;
+    __shared__ f16_t k_tile[2][64 * KS];
+    __shared__ f16_t v_tile[2][D * VS];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
+    uint32_t id = blockIdx.x;
+    const uint32_t part = id % a.parts;
+    id /= a.parts;
+    const uint32_t group_index = id;
+    const uint32_t tile = a.tiles - 1 - id % a.tiles;      // the longest first
+    id /= a.tiles;
+    const Unit whole_unit = unit_of(a, id / a.cache.heads, id % a.cache.heads);
+    if (tile * ATTEND_MANY >= whole_unit.rows) return;
+    // what this workgroup's rows see
+    Unit u = whole_unit;
+    {
+        const uint32_t t0 = tile * ATTEND_MANY / a.group, t1 = min((tile + 1) * ATTEND_MANY - 1, u.rows - 1) / a.group;
+        const int32_t p0 = u.begin + (int32_t)t0, p1 = u.begin + (int32_t)t1;
+        u.hi = p1 < 0 ? 0u : min(u.hi, (uint32_t)p1 + 1u);
+        u.lo = a.window && p0 >= 0 && (uint32_t)p0 + 1u > a.window ? (uint32_t)p0 + 1u - a.window : 0u;
+    }
+    if (part >= unit_parts(a, u)) return;
+    uint32_t c0, c1;
+    part_range(a, u, part, c0, c1);
+    const uint32_t* table = a.batch.tables + (uint64_t)u.seq * a.batch.table_pages;
+    const uint32_t heads = a.cache.heads, q_heads = heads * a.group, T = a.cache.page_tokens;
+
+    const uint32_t row = tile * ATTEND_MANY + wave * 32 + r;
+    const bool there = row < u.rows;
+    const uint32_t safe = min(row, u.rows - 1);
+    const uint32_t token = u.first_token + safe / a.group, q_head = u.head * a.group + safe % a.group;
+    const int32_t pos = u.begin + (int32_t)(safe / a.group);
+    const int32_t least = a.window ? max(pos - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
+    // of the wave's rows
+    const uint32_t w0 = min(tile * ATTEND_MANY + wave * 32, u.rows - 1), w1 = min(tile * ATTEND_MANY + wave * 32 + 31, u.rows - 1);
+    const int32_t pos_first = u.begin + (int32_t)(w0 / a.group), pos_last = u.begin + (int32_t)(w1 / a.group);
+    const int32_t least_first = a.window ? max(pos_first - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
+    const int32_t least_last = a.window ? max(pos_last - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
+
+    half8 q[D / 16];
+    float factor;
+    {
+        float peak = 0.f;
+        const uint64_t at = (uint64_t)token * a.q_stride + (uint64_t)q_head * D + 8 * h;
+#pragma unroll
+        for (int f = 0; f < D / 16; ++f) {
+            float x[8];
+            load_query(a.q, at + 16 * f, a.dtype, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) peak = fmaxf(peak, x[i] == x[i] ? fabsf(x[i]) : __builtin_huge_valf());
+        }
+        peak = fmaxf(peak, __shfl_xor(peak, 32));
+        const int e = query_exponent(peak, a.dtype);
+#pragma unroll
+        for (int f = 0; f < D / 16; ++f) {
+            float x[8];
+            load_query(a.q, at + 16 * f, a.dtype, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[f][i] = (f16_t)ldexpf(x[i], e);
+        }
+        factor = query_factor(peak, a.scale, e);
+    }
+
+    // a step's codes: `PER` runs of 16 keys' channels and 16 values' tokens a thread
+    u32x4 kc[PER], vc[PER];
+    auto fetch = [&](uint32_t c) {
+        uint32_t page[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            page[j] = page_at(a.batch, table, (c * 64 + 16 * j) >> a.cache.shift, a.cache.n_pages);
+            page[j] = page[j] == NO_PAGE ? 0u : page[j];
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t n = threadIdx.x + 256 * i;
+            if (UNITS % 256 == 0 || n < UNITS) {
+                const uint32_t t = n / (D / 16), d = n % (D / 16) * 16, j = t >> 4;
+                const uint32_t kp = j < 2 ? (j == 0 ? page[0] : page[1]) : (j == 2 ? page[2] : page[3]);
+                kc[i] = *(const u32x4*)(a.cache.k + (((uint64_t)kp * heads + u.head) * T + ((c * 64 + t) & (T - 1))) * D + d);
+                const uint32_t jv = n & 3, dv = n >> 2;
+                const uint32_t vp = jv < 2 ? (jv == 0 ? page[0] : page[1]) : (jv == 2 ? page[2] : page[3]);
+                vc[i] = *(const u32x4*)(a.cache.v + (((uint64_t)vp * heads + u.head) * D + dv) * T + ((c * 64 + 16 * jv) & (T - 1)));
+            }
+        }
+    };
+    auto put = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t n = threadIdx.x + 256 * i;
+            if (UNITS % 256 == 0 || n < UNITS) {
+                f16_t* k = &k_tile[buffer][n / (D / 16) * KS + n % (D / 16) * 16];
+                *(half8*)k = codes_to_half(kc[i].x, kc[i].y);
+                *(half8*)(k + 8) = codes_to_half(kc[i].z, kc[i].w);
+                f16_t* v = &v_tile[buffer][(n >> 2) * VS + (n & 3) * 16];
+                *(half8*)v = codes_to_half(vc[i].x, vc[i].y);
+                *(half8*)(v + 8) = codes_to_half(vc[i].z, vc[i].w);
+            }
+        }
+    };
+
+    f32x16 o[ND] = {};
+    float m = NEVER, top = NEVER, l = 0.f;
+    // row m of a product's 32 tokens is token 16 (m / 16) + 8 (m / 4 % 2) + 4 (m / 8 % 2) + m % 4: a lane's 16 scores are then two runs of 8 tokens
+    const uint32_t k_row = 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3);
+    if (c0 < c1) fetch(c0);
+    for (uint32_t c = c0; c < c1; ++c) {
+        const int buffer = (c - c0) & 1;
+        put(buffer);
+        if (c + 1 < c1) fetch(c + 1);
+        __syncthreads();
+        const int32_t from = (int32_t)(c * 64);
+        if (from > pos_last || from + 63 < least_first) continue;
+        float ks[4], vs[4];
+        bool missing = false;
+        uint32_t absent = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t page = page_at(a.batch, table, (c * 64 + 16 * j) >> a.cache.shift, a.cache.n_pages);
+            if (page == NO_PAGE) {
+                missing = true;
+                absent |= 1u << j;
+            }
+            const uint64_t at = (uint64_t)(page == NO_PAGE ? 0u : page) * heads + u.head;
+            ks[j] = a.cache.ks[at] * factor;
+            vs[j] = a.cache.vs[at];
+        }
+        f32x16 s[2] = {};
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int f = 0; f < D / 16; ++f)
+                s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)&k_tile[buffer][(32 * mt + k_row) * KS + 16 * f + 8 * h], q[f], s[mt], 0, 0, 0);
+        const bool inside = from + 63 <= pos_first && from >= least_last && !missing;
+        float peaks[4] = {NEVER, NEVER, NEVER, NEVER};
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int j = 2 * mt + i / 8;
+                const int32_t at = from + 16 * j + 8 * (int32_t)h + i % 8;
+                s[mt][i] = inside || (at <= pos && at >= least && !(absent >> j & 1)) ? s[mt][i] * ks[j] : NEVER;
+                peaks[j] = fmaxf(peaks[j], s[mt][i]);
+            }
+        float peak = NEVER, high = NEVER;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            peak = fmaxf(peak, peaks[j]);
+            high = fmaxf(high, vs[j] < __builtin_huge_valf() ? peaks[j] + __builtin_amdgcn_logf(vs[j]) : NEVER);
+        }
+        peak = fmaxf(peak, __shfl_xor(peak, 32));
+        high = fmaxf(high, __shfl_xor(high, 32));
+        if (__any(peak > m || high > top)) {
+            const float m_new = fmaxf(m, peak), top_new = fmaxf(top, high);
+            if (m_new != m) l *= exp2_fast(m - m_new);
+            if (top_new != top) {
+                const float keep = exp2_fast(top - top_new);
+#pragma unroll
+                for (int d = 0; d < ND; ++d) o[d] *= keep;
+            }
+            m = m_new;
+            top = top_new;
+        }
+        const float base = m == NEVER ? 0.f : m;
+        float weight[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) weight[j] = p_factor(vs[j], m, top);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            half8 p;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = s[j / 2][j % 2 * 8 + i], e = exp2_fast(x - base);
+                l += e;
+                p[i] = (f16_t)(inside || x != NEVER ? e * weight[j] : 0.f);
+            }
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)&v_tile[buffer][(32 * d + r) * VS + 16 * j + 8 * h], p, o[d], 0, 0, 0);
+        }
+    }
+    l += __shfl_xor(l, 32);
+    if (!there) return;
+    const float by = exp2_fast(top - P_TOP - (m == NEVER ? 0.f : m)) * (a.parts == 1 ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
+    const uint64_t at = (uint64_t)token * q_heads + q_head;
+    const uint64_t slot = ((uint64_t)(group_index - group_index % a.tiles + tile) * a.parts + part) * ATTEND_MANY + wave * 32 + r;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int ch = 32 * d + 8 * j + 4 * (int)h;
+            const float y[4] = {o[d][4 * j] * by, o[d][4 * j + 1] * by, o[d][4 * j + 2] * by, o[d][4 * j + 3] * by};
+            if (a.parts == 1) store_out(a.out, at * D + ch, a.dtype, y);
+            else __builtin_memcpy(a.part_out + slot * D + ch, y, 16);
+        }
+    if (h == 0) {
+        if (a.parts > 1) a.part_sums[slot] = make_float2(m, l);
+        else if (a.lse) a.lse[at] = l == 0.f ? NEVER : (m + log2f(l)) * LN2;
+    }
+}
+
+// ---- the parts of the keys' axis joined: a workgroup a row, parts over its groups of lanes --------------------------------------
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t rows) {
+    __shared__ f32x4 joined[256];
+    const uint32_t D = a.cache.dim, per = D / 4, lanes = 256 / per;
+    uint32_t id = blockIdx.x;
+    const uint32_t rr = id % rows;
+    id /= rows;
+    const uint32_t group_index = id, tile = id % a.tiles;
+    id /= a.tiles;
+    Unit u = unit_of(a, id / a.cache.heads, id % a.cache.heads);
+    const uint32_t row = tile * rows + rr;
+    if (row >= u.rows) return;
+    if (!a.pages && rows == ATTEND_MANY) {
+        const uint32_t t0 = tile * rows / a.group, t1 = min((tile + 1) * rows - 1, u.rows - 1) / a.group;
+        const int32_t p0 = u.begin + (int32_t)t0, p1 = u.begin + (int32_t)t1;
+        u.hi = p1 < 0 ? 0u : min(u.hi, (uint32_t)p1 + 1u);
+        u.lo = a.window && p0 >= 0 && (uint32_t)p0 + 1u > a.window ? (uint32_t)p0 + 1u - a.window : 0u;
+    }
+    const uint32_t parts = unit_parts(a, u);
+    const uint64_t slot0 = (uint64_t)group_index * a.parts * rows + rr;
+    float m = NEVER, l = 0.f;
+    for (uint32_t i = 0; i < parts; ++i) m = fmaxf(m, a.part_sums[slot0 + (uint64_t)i * rows].x);
+    for (uint32_t i = 0; i < parts; ++i) {
+        const float2 s = a.part_sums[slot0 + (uint64_t)i * rows];
+        l += s.y * (s.x == m ? 1.f : exp2_fast(s.x - m));
+    }
+    const uint32_t part0 = threadIdx.x / per, d = threadIdx.x % per * 4;
+    f32x4 x = {};
+    if (part0 < lanes)
+        for (uint32_t i = part0; i < parts; i += lanes) {
+            const uint64_t slot = slot0 + (uint64_t)i * rows;
+            const float mi = a.part_sums[slot].x;
+            if (mi == NEVER && a.part_sums[slot].y == 0.f) continue;
+            x += *(const f32x4*)(a.part_out + slot * D + d) * (mi == m ? 1.f : exp2_fast(mi - m));
+        }
+    joined[threadIdx.x] = x;
+    __syncthreads();
+    if (part0 != 0) return;
+    for (uint32_t i = 1; i < lanes; ++i) x += joined[i * per + threadIdx.x];
+    const uint64_t at = (uint64_t)(u.first_token + row / a.group) * (a.cache.heads * a.group) + u.head * a.group + row % a.group;
+    const float by = l == 0.f ? 0.f : 1.f / l;
+    const float y[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
+    store_out(a.out, at * D + d, a.dtype, y);
+    if (a.lse && d == 0) a.lse[at] = l == 0.f ? NEVER : (m + log2f(l)) * LN2;
+}
+
+template <int ND>
+void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
+    const dim3 grid((uint32_t)(p.groups * p.parts));
+    if (p.few) attend_few_kernel<ND><<<grid, dim3(256), 0, stream>>>(a);
+    else attend_many_kernel<ND><<<grid, dim3(256), 0, stream>>>(a);
+}
+
+}  // namespace
+
+hipError_t launch_cache_attention(AttendArgs a, const AttendPlan& p, void* workspace, hipStream_t stream) {
+    a.parts = p.parts;
+    a.part_chunks = p.part_chunks;
+    a.tiles = p.tiles;
+    a.part_out = (float*)workspace;
+    a.part_sums = (float2*)((char*)workspace + p.sums);
+    switch (a.cache.dim / 32) {
+        case 1: launch_attend<1>(a, p, stream); break;
+        case 2: launch_attend<2>(a, p, stream); break;
+        case 3: launch_attend<3>(a, p, stream); break;
+        case 4: launch_attend<4>(a, p, stream); break;
+        case 5: launch_attend<5>(a, p, stream); break;
+        case 6: launch_attend<6>(a, p, stream); break;
+        case 7: launch_attend<7>(a, p, stream); break;
+        default: launch_attend<8>(a, p, stream); break;
+    }
+    if (p.parts > 1) attend_join_kernel<<<dim3((uint32_t)(p.groups * p.rows)), dim3(256), 0, stream>>>(a, p.rows);
+    return hipGetLastError();
+}
+
+}  // namespace dessert

@@ -1,0 +1,41 @@
+// What the kernels of the paged int8 cache share: the cache and the batch as they see them, a sequence's new tokens.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "cache_plans.hpp"
+#include "kernels.hpp"
+#include "number_formats.hpp"
+
+namespace dessert {
+
+constexpr uint32_t NO_PAGE = 0xFFFFFFFFu;
+
+// A sequence's new tokens: rows first .. first + count, at positions begin .. begin + count (negative ones are nowhere).
+struct NewTokens {
+    uint32_t first, count;
+    int32_t begin;
+};
+
+__device__ inline NewTokens new_tokens(const CacheBatch& b, uint32_t s) {
+    NewTokens n;
+    if (b.starts) {
+        const uint32_t lo = b.starts[s], hi = b.starts[s + 1];
+        n.first = min(lo, b.n_tokens);
+        n.count = min(hi > lo ? hi - lo : 0u, min(b.n_tokens - n.first, b.max_tokens));
+    } else {
+        n.first = s;
+        n.count = 1;
+    }
+    n.begin = (int32_t)min(b.lengths[s], CACHE_MOST) - (int32_t)n.count;
+    return n;
+}
+
+// The page at a place of a sequence's table, or NO_PAGE: behind the table's end, or no number of this pool.
+__device__ inline uint32_t page_at(const CacheBatch& b, const uint32_t* table, uint32_t place, uint32_t n_pages) {
+    if (place >= b.table_pages) return NO_PAGE;
+    const uint32_t page = table[place];
+    return page < n_pages ? page : NO_PAGE;
+}
+
+}  // namespace dessert

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "cache_plans.hpp"
 #include "hash_riders.hpp"
 #include "row_plans.hpp"
 
@@ -298,5 +299,84 @@ hipError_t launch_head_rows(const HeadArgs& h, hipStream_t stream);
 hipError_t launch_head_lists(const HeadArgs& h, hipStream_t stream);
 hipError_t launch_head_groups(const HeadArgs& h, hipStream_t stream);
 hipError_t launch_head_best(const HeadArgs& h, hipStream_t stream);
+
+// ---- a paged cache of keys and values in int8 ----------------------------------------------------------------------------
+struct CachePages {
+    int8_t* k;           // [pages][heads][page tokens][dim]
+    int8_t* v;           // [pages][heads][dim][page tokens]
+    float* ks;           // [pages][heads]
+    float* vs;
+    int8_t* bounds;      // [pages][heads][2][dim] or nullptr
+    uint32_t n_pages, heads, page_tokens, shift, dim;   // page_tokens = 1 << shift
+};
+struct CacheBatch {
+    const uint32_t* tables;    // [seqs][table_pages]
+    const uint32_t* lengths;   // [seqs]
+    const uint32_t* starts;    // [seqs + 1] or nullptr: one new token a sequence
+    uint32_t n_seqs, table_pages, n_tokens, max_tokens;
+};
+// new tokens' keys and values of dtype, [heads][dim] side by side, tokens k_stride / v_stride elements apart
+hipError_t launch_cache_append(const CachePages& c, const CacheBatch& b, const void* k, uint64_t k_stride, const void* v, uint64_t v_stride,
+                               uint32_t dtype, hipStream_t stream);
+struct AttendArgs {
+    CachePages cache;
+    CacheBatch batch;
+    const void* q;             // [tokens][heads * group][dim], tokens q_stride apart
+    uint64_t q_stride;
+    uint32_t dtype, group, window, n_select;
+    const uint32_t* pages;     // [tokens][heads][n_select] places in the tables, or nullptr
+    float scale;
+    void* out;                 // [tokens][heads * group][dim]
+    float* lse;                // [tokens][heads * group] or nullptr
+    uint32_t parts, part_chunks, tiles;
+    float* part_out;           // [workgroups][parts][rows][dim]
+    float2* part_sums;         // [workgroups][parts][rows] maximum (in powers of two), sum
+};
+hipError_t launch_cache_attention(AttendArgs a, const AttendPlan& p, void* workspace, hipStream_t stream);
+struct SelectArgs {
+    CachePages cache;
+    CacheBatch batch;
+    const int8_t* q;           // [tokens * heads * group][dim]
+    const float* q_scales;
+    uint32_t group, n_select, n_first, n_last;
+    uint32_t* keys;            // [tokens][heads][table_pages], ordered as the scores are
+    uint32_t* out;             // [tokens][heads][n_select]
+};
+hipError_t launch_cache_select(const SelectArgs& a, hipStream_t stream);
+// Layers whose pages go together; more of them go in several launches.
+constexpr uint32_t CACHE_LAYERS = 32;
+struct CacheLayers {
+    int8_t* k[CACHE_LAYERS];
+    int8_t* v[CACHE_LAYERS];
+    float* ks[CACHE_LAYERS];
+    float* vs[CACHE_LAYERS];
+    int8_t* bounds[CACHE_LAYERS];
+    uint32_t n;
+};
+struct PagesArgs {
+    const CachePages* layers;  // host, [n_layers]
+    uint32_t n_layers;
+    uint32_t* refs;            // [pages]
+    uint32_t* tables;          // [seqs][table_pages]
+    const uint32_t* lengths;   // [seqs]
+    uint32_t n_seqs, table_pages;
+};
+struct AdvanceArgs {
+    PagesArgs p;
+    const uint32_t* parents;   // [n_new] or nullptr
+    const uint32_t* add;       // [n_new]
+    uint32_t n_new;
+    bool counts;               // tables change hands: false where each sequence goes on
+    uint32_t* out_tables;      // [n_new][table_pages]
+    uint32_t* out_lengths;     // [n_new]
+    uint32_t* status;          // [2]
+};
+hipError_t launch_cache_advance(const AdvanceArgs& a, void* workspace, hipStream_t stream);
+struct CompactArgs {
+    PagesArgs p;
+    uint32_t* numbers;         // [pages]
+    uint32_t* live;            // [1]
+};
+hipError_t launch_cache_compact(const CompactArgs& a, void* workspace, hipStream_t stream);
 
 }  // namespace dessert
