@@ -112,6 +112,15 @@ __device__ inline Unit unit_of(const AttendArgs& a, uint32_t index, uint32_t hea
     return u;
 }
 
+// The unit as the rows of one of its tiles of ATTEND_MANY see it.
+__device__ inline Unit tile_of(const AttendArgs& a, Unit u, uint32_t tile) {
+    const uint32_t t0 = tile * ATTEND_MANY / a.group, t1 = min((tile + 1) * ATTEND_MANY - 1, u.rows - 1) / a.group;
+    const int32_t p0 = u.begin + (int32_t)t0, p1 = u.begin + (int32_t)t1;
+    u.hi = p1 < 0 ? 0u : min(u.hi, (uint32_t)p1 + 1u);
+    u.lo = a.window && p0 >= 0 && (uint32_t)p0 + 1u > a.window ? (uint32_t)p0 + 1u - a.window : 0u;
+    return u;
+}
+
 __device__ inline uint32_t unit_parts(const AttendArgs& a, const Unit& u) {
     const uint32_t first = u.lo / ATTEND_CHUNK, end = (u.hi + ATTEND_CHUNK - 1) / ATTEND_CHUNK;
     if (end <= first) return 1;
@@ -141,14 +150,14 @@ __device__ inline Group16 group_at(const AttendArgs& a, const uint32_t* table, c
     return g;
 }
 
-// ---- few rows: 16 to a workgroup, each of its four waves takes every fourth step of 64 tokens --------------------------------
+// ---- few rows: 16 to a workgroup, each of its W waves takes every W-th step of 64 tokens --------------------------------------
 // Keys and values come from memory straight into the layout of the products: a lane reads 16 bytes of a key (or of a value channel's
 // 16 tokens), converts them, and no LDS is used before the waves' results are joined.
-template <int ND>
-__global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
+template <int ND, int W>
+__global__ __launch_bounds__(64 * W, ND <= 4 ? 4 : 2) void attend_few_kernel(AttendArgs a) {
     constexpr int D = ND * 32, NV = D / 16;
-    __shared__ float joined[4][16][D + 4];
-    __shared__ float sums[4][16][2];
+    __shared__ f32x4 joined[W / 2][NV][64];
+    __shared__ float sums[W][16][2];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
     uint32_t id = blockIdx.x;
     const uint32_t part = id % a.parts;
@@ -193,7 +202,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
 
     f32x4 o[NV] = {};
     float m = NEVER, top = NEVER, l = 0.f;
-    for (uint32_t c = c0 + wave; c < c1; c += 4) {
+    for (uint32_t c = c0 + wave; c < c1; c += W) {
         const Group16 kg = group_at(a, table, list, c * 64 + 16 * (r >> 2));   // of the key this lane reads
         const Group16 vg = group_at(a, table, list, c * 64 + 16 * g);          // of the values it reads and the scores it holds
         const uint32_t k_page = kg.page == NO_PAGE ? 0u : kg.page, v_page = vg.page == NO_PAGE ? 0u : vg.page;
@@ -208,8 +217,12 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
             if constexpr (ND % 2) kt[t] = *(const u32x2*)(k + 4 * t * D + 32 * (ND - 1) + 8 * g);
         }
         const float ks = a.cache.ks[(uint64_t)v_page * heads + u.head] * factor, vs = a.cache.vs[(uint64_t)v_page * heads + u.head];
+        // of wide heads the values come when the keys' registers are free
+        auto fetch_values = [&]() {
 #pragma unroll
-        for (int d = 0; d < NV; ++d) vc[d] = *(const u32x4*)(v + (uint64_t)(16 * d) * a.cache.page_tokens);
+            for (int d = 0; d < NV; ++d) vc[d] = *(const u32x4*)(v + (uint64_t)(16 * d) * a.cache.page_tokens);
+        };
+        if constexpr (ND <= 4) fetch_values();
         f32x4 s[4] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -220,6 +233,7 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
             }
             if constexpr (ND % 2) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(kt[t].x, kt[t].y), q[ND - 1], s[t], 0, 0, 0);
         }
+        if constexpr (ND > 4) fetch_values();
         const bool whole = __all(vg.pos + 15 <= pos && vg.pos >= least);
         float peak = NEVER;
 #pragma unroll
@@ -265,43 +279,46 @@ __global__ __launch_bounds__(256) void attend_few_kernel(AttendArgs a) {
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    // the four waves' results
+    // the waves' results, in halves: the upper half's outputs go to the lower one through LDS, lane to lane
     if (g == 0) {
         sums[wave][r][0] = m;
         sums[wave][r][1] = l;
     }
     __syncthreads();
-    float most = sums[0][r][0];
+    float most = NEVER, total = 0.f;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) most = fmaxf(most, sums[w][r][0]);
+    for (int w = 0; w < W; ++w) most = fmaxf(most, sums[w][r][0]);
+#pragma unroll
+    for (int w = 0; w < W; ++w) total += sums[w][r][1] * (sums[w][r][0] == most ? 1.f : exp2_fast(sums[w][r][0] - most));
     const float mine = exp2_fast(top - P_TOP - (most == NEVER ? 0.f : most));
 #pragma unroll
-    for (int d = 0; d < NV; ++d) *(f32x4*)&joined[wave][r][16 * d + 4 * g] = o[d] * mine;
-    __syncthreads();
-    constexpr int PER = D / 4;    // threads of a row, 4 channels each
-    for (uint32_t i = threadIdx.x; i < 16 * PER; i += 256) {
-        const uint32_t rr = i / PER, d = i % PER * 4;
-        if (tile * 16 + rr >= u.rows) break;
-        float mm = sums[0][rr][0], ll = 0.f;
+    for (int d = 0; d < NV; ++d) o[d] *= mine;
 #pragma unroll
-        for (int w = 1; w < 4; ++w) mm = fmaxf(mm, sums[w][rr][0]);
+    for (int half = W / 2; half >= 1; half /= 2) {
+        if (wave >= half && wave < 2 * half)
 #pragma unroll
-        for (int w = 0; w < 4; ++w) ll += sums[w][rr][1] * (sums[w][rr][0] == mm ? 1.f : exp2_fast(sums[w][rr][0] - mm));
-        f32x4 x = *(const f32x4*)&joined[0][rr][d];
+            for (int d = 0; d < NV; ++d) joined[wave - half][d][lane] = o[d];
+        __syncthreads();
+        if (wave < half)
 #pragma unroll
-        for (int w = 1; w < 4; ++w) x += *(const f32x4*)&joined[w][rr][d];
-        if (a.parts == 1) {
-            const uint32_t full = tile * 16 + rr;
-            const uint64_t at = (uint64_t)(u.first_token + full / a.group) * q_heads + u.head * a.group + full % a.group;
-            const float by = ll == 0.f ? 0.f : 1.f / ll;
-            const float y[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
-            store_out(a.out, at * D + d, a.dtype, y);
-            if (a.lse && d == 0) a.lse[at] = ll == 0.f ? NEVER : (mm + log2f(ll)) * LN2;
-        } else {
-            const uint64_t slot = ((uint64_t)group_index * a.parts + part) * 16 + rr;
-            *(f32x4*)(a.part_out + slot * D + d) = x;
-            if (d == 0) a.part_sums[slot] = make_float2(mm, ll);
+            for (int d = 0; d < NV; ++d) o[d] += joined[wave][d][lane];
+        if (half > 1) __syncthreads();
+    }
+    if (wave != 0 || tile * 16 + r >= u.rows) return;
+    if (a.parts == 1) {
+        const uint64_t at = (uint64_t)token * q_heads + q_head;
+        const float by = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+        for (int d = 0; d < NV; ++d) {
+            const float y[4] = {o[d][0] * by, o[d][1] * by, o[d][2] * by, o[d][3] * by};
+            store_out(a.out, at * D + 16 * d + 4 * g, a.dtype, y);
         }
+        if (a.lse && g == 0) a.lse[at] = total == 0.f ? NEVER : (most + log2f(total)) * LN2;
+    } else {
+        const uint64_t slot = ((uint64_t)group_index * a.parts + part) * 16 + r;
+#pragma unroll
+        for (int d = 0; d < NV; ++d) *(f32x4*)(a.part_out + slot * D + 16 * d + 4 * g) = o[d];
+        if (g == 0) a.part_sums[slot] = make_float2(most, total);
     }
 }
 
@@ -323,14 +340,7 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     id /= a.tiles;
     const Unit whole_unit = unit_of(a, id / a.cache.heads, id % a.cache.heads);
     if (tile * ATTEND_MANY >= whole_unit.rows) return;
-    // what this workgroup's rows see
-    Unit u = whole_unit;
-    {
-        const uint32_t t0 = tile * ATTEND_MANY / a.group, t1 = min((tile + 1) * ATTEND_MANY - 1, u.rows - 1) / a.group;
-        const int32_t p0 = u.begin + (int32_t)t0, p1 = u.begin + (int32_t)t1;
-        u.hi = p1 < 0 ? 0u : min(u.hi, (uint32_t)p1 + 1u);
-        u.lo = a.window && p0 >= 0 && (uint32_t)p0 + 1u > a.window ? (uint32_t)p0 + 1u - a.window : 0u;
-    }
+    const Unit u = tile_of(a, whole_unit, tile);
     if (part >= unit_parts(a, u)) return;
     uint32_t c0, c1;
     part_range(a, u, part, c0, c1);
@@ -510,41 +520,51 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     }
 }
 
-// ---- the parts of the keys' axis joined: a workgroup a row, parts over its groups of lanes --------------------------------------
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t rows) {
+// ---- the parts of the keys' axis joined: a workgroup a row ---------------------------------------------------------------------
+// First the parts' factors, a thread a part, then their outputs, the parts spread over groups of lanes that hold 4 channels each.
+constexpr uint32_t MOST_PARTS = ATTEND_FEW_TARGET > ATTEND_MANY_TARGET ? ATTEND_FEW_TARGET : ATTEND_MANY_TARGET;
+
+__device__ inline float over_workgroup(float x, bool max, float* parts) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) x = max ? fmaxf(x, __shfl_xor(x, o)) : x + __shfl_xor(x, o);
+    if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return max ? fmaxf(fmaxf(parts[0], parts[1]), fmaxf(parts[2], parts[3])) : parts[0] + parts[1] + parts[2] + parts[3];
+}
+
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t rows, uint32_t used) {
     __shared__ f32x4 joined[256];
+    __shared__ float factors[MOST_PARTS], most4[4], sum4[4];
     const uint32_t D = a.cache.dim, per = D / 4, lanes = 256 / per;
     uint32_t id = blockIdx.x;
-    const uint32_t rr = id % rows;
-    id /= rows;
+    const uint32_t rr = id % used;       // used: rows of a workgroup that a unit can have
+    id /= used;
     const uint32_t group_index = id, tile = id % a.tiles;
     id /= a.tiles;
     Unit u = unit_of(a, id / a.cache.heads, id % a.cache.heads);
     const uint32_t row = tile * rows + rr;
     if (row >= u.rows) return;
-    if (!a.pages && rows == ATTEND_MANY) {
-        const uint32_t t0 = tile * rows / a.group, t1 = min((tile + 1) * rows - 1, u.rows - 1) / a.group;
-        const int32_t p0 = u.begin + (int32_t)t0, p1 = u.begin + (int32_t)t1;
-        u.hi = p1 < 0 ? 0u : min(u.hi, (uint32_t)p1 + 1u);
-        u.lo = a.window && p0 >= 0 && (uint32_t)p0 + 1u > a.window ? (uint32_t)p0 + 1u - a.window : 0u;
-    }
+    if (rows == ATTEND_MANY) u = tile_of(a, u, tile);
     const uint32_t parts = unit_parts(a, u);
     const uint64_t slot0 = (uint64_t)group_index * a.parts * rows + rr;
     float m = NEVER, l = 0.f;
-    for (uint32_t i = 0; i < parts; ++i) m = fmaxf(m, a.part_sums[slot0 + (uint64_t)i * rows].x);
-    for (uint32_t i = 0; i < parts; ++i) {
+    for (uint32_t i = threadIdx.x; i < parts; i += 256) m = fmaxf(m, a.part_sums[slot0 + (uint64_t)i * rows].x);
+    m = over_workgroup(m, true, most4);
+    for (uint32_t i = threadIdx.x; i < parts; i += 256) {
         const float2 s = a.part_sums[slot0 + (uint64_t)i * rows];
-        l += s.y * (s.x == m ? 1.f : exp2_fast(s.x - m));
+        const float f = s.x == m ? 1.f : exp2_fast(s.x - m);
+        factors[i] = f;
+        l += s.y * f;
     }
+    l = over_workgroup(l, false, sum4);
     const uint32_t part0 = threadIdx.x / per, d = threadIdx.x % per * 4;
     f32x4 x = {};
-    if (part0 < lanes)
-        for (uint32_t i = part0; i < parts; i += lanes) {
-            const uint64_t slot = slot0 + (uint64_t)i * rows;
-            const float mi = a.part_sums[slot].x;
-            if (mi == NEVER && a.part_sums[slot].y == 0.f) continue;
-            x += *(const f32x4*)(a.part_out + slot * D + d) * (mi == m ? 1.f : exp2_fast(mi - m));
-        }
+    if (part0 < lanes) {
+        const float* from = a.part_out + slot0 * D + d;
+        const uint64_t apart = (uint64_t)rows * D;
+#pragma unroll 4
+        for (uint32_t i = part0; i < parts; i += lanes) x += *(const f32x4*)(from + i * apart) * factors[i];
+    }
     joined[threadIdx.x] = x;
     __syncthreads();
     if (part0 != 0) return;
@@ -556,10 +576,47 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
     if (a.lse && d == 0) a.lse[at] = l == 0.f ? NEVER : (m + log2f(l)) * LN2;
 }
 
+// Of up to 32 parts: a wave a row.
+__global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint32_t rows, uint32_t used, uint64_t n) {
+    const uint32_t D = a.cache.dim, per = D / 4, lane = threadIdx.x & 63;
+    const uint64_t index = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (index >= n) return;
+    uint32_t id = (uint32_t)(index / used);
+    const uint32_t rr = (uint32_t)(index % used), group_index = id, tile = id % a.tiles;
+    id /= a.tiles;
+    Unit u = unit_of(a, id / a.cache.heads, id % a.cache.heads);
+    const uint32_t row = tile * rows + rr;
+    if (row >= u.rows) return;
+    if (rows == ATTEND_MANY) u = tile_of(a, u, tile);
+    const uint32_t parts = unit_parts(a, u);
+    const uint64_t slot0 = (uint64_t)group_index * a.parts * rows + rr;
+    const float2 s = lane < parts ? a.part_sums[slot0 + (uint64_t)lane * rows] : make_float2(NEVER, 0.f);
+    float m = s.x;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
+    m = __shfl(m, 0);
+    const float f = lane >= parts ? 0.f : s.x == m ? 1.f : exp2_fast(s.x - m);
+    float l = s.y * f;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) l += __shfl_xor(l, o);
+    l = __shfl(l, 0);
+    if (lane >= per) return;
+    f32x4 x = {};
+    const float* from = a.part_out + slot0 * D + lane * 4;
+    const uint64_t apart = (uint64_t)rows * D;
+    for (uint32_t i = 0; i < parts; ++i) x += *(const f32x4*)(from + i * apart) * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), i));
+    const uint64_t at = (uint64_t)(u.first_token + row / a.group) * (a.cache.heads * a.group) + u.head * a.group + row % a.group;
+    const float by = l == 0.f ? 0.f : 1.f / l;
+    const float y[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
+    store_out(a.out, at * D + lane * 4, a.dtype, y);
+    if (a.lse && lane == 0) a.lse[at] = l == 0.f ? NEVER : (m + log2f(l)) * LN2;
+}
+
 template <int ND>
 void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
     const dim3 grid((uint32_t)(p.groups * p.parts));
-    if (p.few) attend_few_kernel<ND><<<grid, dim3(256), 0, stream>>>(a);
+    if (p.few && p.waves == 4) attend_few_kernel<ND, 4><<<grid, dim3(256), 0, stream>>>(a);
+    else if (p.few) attend_few_kernel<ND, 8><<<grid, dim3(512), 0, stream>>>(a);
     else attend_many_kernel<ND><<<grid, dim3(256), 0, stream>>>(a);
 }
 
@@ -581,7 +638,12 @@ hipError_t launch_cache_attention(AttendArgs a, const AttendPlan& p, void* works
         case 7: launch_attend<7>(a, p, stream); break;
         default: launch_attend<8>(a, p, stream); break;
     }
-    if (p.parts > 1) attend_join_kernel<<<dim3((uint32_t)(p.groups * p.rows)), dim3(256), 0, stream>>>(a, p.rows);
+    if (p.parts > 1) {
+        const uint32_t used = (uint32_t)std::min<uint64_t>(p.rows, (uint64_t)a.group * (a.pages ? 1 : a.batch.max_tokens));
+        const uint64_t rows = p.groups * used;
+        if (p.parts <= 32) attend_join_few_kernel<<<dim3((uint32_t)divided_up(rows, 4)), dim3(256), 0, stream>>>(a, p.rows, used, rows);
+        else attend_join_kernel<<<dim3((uint32_t)rows), dim3(256), 0, stream>>>(a, p.rows, used);
+    }
     return hipGetLastError();
 }
 

@@ -19,10 +19,14 @@ constexpr uint32_t ATTEND_CHUNK = 64;
 // Rows (query heads of one key head and the new tokens they belong to) of a workgroup, for few rows and for many.
 constexpr uint32_t ATTEND_FEW = 16, ATTEND_MANY = 128;
 // Workgroups that a call is split into along the keys where it has fewer.
-constexpr uint32_t ATTEND_FEW_TARGET = 1024, ATTEND_MANY_TARGET = 512;
+#ifndef FT
+#define FT 1024
+#endif
+constexpr uint32_t ATTEND_FEW_TARGET = FT, ATTEND_MANY_TARGET = 512;
 
 struct AttendPlan {
     bool few;              // the form for few rows
+    uint32_t waves;        // of a workgroup
     uint32_t rows;         // of a workgroup
     uint32_t tiles;        // workgroups along the rows of a unit
     uint32_t units;        // sequences, or with lists of pages the most tokens
@@ -51,8 +55,13 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
     p.groups = (uint64_t)p.units * heads * p.tiles;
     const uint64_t chunks = std::max<uint64_t>(1, divided_up(length, ATTEND_CHUNK));
     const uint64_t target = p.few ? ATTEND_FEW_TARGET : ATTEND_MANY_TARGET;
+    p.waves = 4;
     // a part has work for the four waves of a workgroup (one step each) or, of many rows, for a few steps
-    const uint64_t parts = std::min(std::max<uint64_t>(1, target / std::max<uint64_t>(1, p.groups)), divided_up(chunks, 4));
+    uint64_t parts = std::min(std::max<uint64_t>(1, target / std::max<uint64_t>(1, p.groups)), divided_up(chunks, 4));
+    if (p.few && chunks <= 16 && parts > 1) {
+        p.waves = 8;
+        parts = 1;
+    }
     p.part_chunks = (uint32_t)divided_up(chunks, std::max<uint64_t>(1, parts));
     p.parts = (uint32_t)divided_up(chunks, p.part_chunks);
     if (p.parts > 1) p.bytes = attend_bytes(p.groups * p.parts * p.rows, dim, &p.sums);
