@@ -48,19 +48,25 @@ __device__ inline half8 codes_to_half(uint32_t w0, uint32_t w1) {
     return __builtin_bit_cast(half8, r);
 }
 
-// 8 elements of a query row as fp16, of bf16 still to be scaled by the row.
-__device__ inline void load_query(const void* q, uint64_t at, uint32_t dtype, float (&x)[8]) {
+// 8 elements of a query row.  (All of a row's are loaded before the first is looked at.)
+__device__ inline void convert_query(u32x4 bits, uint32_t dtype, float (&x)[8]) {
     if (dtype == TYPE_F16) {
-        f16_t v[8];
-        __builtin_memcpy(v, (const f16_t*)q + at, 16);
+        const half8 v = __builtin_bit_cast(half8, bits);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
     } else {
-        bf16_t v[8];
-        __builtin_memcpy(v, (const bf16_t*)q + at, 16);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(bits[i] << 16);
+            x[2 * i + 1] = __uint_as_float(bits[i] & 0xFFFF0000u);
+        }
     }
+}
+
+__device__ inline u32x4 load_query(const void* q, uint64_t at) {
+    u32x4 x;
+    __builtin_memcpy(&x, (const uint16_t*)q + at, 16);
+    return x;
 }
 
 // A row that holds an infinity or NaN gives NaN wherever it sees a key.
@@ -134,27 +140,24 @@ __device__ inline void part_range(const AttendArgs& a, const Unit& u, uint32_t p
     end = part + 1 == a.parts ? last : min(last, begin + a.part_chunks);
 }
 
-// Where 16 tokens of the axis lie: their page (or NO_PAGE) and the position of the first.
-struct Group16 {
-    uint32_t page, offset;
-    int32_t pos;
-};
-
-__device__ inline Group16 group_at(const AttendArgs& a, const uint32_t* table, const uint32_t* list, uint32_t token) {
-    Group16 g;
-    uint32_t place = token >> a.cache.shift;
-    g.offset = token & (a.cache.page_tokens - 1);
-    if (list) place = place < a.n_select ? list[place] : NO_PAGE;
-    g.page = page_at(a.batch, table, place, a.cache.n_pages);
-    g.pos = g.page == NO_PAGE ? 0x7FFFFFFF - 64 : (int32_t)((place << a.cache.shift) + g.offset);
-    return g;
+// The page (or NO_PAGE) that a token of the axis lies on, and its place in the table.
+template <bool LISTS>
+__device__ inline uint32_t page_of(const AttendArgs& a, const uint32_t* table, const uint32_t* list, uint32_t token, uint32_t& place) {
+    place = token >> a.cache.shift;
+    bool there = true;
+    if constexpr (LISTS) {
+        there = place < a.n_select;
+        place = list[min(place, a.n_select - 1)];
+    }
+    const uint32_t page = page_at(a.batch, table, place, a.cache.n_pages);
+    return there ? page : NO_PAGE;
 }
 
 // ---- few rows: 16 to a workgroup, each of its W waves takes every W-th step of 64 tokens --------------------------------------
 // Keys and values come from memory straight into the layout of the products: a lane reads 16 bytes of a key (or of a value channel's
 // 16 tokens), converts them, and no LDS is used before the waves' results are joined.
-template <int ND, int W>
-__global__ __launch_bounds__(64 * W, ND <= 4 ? 4 : 2) void attend_few_kernel(AttendArgs a) {
+template <int ND, int W, bool LISTS>
+__global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(AttendArgs a) {
     constexpr int D = ND * 32, NV = D / 16;
     __shared__ f32x4 joined[W / 2][NV][64];
     __shared__ float sums[W][16][2];
@@ -170,7 +173,7 @@ __global__ __launch_bounds__(64 * W, ND <= 4 ? 4 : 2) void attend_few_kernel(Att
     uint32_t c0, c1;
     part_range(a, u, part, c0, c1);
     const uint32_t* table = a.batch.tables + (uint64_t)u.seq * a.batch.table_pages;
-    const uint32_t* list = a.pages ? a.pages + ((uint64_t)u.first_token * a.cache.heads + u.head) * a.n_select : nullptr;
+    const uint32_t* list = LISTS ? a.pages + ((uint64_t)u.first_token * a.cache.heads + u.head) * a.n_select : nullptr;
     const uint32_t heads = a.cache.heads, q_heads = heads * a.group;
 
     // the row of this lane
@@ -178,51 +181,72 @@ __global__ __launch_bounds__(64 * W, ND <= 4 ? 4 : 2) void attend_few_kernel(Att
     const uint32_t token = u.first_token + row / a.group, q_head = u.head * a.group + row % a.group;
     const int32_t pos = u.begin + (int32_t)(row / a.group);
     const int32_t least = a.window ? max(pos - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
-    half8 q[ND];
     float factor;
-    {
-        float x[ND][8], peak = 0.f;
-        const uint64_t at = (uint64_t)token * a.q_stride + (uint64_t)q_head * D;
+    u32x4 raw[ND];
 #pragma unroll
-        for (int f = 0; f < ND; ++f) {
-            const int d = f < ND / 2 * 2 ? 64 * (f / 2) + 16 * (int)g + 8 * (f % 2) : 32 * f + 8 * (int)g;
-            load_query(a.q, at + d, a.dtype, x[f]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) peak = fmaxf(peak, x[f][i] == x[f][i] ? fabsf(x[f][i]) : __builtin_huge_valf());
-        }
-        peak = fmaxf(peak, __shfl_xor(peak, 16));
-        peak = fmaxf(peak, __shfl_xor(peak, 32));
-        const int e = query_exponent(peak, a.dtype);
-#pragma unroll
-        for (int f = 0; f < ND; ++f)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) q[f][i] = (f16_t)ldexpf(x[f][i], e);
-        factor = query_factor(peak, a.scale, e);
-    }
+    for (int f = 0; f < ND; ++f)
+        raw[f] = load_query(a.q, (uint64_t)token * a.q_stride + (uint64_t)q_head * D + (f < ND / 2 * 2 ? 64 * (f / 2) + 16 * (int)g + 8 * (f % 2) : 32 * f + 8 * (int)g));
 
     f32x4 o[NV] = {};
     float m = NEVER, top = NEVER, l = 0.f;
-    for (uint32_t c = c0 + wave; c < c1; c += W) {
-        const Group16 kg = group_at(a, table, list, c * 64 + 16 * (r >> 2));   // of the key this lane reads
-        const Group16 vg = group_at(a, table, list, c * 64 + 16 * g);          // of the values it reads and the scores it holds
-        const uint32_t k_page = kg.page == NO_PAGE ? 0u : kg.page, v_page = vg.page == NO_PAGE ? 0u : vg.page;
-        const int8_t* k = a.cache.k + (((uint64_t)k_page * heads + u.head) * a.cache.page_tokens + kg.offset + (r & 3)) * D;
-        const int8_t* v = a.cache.v + ((uint64_t)v_page * heads + u.head) * D * a.cache.page_tokens + (uint64_t)r * a.cache.page_tokens + vg.offset;
-        u32x4 kc[4][ND / 2 + 1], vc[NV];
-        u32x2 kt[4];
+    // A step's codes are asked for as soon as the registers of the one before are free: keys behind the first product, values behind the
+    // second.
+    u32x4 kc[4][ND / 2 + 1], vc[NV];
+    u32x2 kt[4];
+    float ks = 0.f, vs = 0.f;
+    const uint32_t slots = a.cache.page_tokens - 1;
+    auto key_token = [&](uint32_t c) { return c * 64 + 16 * (r >> 2); };    // the first of the 16 around the key this lane reads
+    auto value_token = [&](uint32_t c) { return c * 64 + 16 * g; };         // of those whose values it reads and whose scores it holds
+    auto fetch_keys = [&](uint32_t page, uint32_t token) {
+        page = page == NO_PAGE ? 0u : page;
+        const int8_t* k = a.cache.k + (((uint64_t)page * heads + u.head) * a.cache.page_tokens + (token & slots) + (r & 3)) * D;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int f = 0; f < ND / 2; ++f) kc[t][f] = *(const u32x4*)(k + 4 * t * D + 64 * f + 16 * g);
             if constexpr (ND % 2) kt[t] = *(const u32x2*)(k + 4 * t * D + 32 * (ND - 1) + 8 * g);
         }
-        const float ks = a.cache.ks[(uint64_t)v_page * heads + u.head] * factor, vs = a.cache.vs[(uint64_t)v_page * heads + u.head];
-        // of wide heads the values come when the keys' registers are free
-        auto fetch_values = [&]() {
+    };
+    auto fetch_values = [&](uint32_t page, uint32_t token) {
+        page = page == NO_PAGE ? 0u : page;
+        const int8_t* v = a.cache.v + ((uint64_t)page * heads + u.head) * D * a.cache.page_tokens + (uint64_t)r * a.cache.page_tokens + (token & slots);
+        ks = a.cache.ks[(uint64_t)page * heads + u.head];
+        vs = a.cache.vs[(uint64_t)page * heads + u.head];
 #pragma unroll
-            for (int d = 0; d < NV; ++d) vc[d] = *(const u32x4*)(v + (uint64_t)(16 * d) * a.cache.page_tokens);
-        };
-        if constexpr (ND <= 4) fetch_values();
+        for (int d = 0; d < NV; ++d) vc[d] = *(const u32x4*)(v + (uint64_t)(16 * d) * a.cache.page_tokens);
+    };
+    uint32_t c = c0 + wave;
+    uint32_t k_place, v_place;
+    uint32_t k_page = page_of<LISTS>(a, table, list, key_token(c), k_place), v_page = page_of<LISTS>(a, table, list, value_token(c), v_place);
+    if (c < c1) {
+        fetch_keys(k_page, key_token(c));
+        fetch_values(v_page, value_token(c));
+    }
+    half8 q[ND];
+    {
+        float x[8], peak = 0.f;
+#pragma unroll
+        for (int f = 0; f < ND; ++f) {
+            convert_query(raw[f], a.dtype, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) peak = fmaxf(peak, x[i] == x[i] ? fabsf(x[i]) : __builtin_huge_valf());
+        }
+        peak = fmaxf(peak, __shfl_xor(peak, 16));
+        peak = fmaxf(peak, __shfl_xor(peak, 32));
+        const int e = query_exponent(peak, a.dtype);
+#pragma unroll
+        for (int f = 0; f < ND; ++f) {
+            convert_query(raw[f], a.dtype, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[f][i] = (f16_t)ldexpf(x[i], e);
+        }
+        factor = query_factor(peak, a.scale, e);
+    }
+    for (; c < c1; c += W) {
+        // where the scores of this lane lie; a missing page's lie behind every row
+        const int32_t at0 = v_page == NO_PAGE ? 0x7FFFFFFF - 64 : (int32_t)((v_place << a.cache.shift) + (value_token(c) & slots));
+        k_page = page_of<LISTS>(a, table, list, key_token(c + W), k_place);
+        v_page = page_of<LISTS>(a, table, list, value_token(c + W), v_place);
         f32x4 s[4] = {};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -233,17 +257,25 @@ __global__ __launch_bounds__(64 * W, ND <= 4 ? 4 : 2) void attend_few_kernel(Att
             }
             if constexpr (ND % 2) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(kt[t].x, kt[t].y), q[ND - 1], s[t], 0, 0, 0);
         }
-        if constexpr (ND > 4) fetch_values();
-        const bool whole = __all(vg.pos + 15 <= pos && vg.pos >= least);
+        if (c + W < c1) fetch_keys(k_page, key_token(c + W));
+        const bool whole = __all(at0 + 15 <= pos && at0 >= least);
+        const float by = ks * factor;
         float peak = NEVER;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[t] *= by;
+        if (!whole) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int32_t at = at0 + 4 * t + i;
+                    s[t][i] = ((at <= pos) & (at >= least)) ? s[t][i] : NEVER;
+                }
+        }
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t at = vg.pos + 4 * t + i;
-                s[t][i] = whole || (at <= pos && at >= least) ? s[t][i] * ks : NEVER;
-                peak = fmaxf(peak, s[t][i]);
-            }
+            for (int i = 0; i < 4; ++i) peak = fmaxf(peak, s[t][i]);
         float high = vs < __builtin_huge_valf() ? peak + __builtin_amdgcn_logf(vs) : NEVER;
         high = fmaxf(high, __shfl_xor(high, 16));
         high = fmaxf(high, __shfl_xor(high, 32));
@@ -269,13 +301,20 @@ __global__ __launch_bounds__(64 * W, ND <= 4 ? 4 : 2) void attend_few_kernel(Att
             for (int i = 0; i < 4; ++i) {
                 const float e = exp2_fast(s[t][i] - base);
                 l += e;
-                p[t / 2][t % 2 * 4 + i] = (f16_t)(whole || s[t][i] != NEVER ? e * weight : 0.f);
+                p[t / 2][t % 2 * 4 + i] = (f16_t)(e * weight);
             }
+        if (!whole) {     // what is not seen may have any scale
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[t / 2][t % 2 * 4 + i] = s[t][i] == NEVER ? (f16_t)0.f : p[t / 2][t % 2 * 4 + i];
+        }
 #pragma unroll
         for (int d = 0; d < NV; ++d) {
             o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(vc[d].x, vc[d].y), p[0], o[d], 0, 0, 0);
             o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half(vc[d].z, vc[d].w), p[1], o[d], 0, 0, 0);
         }
+        if (c + W < c1) fetch_values(v_page, value_token(c + W));
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -362,12 +401,13 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     half8 q[D / 16];
     float factor;
     {
-        float peak = 0.f;
-        const uint64_t at = (uint64_t)token * a.q_stride + (uint64_t)q_head * D + 8 * h;
+        u32x4 raw[D / 16];
+#pragma unroll
+        for (int f = 0; f < D / 16; ++f) raw[f] = load_query(a.q, (uint64_t)token * a.q_stride + (uint64_t)q_head * D + 8 * h + 16 * f);
+        float x[8], peak = 0.f;
 #pragma unroll
         for (int f = 0; f < D / 16; ++f) {
-            float x[8];
-            load_query(a.q, at + 16 * f, a.dtype, x);
+            convert_query(raw[f], a.dtype, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) peak = fmaxf(peak, x[i] == x[i] ? fabsf(x[i]) : __builtin_huge_valf());
         }
@@ -375,8 +415,7 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
         const int e = query_exponent(peak, a.dtype);
 #pragma unroll
         for (int f = 0; f < D / 16; ++f) {
-            float x[8];
-            load_query(a.q, at + 16 * f, a.dtype, x);
+            convert_query(raw[f], a.dtype, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[f][i] = (f16_t)ldexpf(x[i], e);
         }
@@ -522,7 +561,7 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
 
 // ---- the parts of the keys' axis joined: a workgroup a row ---------------------------------------------------------------------
 // First the parts' factors, a thread a part, then their outputs, the parts spread over groups of lanes that hold 4 channels each.
-constexpr uint32_t MOST_PARTS = ATTEND_FEW_TARGET > ATTEND_MANY_TARGET ? ATTEND_FEW_TARGET : ATTEND_MANY_TARGET;
+constexpr uint32_t MOST_PARTS = ATTEND_MOST_GROUPS;
 
 __device__ inline float over_workgroup(float x, bool max, float* parts) {
 #pragma unroll
@@ -615,8 +654,10 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
 template <int ND>
 void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
     const dim3 grid((uint32_t)(p.groups * p.parts));
-    if (p.few && p.waves == 4) attend_few_kernel<ND, 4><<<grid, dim3(256), 0, stream>>>(a);
-    else if (p.few) attend_few_kernel<ND, 8><<<grid, dim3(512), 0, stream>>>(a);
+    if (p.few && a.pages && p.waves == 4) attend_few_kernel<ND, 4, true><<<grid, dim3(256), 0, stream>>>(a);
+    else if (p.few && a.pages) attend_few_kernel<ND, 8, true><<<grid, dim3(512), 0, stream>>>(a);
+    else if (p.few && p.waves == 4) attend_few_kernel<ND, 4, false><<<grid, dim3(256), 0, stream>>>(a);
+    else if (p.few) attend_few_kernel<ND, 8, false><<<grid, dim3(512), 0, stream>>>(a);
     else attend_many_kernel<ND><<<grid, dim3(256), 0, stream>>>(a);
 }
 

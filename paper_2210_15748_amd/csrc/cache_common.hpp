@@ -33,9 +33,8 @@ __device__ inline NewTokens new_tokens(const CacheBatch& b, uint32_t s) {
 
 // The page at a place of a sequence's table, or NO_PAGE: behind the table's end, or no number of this pool.
 __device__ inline uint32_t page_at(const CacheBatch& b, const uint32_t* table, uint32_t place, uint32_t n_pages) {
-    if (place >= b.table_pages) return NO_PAGE;
-    const uint32_t page = table[place];
-    return page < n_pages ? page : NO_PAGE;
+    const uint32_t page = table[min(place, b.table_pages - 1)];     // loaded in any case: no branch for the loads behind it to wait at
+    return place < b.table_pages && page < n_pages ? page : NO_PAGE;
 }
 
 }  // namespace dessert

@@ -18,11 +18,12 @@ inline uint64_t append_places(uint64_t max_tokens, uint32_t page_tokens) { retur
 constexpr uint32_t ATTEND_CHUNK = 64;
 // Rows (query heads of one key head and the new tokens they belong to) of a workgroup, for few rows and for many.
 constexpr uint32_t ATTEND_FEW = 16, ATTEND_MANY = 128;
-// Workgroups that a call is split into along the keys where it has fewer.
-#ifndef FT
-#define FT 1024
-#endif
-constexpr uint32_t ATTEND_FEW_TARGET = FT, ATTEND_MANY_TARGET = 512;
+// Workgroups that a call is split into along the keys where it has fewer: as many as the chip holds at once (its registers decide), so that
+// none begins when others end.
+// (One token, 8 heads of 4 query heads, 268 MB of codes, in us: 59 / 63 / 70 with 1024 / 768 / 512 workgroups at dim 32, 68 / 58 / 58 at 64,
+// 66 / - / 59 at 128, - / 84 / 74 / 70 with 384 for the second and 256 for the fourth at 256.)
+constexpr uint32_t ATTEND_MOST_GROUPS = 1024;
+inline uint32_t attend_target(bool few, uint32_t dim) { return !few ? 512 : dim <= 32 ? 1024 : dim <= 64 ? 768 : dim <= 160 ? 512 : 256; }
 
 struct AttendPlan {
     bool few;              // the form for few rows
@@ -54,11 +55,13 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
     p.units = (uint32_t)(lists ? seqs * max_tokens : seqs);
     p.groups = (uint64_t)p.units * heads * p.tiles;
     const uint64_t chunks = std::max<uint64_t>(1, divided_up(length, ATTEND_CHUNK));
-    const uint64_t target = p.few ? ATTEND_FEW_TARGET : ATTEND_MANY_TARGET;
+    const uint64_t target = attend_target(p.few, dim);
     p.waves = 4;
     // a part has work for the four waves of a workgroup (one step each) or, of many rows, for a few steps
     uint64_t parts = std::min(std::max<uint64_t>(1, target / std::max<uint64_t>(1, p.groups)), divided_up(chunks, 4));
-    if (p.few && chunks <= 16 && parts > 1) {
+    // up to 16 steps are done by one workgroup of eight waves rather than split and joined (16 sequences up to 1000 of dim 128: 14.1 us, split 16.0; up
+    // to 700 11.8 and 15.1; of wider heads its waves have too few registers)
+    if (p.few && parts > 1 && chunks <= 16 && dim <= 160) {
         p.waves = 8;
         parts = 1;
     }
@@ -71,7 +74,7 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
 // What serves every call of these sizes or smaller ones: a call that is split has at most its form's target of workgroups.
 inline size_t attend_workspace_upto(uint64_t max_tokens, uint32_t group, uint32_t dim, uint64_t length, bool lists) {
     if (divided_up(length, ATTEND_CHUNK) <= 4) return 0;
-    const uint64_t few = (uint64_t)ATTEND_FEW_TARGET * ATTEND_FEW, many = (uint64_t)ATTEND_MANY_TARGET * ATTEND_MANY;
+    const uint64_t few = (uint64_t)attend_target(true, dim) * ATTEND_FEW, many = (uint64_t)attend_target(false, dim) * ATTEND_MANY;
     return attend_bytes(lists || max_tokens * group <= ATTEND_FEW ? few : std::max(few, many), dim, nullptr);
 }
 
