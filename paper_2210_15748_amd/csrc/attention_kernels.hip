@@ -639,11 +639,28 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) l += __shfl_xor(l, o);
     l = __shfl(l, 0);
-    if (lane >= per) return;
+    // of heads of up to 128 channels each half of the wave sees to every other part
+    const uint32_t halves = per <= 32 ? 2 : 1, half = halves == 2 ? lane >> 5 : 0, at4 = halves == 2 ? lane & 31 : lane;
     f32x4 x = {};
-    const float* from = a.part_out + slot0 * D + lane * 4;
+    const float* from = a.part_out + slot0 * D + min(at4, per - 1) * 4;
     const uint64_t apart = (uint64_t)rows * D;
-    for (uint32_t i = 0; i < parts; ++i) x += *(const f32x4*)(from + i * apart) * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), i));
+    for (uint32_t i0 = 0; i0 < parts; i0 += 8) {
+        f32x4 v[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (j < 8 / halves) v[j] = *(const f32x4*)(from + min(i0 + j * halves + half, parts - 1) * apart);
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+            if (j < 8 / halves) {
+                const uint32_t i = i0 + j * halves + half;
+                const float by = __shfl(f, i & 63);
+                if (i < parts) x += v[j] * by;
+            }
+    }
+    if (halves == 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += __shfl_xor(x[i], 32);
+    if (half || at4 >= per) return;
     const uint64_t at = (uint64_t)(u.first_token + row / a.group) * (a.cache.heads * a.group) + u.head * a.group + row % a.group;
     const float by = l == 0.f ? 0.f : 1.f / l;
     const float y[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
@@ -654,10 +671,15 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
 template <int ND>
 void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
     const dim3 grid((uint32_t)(p.groups * p.parts));
-    if (p.few && a.pages && p.waves == 4) attend_few_kernel<ND, 4, true><<<grid, dim3(256), 0, stream>>>(a);
-    else if (p.few && a.pages) attend_few_kernel<ND, 8, true><<<grid, dim3(512), 0, stream>>>(a);
-    else if (p.few && p.waves == 4) attend_few_kernel<ND, 4, false><<<grid, dim3(256), 0, stream>>>(a);
-    else if (p.few) attend_few_kernel<ND, 8, false><<<grid, dim3(512), 0, stream>>>(a);
+    if (p.few && p.waves == 4) {
+        if (a.pages) attend_few_kernel<ND, 4, true><<<grid, dim3(256), 0, stream>>>(a);
+        else attend_few_kernel<ND, 4, false><<<grid, dim3(256), 0, stream>>>(a);
+    } else if (p.few) {
+        if constexpr (ND <= 5) {
+            if (a.pages) attend_few_kernel<ND, 8, true><<<grid, dim3(512), 0, stream>>>(a);
+            else attend_few_kernel<ND, 8, false><<<grid, dim3(512), 0, stream>>>(a);
+        }
+    }
     else attend_many_kernel<ND><<<grid, dim3(256), 0, stream>>>(a);
 }
 
