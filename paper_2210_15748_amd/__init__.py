@@ -660,7 +660,7 @@ class Cache:
         self.k_codes, self.v_codes, self.k_scales, self.v_scales, self.bounds = tensors
         self.struct = struct
         self.n_pages, self.n_heads, self.page_tokens, self.dim = struct.n_pages, struct.n_heads, struct.page_tokens, struct.dim
-        self.address = C.addressof(struct)
+        self.address, self.raw = C.addressof(struct), bytes(struct)
 
 
 class CacheBatch:
@@ -800,17 +800,36 @@ def cache_select(ix: Index, cache: Cache, batch: CacheBatch, q_codes: torch.Tens
 
 
 def _layers(caches):
-    """(array of dessert_cache_t, its length)"""
-    caches = [caches] if isinstance(caches, Cache) else list(caches)
-    if not caches:
+    """(dessert_cache_t of each layer side by side, how many, pages)"""
+    if isinstance(caches, Cache):
+        return caches.raw, 1, caches.n_pages
+    raw = [c.raw for c in caches]
+    if not raw:
         raise ValueError("no layers")
-    return (_CacheStruct * len(caches))(*(c.struct for c in caches)), len(caches)
+    return b"".join(raw), len(raw), caches[0].n_pages
 
 
-def _page_outputs(ix: Index, outs, shapes, made, dtypes=_TOKEN_TYPES):
-    o = (None,) * len(shapes) if outs is None else outs
-    return tuple(_output(ix, t, shape, f"outs[{i}]", made, t.dtype if t is not None and t.dtype in dtypes else torch.int32)
-                 for i, (t, shape) in enumerate(zip(o, shapes)))
+def _numbers(ix: Index, t: torch.Tensor, n: Optional[int], name: str) -> int:
+    """The address of a vector of 32-bit numbers that a call reads or writes where it lies (n = None: of any length)."""
+    shape = t.shape
+    if len(shape) != 1 or (n is not None and shape[0] != n) or t.dtype not in _TOKEN_TYPES or t.device != ix.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{'any' if n is None else n}] on {ix.device} of dtype int32 / uint32")
+    return t.data_ptr()
+
+
+def _tables(ix: Index, tables: torch.Tensor, lengths: torch.Tensor):
+    """(address of tables, of lengths, sequences, width)"""
+    shape = tables.shape
+    if len(shape) != 2 or tables.dtype not in _TOKEN_TYPES or tables.device != ix.device or not tables.is_contiguous():
+        raise ValueError(f"tables must be a contiguous matrix on {ix.device} of dtype int32 / uint32")
+    n, width = shape
+    if n > _MOST or width > _MOST:
+        raise ValueError(f"tables of {n} rows of {width}, at most 2^31 - 1 of each are taken")
+    return tables.data_ptr(), _numbers(ix, lengths, n, "lengths"), n, width
+
+
+def _page_output(ix: Index, t: Optional[torch.Tensor], shape, name: str, made) -> torch.Tensor:
+    return _output(ix, t, shape, name, made, torch.uint32 if t is not None and t.dtype == torch.uint32 else torch.int32)
 
 
 def cache_advance_workspace_bytes(ix: Index, n_pages: int, n_new: int) -> int:
@@ -823,21 +842,19 @@ def cache_advance(ix: Index, caches, refs: torch.Tensor, tables: torch.Tensor, l
     seqs] (-1: none) or None, all int32 / uint32.  Returns (tables [new seqs, table pages], lengths [new seqs], status [2]: free
     pages, sequences without room); ``outs``: the three tensors to write, apart from the old ones."""
     made = []
-    layers, n_layers = _layers(caches)
-    pages = layers[0].n_pages
-    r_ptr = _kept(ix, refs, (pages,), "refs", _TOKEN_TYPES)
-    t_ptr = _kept(ix, tables, (None, None), "tables", _TOKEN_TYPES)
-    n, width = tables.shape
-    l_ptr = _kept(ix, lengths, (n,), "lengths", _TOKEN_TYPES)
-    a_ptr = _kept(ix, add, (None,), "add", _TOKEN_TYPES)
+    layers, n_layers, pages = _layers(caches)
+    r_ptr = _numbers(ix, refs, pages, "refs")
+    t_ptr, l_ptr, n, width = _tables(ix, tables, lengths)
+    a_ptr = _numbers(ix, add, None, "add")
     new = add.shape[0]
-    p_ptr = None if parents is None else _kept(ix, parents, (new,), "parents", _TOKEN_TYPES)
-    o = _page_outputs(ix, outs, ((new, width), (new,), (2,)), made)
+    p_ptr = None if parents is None else _numbers(ix, parents, new, "parents")
+    o = (None, None, None) if outs is None else outs
+    o = (_page_output(ix, o[0], (new, width), "outs[0]", made), _page_output(ix, o[1], (new,), "outs[1]", made),
+         _page_output(ix, o[2], (2,), "outs[2]", made))
     ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_advance_workspace_bytes, pages, new)
     _lend(ix, made)
-    _check(lib().dessert_cache_advance(ix.handle, C.addressof(layers), n_layers, r_ptr, t_ptr, _size(width, "the tables' width"), l_ptr,
-                                       _size(n, "the number of sequences"), p_ptr, a_ptr, _size(new, "the number of sequences"), ws_ptr, ws_bytes,
-                                       *map(_ptr, o)))
+    _check(lib().dessert_cache_advance(ix.handle, layers, n_layers, r_ptr, t_ptr, width, l_ptr, n, p_ptr, a_ptr, _size(new, "the number of sequences"),
+                                       ws_ptr, ws_bytes, o[0].data_ptr(), o[1].data_ptr(), o[2].data_ptr()))
     return o
 
 
@@ -850,17 +867,15 @@ def cache_compact(ix: Index, caches, refs: torch.Tensor, tables: torch.Tensor, l
     """dessert_cache_compact: caches as for cache_advance, refs [pages] and tables [seqs, table pages] (both changed), lengths [seqs], all int32 / uint32.
     Returns (new numbers [pages], pages in use [1])."""
     made = []
-    layers, n_layers = _layers(caches)
-    pages = layers[0].n_pages
-    r_ptr = _kept(ix, refs, (pages,), "refs", _TOKEN_TYPES)
-    t_ptr = _kept(ix, tables, (None, None), "tables", _TOKEN_TYPES)
-    n, width = tables.shape
-    l_ptr = _kept(ix, lengths, (n,), "lengths", _TOKEN_TYPES)
-    o = _page_outputs(ix, outs, ((pages,), (1,)), made)
+    layers, n_layers, pages = _layers(caches)
+    r_ptr = _numbers(ix, refs, pages, "refs")
+    t_ptr, l_ptr, n, width = _tables(ix, tables, lengths)
+    o = (None, None) if outs is None else outs
+    o = (_page_output(ix, o[0], (pages,), "outs[0]", made), _page_output(ix, o[1], (1,), "outs[1]", made))
     ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_compact_workspace_bytes, pages)
     _lend(ix, made)
-    _check(lib().dessert_cache_compact(ix.handle, C.addressof(layers), n_layers, r_ptr, t_ptr, _size(width, "the tables' width"), l_ptr,
-                                       _size(n, "the number of sequences"), ws_ptr, ws_bytes, *map(_ptr, o)))
+    _check(lib().dessert_cache_compact(ix.handle, layers, n_layers, r_ptr, t_ptr, width, l_ptr, n, ws_ptr, ws_bytes, o[0].data_ptr(),
+                                       o[1].data_ptr()))
     return o
 
 

@@ -1696,7 +1696,7 @@ dessert_status_t dessert_cache_advance(const dessert_index_t* ix, const dessert_
     if (n_new && n_seqs && (overlap(tables_dev, 4ull * n_seqs * table_pages, out_tables_dev, 4ull * n_new * table_pages) ||
                             overlap(lengths_dev, 4ull * n_seqs, out_lengths_dev, 4ull * n_new)))
         return fail(DESSERT_EINVAL, "out_tables_dev and out_lengths_dev must lie apart from what they are made of");
-    if (n_new > CACHE_MOST || (uint64_t)n_new * divided_up((uint64_t)pages[0].heads * pages[0].page_tokens * pages[0].dim, 8192) > MAX_WORKGROUPS)
+    if (n_new > CACHE_MOST || (uint64_t)n_new * table_pages > 0xFFFFFFFFull || (uint64_t)n_new * divided_up((uint64_t)pages[0].heads * pages[0].page_tokens * pages[0].dim, 8192) > MAX_WORKGROUPS)
         return fail(DESSERT_EINVAL, "too many sequences for one call");
     st = check_workspace(workspace_dev, workspace_bytes, advance_plan(pages[0].n_pages, n_new).bytes);
     if (st != DESSERT_OK) return st;

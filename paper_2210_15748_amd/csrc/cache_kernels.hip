@@ -550,13 +550,11 @@ void launch_select(const SelectArgs& a, hipStream_t stream) {
 template <typename T>
 void launch_append(const CachePages& c, const CacheBatch& b, const T* k, uint64_t k_stride, const T* v, uint64_t v_stride, hipStream_t stream) {
     const uint32_t places = (uint32_t)append_places(b.max_tokens, c.page_tokens);
-    // waves: as many as see to the new slots of a page in one round, four at most; enough for rounds of 16 slots; four where the chip has room for
-    // them all, as they share the earlier codes of a page whose scale rises
+    // waves: as many as see to the new slots of a page in one round, four at most; enough for rounds of 16 slots
     const uint32_t per = c.dim / 8, slots = std::min<uint64_t>(c.page_tokens, std::max<uint64_t>(16, (uint64_t)b.max_tokens + 15));
     uint32_t waves = 1;
     while (waves < 4 && 4 * (64 * waves / per & ~3u) < std::max(16u, slots)) waves *= 2;
     const uint64_t units = (uint64_t)b.n_seqs * places * c.heads * 2;
-    if (units <= 1024) waves = 4;
     in_launches(units, 1, 256, [&](uint64_t first, uint64_t, uint32_t workgroups) {
         const dim3 grid(workgroups);
         if (waves == 1) append_kernel<T, 1><<<grid, dim3(64), 0, stream>>>(c, b, k, k_stride, v, v_stride, places, first);
