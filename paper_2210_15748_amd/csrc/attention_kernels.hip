@@ -23,13 +23,25 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr float NEVER = -__builtin_huge_valf();
-constexpr float P_TOP = 12.f;      // the largest of P so far is 2^12
+// What products (at most 2^31) are multiplied by is at least this, which changes no score by more than 2^-29: -inf, where a key is not seen, stays that.
+constexpr float LEAST_SCALE = 0x1p-60f;
+constexpr float P_TOP = 12.f;      // the largest of P so far is 2^12,
+constexpr float SLACK = 3.f;       // or of many rows up to 2^15
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// In a branch: keeps the compiler from working it out for all and choosing afterwards.
+__device__ inline void rarely() { asm volatile("; seldom"); }
 
 // What e^(s - m) is multiplied by to be a part of P.  (The exponent passes 120 only with scales that are 2^100 apart.)
 __device__ inline float p_factor(float vs, float m, float top) {
     return vs * exp2_fast(fminf((m == NEVER ? 0.f : m) - (top == NEVER ? 0.f : top) + P_TOP, 120.f));
+}
+
+// The larger of a lane's and the one 32 lanes on.
+__device__ inline float over_halves(float x) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
 }
 
 // 4 signed bytes to fp16, exactly: 1024 + (c + 128) is 0x6400 | byte.
@@ -69,10 +81,8 @@ __device__ inline u32x4 load_query(const void* q, uint64_t at) {
     return x;
 }
 
-// A row that holds an infinity or NaN gives NaN wherever it sees a key.
-__device__ inline float query_factor(float peak, float scale, int e) {
-    return peak < __builtin_huge_valf() ? ldexpf(scale * LOG2E, -e) : __builtin_nanf("");
-}
+// An element as the products take it; of a row that holds an infinity or NaN all are NaN, which it then gives wherever it sees a key.
+__device__ inline f16_t query_element(float x, float peak, int e) { return peak < __builtin_huge_valf() ? (f16_t)ldexpf(x, e) : (f16_t)__builtin_nanf(""); }
 
 // The power of two that brings a bf16 row's largest magnitude to [2^13, 2^14); 1 for fp16, rows of zeros, infinities and NaN.
 __device__ inline int query_exponent(float peak, uint32_t dtype) {
@@ -238,9 +248,9 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         for (int f = 0; f < ND; ++f) {
             convert_query(raw[f], a.dtype, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[f][i] = (f16_t)ldexpf(x[i], e);
+            for (int i = 0; i < 8; ++i) q[f][i] = query_element(x[i], peak, e);
         }
-        factor = query_factor(peak, a.scale, e);
+        factor = ldexpf(a.scale * LOG2E, -e);
     }
     for (; c < c1; c += W) {
         // where the scores of this lane lie; a missing page's lie behind every row
@@ -264,6 +274,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[t] *= by;
         if (!whole) {
+            rarely();
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -303,7 +314,8 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
                 l += e;
                 p[t / 2][t % 2 * 4 + i] = (f16_t)(e * weight);
             }
-        if (!whole) {     // what is not seen may have any scale
+        if (!whole && !(fabsf(weight) < __builtin_huge_valf())) {
+            rarely();      // what is not seen may have any scale
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -417,45 +429,55 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
         for (int f = 0; f < D / 16; ++f) {
             convert_query(raw[f], a.dtype, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[f][i] = (f16_t)ldexpf(x[i], e);
+            for (int i = 0; i < 8; ++i) q[f][i] = query_element(a.scale < 0.f ? -x[i] : x[i], peak, e);
         }
-        factor = query_factor(peak, a.scale, e);
+        factor = ldexpf(fabsf(a.scale) * LOG2E, -e);
     }
 
-    // a step's codes: `PER` runs of 16 keys' channels and 16 values' tokens a thread
+    // a step's codes: `PER` runs of 16 keys' channels and 16 values' tokens a thread; the pages of its four 16 tokens and their scales
     u32x4 kc[PER], vc[PER];
+    uint32_t absent, next_absent;
+    float ks[4], vs[4], next_ks[4], next_vs[4];
     auto fetch = [&](uint32_t c) {
         uint32_t page[4];
+        next_absent = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             page[j] = page_at(a.batch, table, (c * 64 + 16 * j) >> a.cache.shift, a.cache.n_pages);
+            next_absent |= page[j] == NO_PAGE ? 1u << j : 0u;
             page[j] = page[j] == NO_PAGE ? 0u : page[j];
+            next_ks[j] = a.cache.ks[(uint64_t)page[j] * heads + u.head];
+            next_vs[j] = a.cache.vs[(uint64_t)page[j] * heads + u.head];
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const uint32_t n = threadIdx.x + 256 * i;
-            if (UNITS % 256 == 0 || n < UNITS) {
-                const uint32_t t = n / (D / 16), d = n % (D / 16) * 16, j = t >> 4;
-                const uint32_t kp = j < 2 ? (j == 0 ? page[0] : page[1]) : (j == 2 ? page[2] : page[3]);
-                kc[i] = *(const u32x4*)(a.cache.k + (((uint64_t)kp * heads + u.head) * T + ((c * 64 + t) & (T - 1))) * D + d);
-                const uint32_t jv = n & 3, dv = n >> 2;
-                const uint32_t vp = jv < 2 ? (jv == 0 ? page[0] : page[1]) : (jv == 2 ? page[2] : page[3]);
-                vc[i] = *(const u32x4*)(a.cache.v + (((uint64_t)vp * heads + u.head) * D + dv) * T + ((c * 64 + 16 * jv) & (T - 1)));
-            }
+            const uint32_t n = min(threadIdx.x + 256 * i, (uint32_t)UNITS - 1);
+            const uint32_t t = n / (D / 16), d = n % (D / 16) * 16, j = t >> 4;
+            const uint32_t kp = j < 2 ? (j == 0 ? page[0] : page[1]) : (j == 2 ? page[2] : page[3]);
+            kc[i] = *(const u32x4*)(a.cache.k + (((uint64_t)kp * heads + u.head) * T + ((c * 64 + t) & (T - 1))) * D + d);
+            const uint32_t jv = n & 3, dv = n >> 2;
+            const uint32_t vp = jv < 2 ? (jv == 0 ? page[0] : page[1]) : (jv == 2 ? page[2] : page[3]);
+            vc[i] = *(const u32x4*)(a.cache.v + (((uint64_t)vp * heads + u.head) * D + dv) * T + ((c * 64 + 16 * jv) & (T - 1)));
         }
     };
     auto put = [&](int buffer) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const uint32_t n = threadIdx.x + 256 * i;
-            if (UNITS % 256 == 0 || n < UNITS) {
-                f16_t* k = &k_tile[buffer][n / (D / 16) * KS + n % (D / 16) * 16];
-                *(half8*)k = codes_to_half(kc[i].x, kc[i].y);
-                *(half8*)(k + 8) = codes_to_half(kc[i].z, kc[i].w);
-                f16_t* v = &v_tile[buffer][(n >> 2) * VS + (n & 3) * 16];
-                *(half8*)v = codes_to_half(vc[i].x, vc[i].y);
-                *(half8*)(v + 8) = codes_to_half(vc[i].z, vc[i].w);
-            }
+            const uint32_t n = min(threadIdx.x + 256 * i, (uint32_t)UNITS - 1);
+            f16_t* k = &k_tile[buffer][n / (D / 16) * KS + n % (D / 16) * 16];
+            *(half8*)k = codes_to_half(kc[i].x, kc[i].y);
+            *(half8*)(k + 8) = codes_to_half(kc[i].z, kc[i].w);
+            f16_t* v = &v_tile[buffer][(n >> 2) * VS + (n & 3) * 16];
+            *(half8*)v = codes_to_half(vc[i].x, vc[i].y);
+            *(half8*)(v + 8) = codes_to_half(vc[i].z, vc[i].w);
+        }
+    };
+    auto next = [&]() {
+        absent = next_absent;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            ks[j] = next_ks[j];
+            vs[j] = next_vs[j];
         }
     };
 
@@ -463,81 +485,113 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     float m = NEVER, top = NEVER, l = 0.f;
     // row m of a product's 32 tokens is token 16 (m / 16) + 8 (m / 4 % 2) + 4 (m / 8 % 2) + m % 4: a lane's 16 scores are then two runs of 8 tokens
     const uint32_t k_row = 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3);
-    if (c0 < c1) fetch(c0);
+    if (c0 < c1) {
+        fetch(c0);
+        put(0);
+        next();
+        fetch(c0 + 1);
+    }
     for (uint32_t c = c0; c < c1; ++c) {
         const int buffer = (c - c0) & 1;
-        put(buffer);
-        if (c + 1 < c1) fetch(c + 1);
         __syncthreads();
         const int32_t from = (int32_t)(c * 64);
-        if (from > pos_last || from + 63 < least_first) continue;
-        float ks[4], vs[4];
-        bool missing = false;
-        uint32_t absent = 0;
+        const bool seen = from <= pos_last && from + 63 >= least_first;
+        f32x16 s[2] = {};
+        if (seen) {
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int f = 0; f < D / 16; ++f)
+                    s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)&k_tile[buffer][(32 * mt + k_row) * KS + 16 * f + 8 * h], q[f], s[mt], 0, 0, 0);
+        }
+        // behind the barrier nobody reads the other buffer: the next step goes there beside the products (behind the last step nothing of use)
+        put(buffer ^ 1);
+        float by[4], weight[4];
+        uint32_t gone = absent;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t page = page_at(a.batch, table, (c * 64 + 16 * j) >> a.cache.shift, a.cache.n_pages);
-            if (page == NO_PAGE) {
-                missing = true;
-                absent |= 1u << j;
-            }
-            const uint64_t at = (uint64_t)(page == NO_PAGE ? 0u : page) * heads + u.head;
-            ks[j] = a.cache.ks[at] * factor;
-            vs[j] = a.cache.vs[at];
+            by[j] = ks[j] * factor;
+            by[j] = by[j] < LEAST_SCALE ? LEAST_SCALE : by[j];
+            weight[j] = vs[j];
         }
-        f32x16 s[2] = {};
+        next();
+        fetch(c + 2);
+        if (!seen) continue;
+        const bool inside = from + 63 <= pos_first && from >= least_last && !gone;
+        if (!inside) {
+            rarely();
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-            for (int f = 0; f < D / 16; ++f)
-                s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)&k_tile[buffer][(32 * mt + k_row) * KS + 16 * f + 8 * h], q[f], s[mt], 0, 0, 0);
-        const bool inside = from + 63 <= pos_first && from >= least_last && !missing;
-        float peaks[4] = {NEVER, NEVER, NEVER, NEVER};
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int j = 2 * mt + i / 8;
-                const int32_t at = from + 16 * j + 8 * (int32_t)h + i % 8;
-                s[mt][i] = inside || (at <= pos && at >= least && !(absent >> j & 1)) ? s[mt][i] * ks[j] : NEVER;
-                peaks[j] = fmaxf(peaks[j], s[mt][i]);
-            }
+                for (int i = 0; i < 16; ++i) {
+                    const int j = 2 * mt + i / 8;
+                    const int32_t at = from + 16 * j + 8 * (int32_t)h + i % 8;
+                    s[mt][i] = ((at <= pos) & (at >= least) & !(gone >> j & 1)) ? s[mt][i] : NEVER;
+                }
+        }
         float peak = NEVER, high = NEVER;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            peak = fmaxf(peak, peaks[j]);
-            high = fmaxf(high, vs[j] < __builtin_huge_valf() ? peaks[j] + __builtin_amdgcn_logf(vs[j]) : NEVER);
+            float x = s[j / 2][j % 2 * 8];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) x = fmaxf(x, s[j / 2][j % 2 * 8 + i]);
+            x *= by[j];
+            peak = fmaxf(peak, x);
+            high = fmaxf(high, weight[j] < __builtin_huge_valf() ? x + __builtin_amdgcn_logf(weight[j]) : NEVER);
         }
-        peak = fmaxf(peak, __shfl_xor(peak, 32));
-        high = fmaxf(high, __shfl_xor(high, 32));
-        if (__any(peak > m || high > top)) {
+        peak = over_halves(peak);
+        high = over_halves(high);
+        // The references m and top follow the largest only when it has passed them by SLACK: what they are does not matter, as long as P stays in range.
+        if (__any(peak > m + SLACK || high > top + SLACK)) {
             const float m_new = fmaxf(m, peak), top_new = fmaxf(top, high);
             if (m_new != m) l *= exp2_fast(m - m_new);
-            if (top_new != top) {
-                const float keep = exp2_fast(top - top_new);
+            const float keep = top_new != top ? exp2_fast(top - top_new) : 1.f;
 #pragma unroll
-                for (int d = 0; d < ND; ++d) o[d] *= keep;
-            }
+            for (int d = 0; d < ND; ++d) o[d] *= keep;
             m = m_new;
             top = top_new;
         }
         const float base = m == NEVER ? 0.f : m;
-        float weight[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) weight[j] = p_factor(vs[j], m, top);
+        for (int j = 0; j < 4; ++j) weight[j] = p_factor(weight[j], m, top);
+        half8 p[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            half8 p;
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float x = s[j / 2][j % 2 * 8 + i], e = exp2_fast(x - base);
-                l += e;
-                p[i] = (f16_t)(inside || x != NEVER ? e * weight[j] : 0.f);
+                const float e = exp2_fast(fmaf(s[j / 2][j % 2 * 8 + i], by[j], -base));
+                s[j / 2][j % 2 * 8 + i] = e;
+                p[j][i] = (f16_t)(e * weight[j]);
             }
+        if (!inside) {
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += fabsf(weight[j]) + fabsf(by[j]);
+            if (__any(!(sum < __builtin_huge_valf()))) {      // what is not seen may have any scale
+                rarely();
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int32_t at = from + 16 * j + 8 * (int32_t)h + i;
+                        const bool shown = (at <= pos) & (at >= least) & !(gone >> j & 1);
+                        s[j / 2][j % 2 * 8 + i] = shown ? s[j / 2][j % 2 * 8 + i] : 0.f;
+                        p[j][i] = shown ? p[j][i] : (f16_t)0.f;
+                    }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float part = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part += s[j / 2][j % 2 * 8 + i];
+            l += part;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int d = 0; d < ND; ++d)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)&v_tile[buffer][(32 * d + r) * VS + 16 * j + 8 * h], p, o[d], 0, 0, 0);
-        }
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)&v_tile[buffer][(32 * d + r) * VS + 16 * j + 8 * h], p[j], o[d], 0, 0, 0);
     }
     l += __shfl_xor(l, 32);
     if (!there) return;
