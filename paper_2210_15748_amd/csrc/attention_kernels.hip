@@ -377,19 +377,20 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
 // Keys and values are converted once for the workgroup's four waves on their way into LDS, two steps' worth of it: while one is computed
 // with, the next one's codes are under way from memory.  Rows in LDS are 16 bytes apart from a multiple of their length: a wave's 16-byte
 // reads then spread over all banks.
-template <int ND>
+// ONE: a step lies on one page (of 64 tokens or more), so its page and scales are the same for all.
+template <int ND, bool ONE>
 __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(AttendArgs a) {
+    constexpr int NG = ONE ? 1 : 4;     // groups of a step's tokens with scales of their own
     constexpr int D = ND * 32, KS = D + 8, VS = 64 + 8, UNITS = D * 4, PER = (UNITS + 255) / 256;
     __shared__ f16_t k_tile[2][64 * KS];
     __shared__ f16_t v_tile[2][D * VS];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
+    // Heads next to one another go to XCDs next to one another, so a head's tiles share an L2; the tiles with the most keys come first.
     uint32_t id = blockIdx.x;
-    const uint32_t part = id % a.parts;
-    id /= a.parts;
-    const uint32_t group_index = id;
-    const uint32_t tile = a.tiles - 1 - id % a.tiles;      // the longest first
-    id /= a.tiles;
-    const Unit whole_unit = unit_of(a, id / a.cache.heads, id % a.cache.heads);
+    const uint32_t unit_heads = gridDim.x / (a.parts * a.tiles), unit_head = id % unit_heads;
+    id /= unit_heads;
+    const uint32_t tile = a.tiles - 1 - id % a.tiles, part = id / a.tiles;
+    const Unit whole_unit = unit_of(a, unit_head / a.cache.heads, unit_head % a.cache.heads);
     if (tile * ATTEND_MANY >= whole_unit.rows) return;
     const Unit u = tile_of(a, whole_unit, tile);
     if (part >= unit_parts(a, u)) return;
@@ -437,27 +438,38 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     // a step's codes: `PER` runs of 16 keys' channels and 16 values' tokens a thread; the pages of its four 16 tokens and their scales
     u32x4 kc[PER], vc[PER];
     uint32_t absent, next_absent;
-    float ks[4], vs[4], next_ks[4], next_vs[4];
+    float ks[NG], vs[NG], next_ks[NG], next_vs[NG];
     auto fetch = [&](uint32_t c) {
-        uint32_t page[4];
+        uint32_t page[NG];
         next_absent = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NG; ++j) {
             page[j] = page_at(a.batch, table, (c * 64 + 16 * j) >> a.cache.shift, a.cache.n_pages);
-            next_absent |= page[j] == NO_PAGE ? 1u << j : 0u;
+            next_absent |= page[j] == NO_PAGE ? (ONE ? 15u : 1u << j) : 0u;
             page[j] = page[j] == NO_PAGE ? 0u : page[j];
             next_ks[j] = a.cache.ks[(uint64_t)page[j] * heads + u.head];
             next_vs[j] = a.cache.vs[(uint64_t)page[j] * heads + u.head];
         }
+        if constexpr (ONE) {
+            const int8_t* k = a.cache.k + (((uint64_t)page[0] * heads + u.head) * T + ((c * 64) & (T - 1))) * D;     // the same for all
+            const int8_t* v = a.cache.v + ((uint64_t)page[0] * heads + u.head) * D * T + ((c * 64) & (T - 1));
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const uint32_t n = min(threadIdx.x + 256 * i, (uint32_t)UNITS - 1);
-            const uint32_t t = n / (D / 16), d = n % (D / 16) * 16, j = t >> 4;
-            const uint32_t kp = j < 2 ? (j == 0 ? page[0] : page[1]) : (j == 2 ? page[2] : page[3]);
-            kc[i] = *(const u32x4*)(a.cache.k + (((uint64_t)kp * heads + u.head) * T + ((c * 64 + t) & (T - 1))) * D + d);
-            const uint32_t jv = n & 3, dv = n >> 2;
-            const uint32_t vp = jv < 2 ? (jv == 0 ? page[0] : page[1]) : (jv == 2 ? page[2] : page[3]);
-            vc[i] = *(const u32x4*)(a.cache.v + (((uint64_t)vp * heads + u.head) * D + dv) * T + ((c * 64 + 16 * jv) & (T - 1)));
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t n = min(threadIdx.x + 256 * i, (uint32_t)UNITS - 1);
+                kc[i] = *(const u32x4*)(k + 16 * n);
+                vc[i] = *(const u32x4*)(v + ((n >> 2) * T + 16 * (n & 3)));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const uint32_t n = min(threadIdx.x + 256 * i, (uint32_t)UNITS - 1);
+                const uint32_t t = n / (D / 16), d = n % (D / 16) * 16, j = t >> 4;
+                const uint32_t kp = j < 2 ? (j == 0 ? page[0] : page[1 % NG]) : (j == 2 ? page[2 % NG] : page[3 % NG]);
+                kc[i] = *(const u32x4*)(a.cache.k + (((uint64_t)kp * heads + u.head) * T + ((c * 64 + t) & (T - 1))) * D + d);
+                const uint32_t jv = n & 3, dv = n >> 2;
+                const uint32_t vp = jv < 2 ? (jv == 0 ? page[0] : page[1 % NG]) : (jv == 2 ? page[2 % NG] : page[3 % NG]);
+                vc[i] = *(const u32x4*)(a.cache.v + (((uint64_t)vp * heads + u.head) * D + dv) * T + ((c * 64 + 16 * jv) & (T - 1)));
+            }
         }
     };
     auto put = [&](int buffer) {
@@ -475,7 +487,7 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     auto next = [&]() {
         absent = next_absent;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NG; ++j) {
             ks[j] = next_ks[j];
             vs[j] = next_vs[j];
         }
@@ -495,7 +507,7 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
         const int buffer = (c - c0) & 1;
         __syncthreads();
         const int32_t from = (int32_t)(c * 64);
-        const bool seen = from <= pos_last && from + 63 >= least_first;
+        const bool seen = from <= pos_last && from + 63 >= least_first && tile * ATTEND_MANY + wave * 32 < u.rows;
         f32x16 s[2] = {};
         if (seen) {
 #pragma unroll
@@ -506,10 +518,10 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
         }
         // behind the barrier nobody reads the other buffer: the next step goes there beside the products (behind the last step nothing of use)
         put(buffer ^ 1);
-        float by[4], weight[4];
+        float by[NG], weight[NG];
         uint32_t gone = absent;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NG; ++j) {
             by[j] = ks[j] * factor;
             by[j] = by[j] < LEAST_SCALE ? LEAST_SCALE : by[j];
             weight[j] = vs[j];
@@ -531,10 +543,10 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
         }
         float peak = NEVER, high = NEVER;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NG; ++j) {
             float x = s[j / 2][j % 2 * 8];
 #pragma unroll
-            for (int i = 1; i < 8; ++i) x = fmaxf(x, s[j / 2][j % 2 * 8 + i]);
+            for (int i = 1; i < 32 / NG; ++i) x = fmaxf(x, s[(8 * j + i) / 16][(8 * j + i) % 16]);
             x *= by[j];
             peak = fmaxf(peak, x);
             high = fmaxf(high, weight[j] < __builtin_huge_valf() ? x + __builtin_amdgcn_logf(weight[j]) : NEVER);
@@ -553,39 +565,55 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
         }
         const float base = m == NEVER ? 0.f : m;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) weight[j] = p_factor(weight[j], m, top);
+        for (int j = 0; j < NG; ++j) weight[j] = p_factor(weight[j], m, top);
         half8 p[4];
+        // A step's P and sums from the same exponentials e^(s - m) weight where the weight is an ordinary number for all rows, otherwise (scales very
+        // far apart, or 0, or no numbers) from e^(s - m).
+        if (ONE && __all(weight[0] > 0x1p-60f && weight[0] < 0x1p60f)) {
+            const float shift = __builtin_amdgcn_logf(weight[0]) - base;
+            float part[4] = {};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e = exp2_fast(fmaf(s[j / 2][j % 2 * 8 + i], by[j], -base));
-                s[j / 2][j % 2 * 8 + i] = e;
-                p[j][i] = (f16_t)(e * weight[j]);
+                for (int i = 0; i < 8; ++i) {
+                    const float e = exp2_fast(fmaf(s[j / 2][j % 2 * 8 + i], by[0], shift));
+                    part[j] += e;
+                    p[j][i] = (f16_t)e;
+                }
+            l += (part[0] + part[1] + (part[2] + part[3])) / weight[0];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float e = exp2_fast(fmaf(s[j / 2][j % 2 * 8 + i], by[ONE ? 0 : j], -base));
+                    s[j / 2][j % 2 * 8 + i] = e;
+                    p[j][i] = (f16_t)(e * weight[ONE ? 0 : j]);
+                }
+            if (!inside) {
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < NG; ++j) sum += fabsf(weight[j]) + fabsf(by[j]);
+                if (__any(!(sum < __builtin_huge_valf()))) {      // what is not seen may have any scale
+                    rarely();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int32_t at = from + 16 * j + 8 * (int32_t)h + i;
+                            const bool shown = (at <= pos) & (at >= least) & !(gone >> j & 1);
+                            s[j / 2][j % 2 * 8 + i] = shown ? s[j / 2][j % 2 * 8 + i] : 0.f;
+                            p[j][i] = shown ? p[j][i] : (f16_t)0.f;
+                        }
+                }
             }
-        if (!inside) {
-            float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum += fabsf(weight[j]) + fabsf(by[j]);
-            if (__any(!(sum < __builtin_huge_valf()))) {      // what is not seen may have any scale
-                rarely();
+            for (int j = 0; j < 4; ++j) {
+                float part = 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int32_t at = from + 16 * j + 8 * (int32_t)h + i;
-                        const bool shown = (at <= pos) & (at >= least) & !(gone >> j & 1);
-                        s[j / 2][j % 2 * 8 + i] = shown ? s[j / 2][j % 2 * 8 + i] : 0.f;
-                        p[j][i] = shown ? p[j][i] : (f16_t)0.f;
-                    }
+                for (int i = 0; i < 8; ++i) part += s[j / 2][j % 2 * 8 + i];
+                l += part;
             }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float part = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) part += s[j / 2][j % 2 * 8 + i];
-            l += part;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -597,7 +625,7 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     if (!there) return;
     const float by = exp2_fast(top - P_TOP - (m == NEVER ? 0.f : m)) * (a.parts == 1 ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
     const uint64_t at = (uint64_t)token * q_heads + q_head;
-    const uint64_t slot = ((uint64_t)(group_index - group_index % a.tiles + tile) * a.parts + part) * ATTEND_MANY + wave * 32 + r;
+    const uint64_t slot = (((uint64_t)unit_head * a.tiles + tile) * a.parts + part) * ATTEND_MANY + wave * 32 + r;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -734,7 +762,8 @@ void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t stream)
             else attend_few_kernel<ND, 8, false><<<grid, dim3(512), 0, stream>>>(a);
         }
     }
-    else attend_many_kernel<ND><<<grid, dim3(256), 0, stream>>>(a);
+    else if (a.cache.page_tokens >= 64) attend_many_kernel<ND, true><<<grid, dim3(256), 0, stream>>>(a);
+    else attend_many_kernel<ND, false><<<grid, dim3(256), 0, stream>>>(a);
 }
 
 }  // namespace
