@@ -128,9 +128,9 @@ __device__ inline Unit unit_of(const AttendArgs& a, uint32_t index, uint32_t hea
     return u;
 }
 
-// The unit as the rows of one of its tiles of ATTEND_MANY see it.
-__device__ inline Unit tile_of(const AttendArgs& a, Unit u, uint32_t tile) {
-    const uint32_t t0 = tile * ATTEND_MANY / a.group, t1 = min((tile + 1) * ATTEND_MANY - 1, u.rows - 1) / a.group;
+// The unit as the rows of one of its tiles see it.
+__device__ inline Unit tile_of(const AttendArgs& a, Unit u, uint32_t tile, uint32_t rows) {
+    const uint32_t t0 = tile * rows / a.group, t1 = min((tile + 1) * rows - 1, u.rows - 1) / a.group;
     const int32_t p0 = u.begin + (int32_t)t0, p1 = u.begin + (int32_t)t1;
     u.hi = p1 < 0 ? 0u : min(u.hi, (uint32_t)p1 + 1u);
     u.lo = a.window && p0 >= 0 && (uint32_t)p0 + 1u > a.window ? (uint32_t)p0 + 1u - a.window : 0u;
@@ -373,40 +373,45 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     }
 }
 
-// ---- many rows: 128 to a workgroup, 32 to a wave, all over the same steps of 64 tokens ---------------------------------------
-// Keys and values are converted once for the workgroup's four waves on their way into LDS, two steps' worth of it: while one is computed
+// ---- many rows: 128 or 256 to a workgroup, 32 to a wave, all over the same steps of 64 tokens ---------------------------------------
+// Keys and values are converted once for the workgroup's waves on their way into LDS, two steps' worth of it: while one is computed
 // with, the next one's codes are under way from memory.  Rows in LDS are 16 bytes apart from a multiple of their length: a wave's 16-byte
 // reads then spread over all banks.
 // ONE: a step lies on one page (of 64 tokens or more), so its page and scales are the same for all.
-template <int ND, bool ONE>
-__global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(AttendArgs a) {
+template <int ND, int W, bool ONE>
+__global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many_kernel(AttendArgs a) {
+    constexpr uint32_t ROWS = 32 * W;
     constexpr int NG = ONE ? 1 : 4;     // groups of a step's tokens with scales of their own
-    constexpr int D = ND * 32, KS = D + 8, VS = 64 + 8, UNITS = D * 4, PER = (UNITS + 255) / 256;
+    constexpr int D = ND * 32, KS = D + 8, VS = 64 + 8, UNITS = D * 4, PER = (UNITS + 64 * W - 1) / (64 * W);
     __shared__ f16_t k_tile[2][64 * KS];
     __shared__ f16_t v_tile[2][D * VS];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, h = lane >> 5;
-    // Heads next to one another go to XCDs next to one another, so a head's tiles share an L2; the tiles with the most keys come first.
+    // Workgroups go to the 8 XCDs in turn: where the heads of all sequences are a multiple of 8, an XCD gets all tiles of some of them, one after the
+    // other, and their keys and values stay in its L2.  A head's longest tiles come first.  (Tiles of a long and a short sequence by turns
+    // would be as bad as can be: an XCD's workgroups go to its parts in turn as well, and some would get the long ones only.)
     uint32_t id = blockIdx.x;
-    const uint32_t unit_heads = gridDim.x / (a.parts * a.tiles), unit_head = id % unit_heads;
-    id /= unit_heads;
-    const uint32_t tile = a.tiles - 1 - id % a.tiles, part = id / a.tiles;
+    const uint32_t unit_heads = gridDim.x / (a.parts * a.tiles), xcds = unit_heads % 8 ? 1 : 8, lane_of = id % xcds;
+    id /= xcds;
+    const uint32_t tile = a.tiles - 1 - id % a.tiles;
+    id /= a.tiles;
+    const uint32_t part = id % a.parts, unit_head = id / a.parts * xcds + lane_of;
     const Unit whole_unit = unit_of(a, unit_head / a.cache.heads, unit_head % a.cache.heads);
-    if (tile * ATTEND_MANY >= whole_unit.rows) return;
-    const Unit u = tile_of(a, whole_unit, tile);
+    if (tile * ROWS >= whole_unit.rows) return;
+    const Unit u = tile_of(a, whole_unit, tile, ROWS);
     if (part >= unit_parts(a, u)) return;
     uint32_t c0, c1;
     part_range(a, u, part, c0, c1);
     const uint32_t* table = a.batch.tables + (uint64_t)u.seq * a.batch.table_pages;
     const uint32_t heads = a.cache.heads, q_heads = heads * a.group, T = a.cache.page_tokens;
 
-    const uint32_t row = tile * ATTEND_MANY + wave * 32 + r;
+    const uint32_t row = tile * ROWS + wave * 32 + r;
     const bool there = row < u.rows;
     const uint32_t safe = min(row, u.rows - 1);
     const uint32_t token = u.first_token + safe / a.group, q_head = u.head * a.group + safe % a.group;
     const int32_t pos = u.begin + (int32_t)(safe / a.group);
     const int32_t least = a.window ? max(pos - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
     // of the wave's rows
-    const uint32_t w0 = min(tile * ATTEND_MANY + wave * 32, u.rows - 1), w1 = min(tile * ATTEND_MANY + wave * 32 + 31, u.rows - 1);
+    const uint32_t w0 = min(tile * ROWS + wave * 32, u.rows - 1), w1 = min(tile * ROWS + wave * 32 + 31, u.rows - 1);
     const int32_t pos_first = u.begin + (int32_t)(w0 / a.group), pos_last = u.begin + (int32_t)(w1 / a.group);
     const int32_t least_first = a.window ? max(pos_first - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
     const int32_t least_last = a.window ? max(pos_last - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
@@ -438,31 +443,35 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     // a step's codes: `PER` runs of 16 keys' channels and 16 values' tokens a thread; the pages of its four 16 tokens and their scales
     u32x4 kc[PER], vc[PER];
     uint32_t absent, next_absent;
-    float ks[NG], vs[NG], next_ks[NG], next_vs[NG];
+    float ks[NG], vs[NG], next_ks, next_vs;
+    // A lane keeps the page and the scales of one of the four: vector loads, which come in order with the codes, a step ahead of their use.
+    uint32_t own_page = page_at(a.batch, table, (c0 * 64 + 16 * (lane & 3)) >> a.cache.shift, a.cache.n_pages);
     auto fetch = [&](uint32_t c) {
         uint32_t page[NG];
         next_absent = 0;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            page[j] = page_at(a.batch, table, (c * 64 + 16 * j) >> a.cache.shift, a.cache.n_pages);
+            page[j] = (uint32_t)__builtin_amdgcn_readlane((int)own_page, j);
             next_absent |= page[j] == NO_PAGE ? (ONE ? 15u : 1u << j) : 0u;
             page[j] = page[j] == NO_PAGE ? 0u : page[j];
-            next_ks[j] = a.cache.ks[(uint64_t)page[j] * heads + u.head];
-            next_vs[j] = a.cache.vs[(uint64_t)page[j] * heads + u.head];
         }
+        const uint64_t at = (uint64_t)(own_page == NO_PAGE ? 0u : own_page) * heads + u.head;
+        next_ks = a.cache.ks[at];
+        next_vs = a.cache.vs[at];
+        own_page = page_at(a.batch, table, ((c + 1) * 64 + 16 * (lane & 3)) >> a.cache.shift, a.cache.n_pages);
         if constexpr (ONE) {
             const int8_t* k = a.cache.k + (((uint64_t)page[0] * heads + u.head) * T + ((c * 64) & (T - 1))) * D;     // the same for all
             const int8_t* v = a.cache.v + ((uint64_t)page[0] * heads + u.head) * D * T + ((c * 64) & (T - 1));
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const uint32_t n = min(threadIdx.x + 256 * i, (uint32_t)UNITS - 1);
+                const uint32_t n = min(threadIdx.x + 64 * W * i, (uint32_t)UNITS - 1);
                 kc[i] = *(const u32x4*)(k + 16 * n);
                 vc[i] = *(const u32x4*)(v + ((n >> 2) * T + 16 * (n & 3)));
             }
         } else {
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const uint32_t n = min(threadIdx.x + 256 * i, (uint32_t)UNITS - 1);
+                const uint32_t n = min(threadIdx.x + 64 * W * i, (uint32_t)UNITS - 1);
                 const uint32_t t = n / (D / 16), d = n % (D / 16) * 16, j = t >> 4;
                 const uint32_t kp = j < 2 ? (j == 0 ? page[0] : page[1 % NG]) : (j == 2 ? page[2 % NG] : page[3 % NG]);
                 kc[i] = *(const u32x4*)(a.cache.k + (((uint64_t)kp * heads + u.head) * T + ((c * 64 + t) & (T - 1))) * D + d);
@@ -475,7 +484,7 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     auto put = [&](int buffer) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const uint32_t n = min(threadIdx.x + 256 * i, (uint32_t)UNITS - 1);
+            const uint32_t n = min(threadIdx.x + 64 * W * i, (uint32_t)UNITS - 1);
             f16_t* k = &k_tile[buffer][n / (D / 16) * KS + n % (D / 16) * 16];
             *(half8*)k = codes_to_half(kc[i].x, kc[i].y);
             *(half8*)(k + 8) = codes_to_half(kc[i].z, kc[i].w);
@@ -488,8 +497,8 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
         absent = next_absent;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            ks[j] = next_ks[j];
-            vs[j] = next_vs[j];
+            ks[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(next_ks), j));
+            vs[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(next_vs), j));
         }
     };
 
@@ -507,13 +516,13 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
         const int buffer = (c - c0) & 1;
         __syncthreads();
         const int32_t from = (int32_t)(c * 64);
-        const bool seen = from <= pos_last && from + 63 >= least_first && tile * ATTEND_MANY + wave * 32 < u.rows;
+        const bool seen = from <= pos_last && from + 63 >= least_first && tile * ROWS + wave * 32 < u.rows;
         f32x16 s[2] = {};
         if (seen) {
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            for (int f = 0; f < D / 16; ++f)
 #pragma unroll
-                for (int f = 0; f < D / 16; ++f)
+                for (int mt = 0; mt < 2; ++mt)
                     s[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)&k_tile[buffer][(32 * mt + k_row) * KS + 16 * f + 8 * h], q[f], s[mt], 0, 0, 0);
         }
         // behind the barrier nobody reads the other buffer: the next step goes there beside the products (behind the last step nothing of use)
@@ -625,7 +634,7 @@ __global__ __launch_bounds__(256, ND <= 4 ? 2 : 1) void attend_many_kernel(Atten
     if (!there) return;
     const float by = exp2_fast(top - P_TOP - (m == NEVER ? 0.f : m)) * (a.parts == 1 ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
     const uint64_t at = (uint64_t)token * q_heads + q_head;
-    const uint64_t slot = (((uint64_t)unit_head * a.tiles + tile) * a.parts + part) * ATTEND_MANY + wave * 32 + r;
+    const uint64_t slot = (((uint64_t)unit_head * a.tiles + tile) * a.parts + part) * ROWS + wave * 32 + r;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -665,7 +674,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
     Unit u = unit_of(a, id / a.cache.heads, id % a.cache.heads);
     const uint32_t row = tile * rows + rr;
     if (row >= u.rows) return;
-    if (rows == ATTEND_MANY) u = tile_of(a, u, tile);
+    if (rows != ATTEND_FEW) u = tile_of(a, u, tile, rows);
     const uint32_t parts = unit_parts(a, u);
     const uint64_t slot0 = (uint64_t)group_index * a.parts * rows + rr;
     float m = NEVER, l = 0.f;
@@ -708,7 +717,7 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
     Unit u = unit_of(a, id / a.cache.heads, id % a.cache.heads);
     const uint32_t row = tile * rows + rr;
     if (row >= u.rows) return;
-    if (rows == ATTEND_MANY) u = tile_of(a, u, tile);
+    if (rows != ATTEND_FEW) u = tile_of(a, u, tile, rows);
     const uint32_t parts = unit_parts(a, u);
     const uint64_t slot0 = (uint64_t)group_index * a.parts * rows + rr;
     const float2 s = lane < parts ? a.part_sums[slot0 + (uint64_t)lane * rows] : make_float2(NEVER, 0.f);
@@ -762,8 +771,15 @@ void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t stream)
             else attend_few_kernel<ND, 8, false><<<grid, dim3(512), 0, stream>>>(a);
         }
     }
-    else if (a.cache.page_tokens >= 64) attend_many_kernel<ND, true><<<grid, dim3(256), 0, stream>>>(a);
-    else attend_many_kernel<ND, false><<<grid, dim3(256), 0, stream>>>(a);
+    else if (p.rows == 256) {
+        if constexpr (ND == 4 || ND == 5) {
+            if (a.cache.page_tokens >= 64) attend_many_kernel<ND, 8, true><<<grid, dim3(512), 0, stream>>>(a);
+            else attend_many_kernel<ND, 8, false><<<grid, dim3(512), 0, stream>>>(a);
+        }
+    } else {
+        if (a.cache.page_tokens >= 64) attend_many_kernel<ND, 4, true><<<grid, dim3(256), 0, stream>>>(a);
+        else attend_many_kernel<ND, 4, false><<<grid, dim3(256), 0, stream>>>(a);
+    }
 }
 
 }  // namespace

@@ -51,6 +51,8 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
     const uint64_t rows = lists ? group : max_tokens * group;
     p.few = lists || rows <= ATTEND_FEW;
     p.rows = p.few ? ATTEND_FEW : ATTEND_MANY;
+    // (3584 tokens of 32 heads over up to 8192, in us with 128 / 256 rows to a workgroup: 421 / 464 at dim 64, 591 / 553 at 128, 1040 / 724 at 160)
+    if (!p.few && dim >= 128 && dim <= 160 && seqs * heads * divided_up(rows, 2 * ATTEND_MANY) >= 256) p.rows = 2 * ATTEND_MANY;
     p.tiles = (uint32_t)std::max<uint64_t>(1, divided_up(rows, p.rows));
     p.units = (uint32_t)(lists ? seqs * max_tokens : seqs);
     p.groups = (uint64_t)p.units * heads * p.tiles;
