@@ -572,6 +572,11 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
             m = m_new;
             top = top_new;
         }
+        half8 vf[ND];      // of wide heads, one wave to a SIMD: the first values' way from LDS is hidden behind the exponentials
+        if constexpr (ND >= 7) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d) vf[d] = *(const half8*)&v_tile[buffer][(32 * d + r) * VS + 8 * h];
+        }
         const float base = m == NEVER ? 0.f : m;
 #pragma unroll
         for (int j = 0; j < NG; ++j) weight[j] = p_factor(weight[j], m, top);
@@ -628,7 +633,8 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int d = 0; d < ND; ++d)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)&v_tile[buffer][(32 * d + r) * VS + 16 * j + 8 * h], p[j], o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ND >= 7 && j == 0 ? vf[d] : *(const half8*)&v_tile[buffer][(32 * d + r) * VS + 16 * j + 8 * h],
+                                                              p[j], o[d], 0, 0, 0);
     }
     l += __shfl_xor(l, 32);
     if (!there) return;
@@ -772,7 +778,7 @@ void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t stream)
         }
     }
     else if (p.rows == 256) {
-        if constexpr (ND == 4 || ND == 5) {
+        if constexpr (ND >= 4 && ND <= 6) {
             if (a.cache.page_tokens >= 64) attend_many_kernel<ND, 8, true><<<grid, dim3(512), 0, stream>>>(a);
             else attend_many_kernel<ND, 8, false><<<grid, dim3(512), 0, stream>>>(a);
         }

@@ -18,6 +18,9 @@ inline uint64_t append_places(uint64_t max_tokens, uint32_t page_tokens) { retur
 constexpr uint32_t ATTEND_CHUNK = 64;
 // Rows (query heads of one key head and the new tokens they belong to) of a workgroup, for few rows and for many.
 constexpr uint32_t ATTEND_FEW = 16, ATTEND_MANY = 128;
+// Up to so many rows of a unit the form for few takes, 16 at a time.  (16 sequences up to 8192, 8 heads of dim 128, us with the one for many / for few:
+// 32 rows 96 / 76, 48 rows 111 / 97, 64 rows 110 / 110; 32 sequences up to 1000 of dim 64: 32 rows 29 / 14, 64 rows 36 / 24.)
+constexpr uint32_t ATTEND_FEW_ROWS = 64;
 // Workgroups that a call is split into along the keys where it has fewer: as many as the chip holds at once (its registers decide), so that
 // none begins when others end.
 // (One token, 8 heads of 4 query heads, 268 MB of codes, in us: 59 / 63 / 70 with 1024 / 768 / 512 workgroups at dim 32, 68 / 58 / 58 at 64,
@@ -49,10 +52,11 @@ inline size_t attend_bytes(uint64_t slots, uint32_t dim, size_t* sums) {
 inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads, uint32_t group, uint32_t dim, uint64_t length, bool lists) {
     AttendPlan p{};
     const uint64_t rows = lists ? group : max_tokens * group;
-    p.few = lists || rows <= ATTEND_FEW;
+    p.few = lists || rows <= ATTEND_FEW_ROWS;
     p.rows = p.few ? ATTEND_FEW : ATTEND_MANY;
-    // (3584 tokens of 32 heads over up to 8192, in us with 128 / 256 rows to a workgroup: 421 / 464 at dim 64, 591 / 553 at 128, 1040 / 724 at 160)
-    if (!p.few && dim >= 128 && dim <= 160 && seqs * heads * divided_up(rows, 2 * ATTEND_MANY) >= 256) p.rows = 2 * ATTEND_MANY;
+    // (3584 tokens of 32 heads over up to 8192, in us with 128 / 256 rows to a workgroup: 421 / 464 at dim 64, 591 / 553 at 128, 1040 / 724 at 160, 1058 / 841 at 192,
+    // 1370 / 1622 at 256: there the registers of half as many waves are too few)
+    if (!p.few && dim >= 128 && dim <= 192 && seqs * heads * divided_up(rows, 2 * ATTEND_MANY) >= 256) p.rows = 2 * ATTEND_MANY;
     p.tiles = (uint32_t)std::max<uint64_t>(1, divided_up(rows, p.rows));
     p.units = (uint32_t)(lists ? seqs * max_tokens : seqs);
     p.groups = (uint64_t)p.units * heads * p.tiles;
@@ -77,7 +81,7 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
 inline size_t attend_workspace_upto(uint64_t max_tokens, uint32_t group, uint32_t dim, uint64_t length, bool lists) {
     if (divided_up(length, ATTEND_CHUNK) <= 4) return 0;
     const uint64_t few = (uint64_t)attend_target(true, dim) * ATTEND_FEW, many = (uint64_t)attend_target(false, dim) * ATTEND_MANY;
-    return attend_bytes(lists || max_tokens * group <= ATTEND_FEW ? few : std::max(few, many), dim, nullptr);
+    return attend_bytes(lists || max_tokens * group <= ATTEND_FEW_ROWS ? few : std::max(few, many), dim, nullptr);
 }
 
 // Scores of the pages of a batch's tokens; all ones for more than any memory holds.
