@@ -760,6 +760,7 @@ def cache_attention(ix: Index, cache: Cache, batch: CacheBatch, q: torch.Tensor,
     made = []
     n = batch.n_tokens
     q_ptr, heads, apart = _states(ix, q, n, None, cache.dim, "q", made, _HALF_TYPES)
+    window = _size(window, "window")
     if pages is None:
         p_ptr, n_select = None, 0
     else:
@@ -771,7 +772,7 @@ def cache_attention(ix: Index, cache: Cache, batch: CacheBatch, q: torch.Tensor,
     ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_attention_workspace_bytes, cache, batch, heads, n_select)
     _lend(ix, made)
     _check(lib().dessert_cache_attention(ix.handle, cache.address, batch.address, q_ptr, _FLOAT_TYPES[q.dtype], apart, heads,
-                                         cache.dim ** -0.5 if scale is None else scale, _size(window, "window"), p_ptr, n_select, ws_ptr, ws_bytes,
+                                         cache.dim ** -0.5 if scale is None else scale, window, p_ptr, n_select, ws_ptr, ws_bytes,
                                          out.data_ptr(), out_lse.data_ptr()))
     return out, out_lse
 
@@ -791,11 +792,11 @@ def cache_select(ix: Index, cache: Cache, batch: CacheBatch, q_codes: torch.Tens
     if n == 0 or rows % n:
         raise ValueError(f"q_codes has {rows} rows for {n} tokens")
     s_ptr = _vector(ix, q_scales, rows, "q_scales", made, _FLOAT32)
+    n_first, n_last = _size(n_first, "n_first"), _size(n_last, "n_last")
     out = _output(ix, out, (n, cache.n_heads, _size(n_select, "n_select")), "out", made, torch.uint32)
     ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_select_workspace_bytes, cache, batch)
     _lend(ix, made)
-    _check(lib().dessert_cache_select(ix.handle, cache.address, batch.address, q_ptr, s_ptr, rows // n, n_select, _size(n_first, "n_first"),
-                                      _size(n_last, "n_last"), ws_ptr, ws_bytes, out.data_ptr()))
+    _check(lib().dessert_cache_select(ix.handle, cache.address, batch.address, q_ptr, s_ptr, rows // n, n_select, n_first, n_last, ws_ptr, ws_bytes, out.data_ptr()))
     return out
 
 

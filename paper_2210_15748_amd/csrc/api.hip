@@ -1543,9 +1543,11 @@ dessert_status_t check_group(uint32_t n_q_heads, const CachePages& c, uint32_t* 
     return DESSERT_OK;
 }
 
-// The keys that a row looks at, at most.
-uint64_t attended(const dessert_cache_batch_t& b, uint32_t page_tokens, uint32_t n_select) {
-    return n_select ? (uint64_t)n_select * page_tokens : std::min<uint64_t>(b.max_length, (uint64_t)b.table_pages * page_tokens);
+// The keys that a sequence's rows look at, at most.
+uint64_t attended(const dessert_cache_batch_t& b, uint32_t page_tokens, uint32_t n_select, uint32_t window) {
+    if (n_select) return (uint64_t)n_select * page_tokens;
+    const uint64_t length = std::min<uint64_t>(b.max_length, (uint64_t)b.table_pages * page_tokens);
+    return window ? std::min<uint64_t>(length, (uint64_t)window + b.max_tokens - 1) : length;
 }
 
 // The caches of the layers that go on together.
@@ -1597,7 +1599,7 @@ size_t dessert_cache_attention_workspace_bytes(const dessert_index_t* ix, const 
     CacheBatch b;
     uint32_t group;
     if (!ix || check_cache(cache, &c) != DESSERT_OK || check_cache_batch(batch, c, &b) != DESSERT_OK || check_group(n_q_heads, c, &group) != DESSERT_OK) return 0;
-    return attend_workspace_upto(b.max_tokens, group, c.dim, attended(*batch, c.page_tokens, n_select), n_select != 0);
+    return attend_workspace_upto(b.max_tokens, group, c.dim, attended(*batch, c.page_tokens, n_select, 0), n_select != 0);
 }
 
 dessert_status_t dessert_cache_attention(const dessert_index_t* ix, const dessert_cache_t* cache, const dessert_cache_batch_t* batch,
@@ -1622,7 +1624,7 @@ dessert_status_t dessert_cache_attention(const dessert_index_t* ix, const desser
         const uint64_t units = (uint64_t)a.batch.n_seqs * (n_select ? a.batch.max_tokens : 1);
         if ((uint64_t)a.batch.max_tokens * a.group > CACHE_MOST || units > MAX_WORKGROUPS || units * a.cache.heads > MAX_WORKGROUPS)
             return fail(DESSERT_EINVAL, "too many tokens for one call");
-        p = attend_plan(a.batch.n_seqs, a.batch.max_tokens, a.cache.heads, a.group, a.cache.dim, attended(*batch, a.cache.page_tokens, n_select), n_select != 0);
+        p = attend_plan(a.batch.n_seqs, a.batch.max_tokens, a.cache.heads, a.group, a.cache.dim, attended(*batch, a.cache.page_tokens, n_select, window), n_select != 0);
         if (p.groups * p.parts > MAX_WORKGROUPS) return fail(DESSERT_EINVAL, "too many tokens for one call");
         st = check_workspace(workspace_dev, workspace_bytes, p.bytes);
         if (st != DESSERT_OK) return st;

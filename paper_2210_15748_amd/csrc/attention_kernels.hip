@@ -335,7 +335,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         sums[wave][r][0] = m;
         sums[wave][r][1] = l;
     }
-    __syncthreads();
+    barrier();
     float most = NEVER, total = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) most = fmaxf(most, sums[w][r][0]);
@@ -349,11 +349,11 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         if (wave >= half && wave < 2 * half)
 #pragma unroll
             for (int d = 0; d < NV; ++d) joined[wave - half][d][lane] = o[d];
-        __syncthreads();
+        barrier();
         if (wave < half)
 #pragma unroll
             for (int d = 0; d < NV; ++d) o[d] += joined[wave][d][lane];
-        if (half > 1) __syncthreads();
+        if (half > 1) barrier();
     }
     if (wave != 0 || tile * 16 + r >= u.rows) return;
     if (a.parts == 1) {
@@ -514,7 +514,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     }
     for (uint32_t c = c0; c < c1; ++c) {
         const int buffer = (c - c0) & 1;
-        __syncthreads();
+        barrier();
         const int32_t from = (int32_t)(c * 64);
         const bool seen = from <= pos_last && from + 63 >= least_first && tile * ROWS + wave * 32 < u.rows;
         f32x16 s[2] = {};
@@ -664,7 +664,7 @@ __device__ inline float over_workgroup(float x, bool max, float* parts) {
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) x = max ? fmaxf(x, __shfl_xor(x, o)) : x + __shfl_xor(x, o);
     if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
-    __syncthreads();
+    barrier();
     return max ? fmaxf(fmaxf(parts[0], parts[1]), fmaxf(parts[2], parts[3])) : parts[0] + parts[1] + parts[2] + parts[3];
 }
 
@@ -702,7 +702,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
         for (uint32_t i = part0; i < parts; i += lanes) x += *(const f32x4*)(from + i * apart) * factors[i];
     }
     joined[threadIdx.x] = x;
-    __syncthreads();
+    barrier();
     if (part0 != 0) return;
     for (uint32_t i = 1; i < lanes; ++i) x += joined[i * per + threadIdx.x];
     const uint64_t at = (uint64_t)(u.first_token + row / a.group) * (a.cache.heads * a.group) + u.head * a.group + row % a.group;

@@ -11,6 +11,13 @@ namespace dessert {
 
 constexpr uint32_t NO_PAGE = 0xFFFFFFFFu;
 
+// A barrier with the wave's LDS operations waited for.  (The compiler leaves the wait out of barriers at the heads of some loops, over whose back
+// edges LDS operations come.)
+__device__ inline void barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 // A sequence's new tokens: rows first .. first + count, at positions begin .. begin + count (negative ones are nowhere).
 struct NewTokens {
     uint32_t first, count;

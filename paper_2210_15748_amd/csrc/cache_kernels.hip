@@ -121,13 +121,13 @@ __global__ __launch_bounds__(64 * W) void append_kernel(CachePages c, CacheBatch
     int8_t* bounds = c.bounds ? c.bounds + at * 2 * D : nullptr;
     if constexpr (W > 1) {
         if ((threadIdx.x & 63) == 0) peaks[threadIdx.x >> 6] = peak;
-        __syncthreads();
+        barrier();
 #pragma unroll
         for (int w = 0; w < W; ++w) peak = max(peak, peaks[w]);
     }
     const PageScale scale(had, peak);
     const float factor = 1.f / scale.now, ratio = had / scale.now;
-    __syncthreads();      // every thread has read the scale
+    barrier();      // every thread has read the scale
     if (threadIdx.x == 0) scales[at] = scale.now;
 
     if (!values) {
@@ -172,13 +172,13 @@ __global__ __launch_bounds__(64 * W) void append_kernel(CachePages c, CacheBatch
             }
         }
         if (bounds) {
-            __syncthreads();
+            barrier();
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 atomicMin(&least[d8 * 8 + j], low[j]);
                 atomicMax(&most[d8 * 8 + j], high[j]);
             }
-            __syncthreads();
+            barrier();
             for (uint32_t d = threadIdx.x; d < D; d += 64 * W) {
                 bounds[d] = (int8_t)least[d];
                 bounds[D + d] = (int8_t)most[d];
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(64 * W) void append_kernel(CachePages c, CacheBatch
             for (int j = 0; j < 8; ++j)
                 tile[(d8 * 8 + j) * row + quad] = (uint32_t)(q[0] >> 8 * j & 255) | (uint32_t)(q[1] >> 8 * j & 255) << 8 |
                                                   (uint32_t)(q[2] >> 8 * j & 255) << 16 | (uint32_t)(q[3] >> 8 * j & 255) << 24;
-        __syncthreads();
+        barrier();
         const uint32_t groups = R / 16;
         for (uint32_t i = threadIdx.x; i < D * groups; i += 64 * W) {
             const uint32_t d = i / groups, g = i % groups, slot = base + round * R + g * 16;
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(64 * W) void append_kernel(CachePages c, CacheBatch
             }
             __builtin_memcpy(to, &z, 16);
         }
-        __syncthreads();
+        barrier();
     }
 }
 
@@ -345,9 +345,9 @@ __device__ inline uint32_t sum_before(uint32_t x, uint32_t* parts, uint32_t& tot
         total = __shfl((int)y, 63);
         return y - x;
     }
-    __syncthreads();
+    barrier();
     if (lane == 63) parts[wave] = y;
-    __syncthreads();
+    barrier();
     uint32_t before = 0;
     total = 0;
 #pragma unroll
@@ -392,7 +392,7 @@ __device__ inline void pick(const uint32_t* keys, uint32_t n, uint32_t n_select,
                 parts[W + (threadIdx.x >> 6)] = hi;
                 parts[2 * W + (threadIdx.x >> 6)] = there;
             }
-            __syncthreads();
+            barrier();
             there = 0;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
@@ -400,7 +400,7 @@ __device__ inline void pick(const uint32_t* keys, uint32_t n, uint32_t n_select,
                 hi = max(hi, parts[W + w]);
                 there += parts[2 * W + w];
             }
-            __syncthreads();
+            barrier();
         }
         if (there > n_select && hi) {
             const uint32_t differ = lo ^ hi;
@@ -414,7 +414,7 @@ __device__ inline void pick(const uint32_t* keys, uint32_t n, uint32_t n_select,
                 if constexpr (W > 1) {
                     uint32_t* slot = parts + (bit & 1) * W;
                     if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = count;
-                    __syncthreads();
+                    barrier();
                     count = 0;
 #pragma unroll
                     for (int w = 0; w < W; ++w) count += slot[w];
@@ -495,12 +495,12 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
         uint32_t want = a.n_select, mask = 0;
         for (int shift = 24; shift >= 0; shift -= 8) {
             if (threadIdx.x < 256) counts[threadIdx.x] = 0;
-            __syncthreads();
+            barrier();
             for (uint32_t i = threadIdx.x; i < n; i += 1024) {
                 const uint32_t key = keys[i];
                 if ((key & mask) == border) atomicAdd(&counts[key >> shift & 255], 1u);
             }
-            __syncthreads();
+            barrier();
             // digits from the highest: thread i sees to digit 255 - i
             const uint32_t here = threadIdx.x < 256 ? counts[255 - threadIdx.x] : 0u;
             uint32_t total;
@@ -509,11 +509,11 @@ __global__ __launch_bounds__(1024) void select_pages_kernel(SelectArgs a) {
                 found[0] = 255 - threadIdx.x;
                 found[1] = want - before;
             }
-            __syncthreads();
+            barrier();
             border |= found[0] << shift;
             want = found[1];
             mask |= 255u << shift;
-            __syncthreads();
+            barrier();
         }
         ties = border ? want : 0u;
     }

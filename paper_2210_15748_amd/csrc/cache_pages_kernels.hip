@@ -15,7 +15,7 @@ __device__ inline uint32_t load_now(const uint32_t* p) { return __hip_atomic_loa
 // write L2 back, a few microseconds each time.)
 __device__ inline void arrived() {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
+    barrier();
 }
 
 struct AdvanceWork {
@@ -71,9 +71,9 @@ __device__ inline uint32_t before_1024(uint32_t x, uint32_t* parts, uint32_t& to
         const uint32_t z = __shfl_up((int)y, o);
         if (lane >= (uint32_t)o) y += z;
     }
-    __syncthreads();
+    barrier();
     if (lane == 63) parts[wave] = y;
-    __syncthreads();
+    barrier();
     uint32_t before = 0;
     total = 0;
 #pragma unroll
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(1024) void advance_decide_kernel(AdvanceArgs a, Adv
             }
         free_count += total;
     }
-    __syncthreads();
+    barrier();
     // copies that are not granted leave their page with the one that would keep it, which is not granted then either
     for (uint32_t b = threadIdx.x; b < n; b += 1024) {
         const Wish x = wish_of(a, n_pages, shift, b);
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(1024) void advance_decide_kernel(AdvanceArgs a, Adv
             else atomicAdd(&taken, want.y);
         }
     }
-    __syncthreads();
+    barrier();
     if (threadIdx.x == 0) {
         a.status[0] = free_count - taken;
         a.status[1] = refused;
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(1024) void advance_few_kernel(AdvanceArgs a, Advanc
             w.stays[x.last] = 0;
         }
     }
-    __syncthreads();
+    barrier();
     if (make_tables) {
         for (uint32_t i = threadIdx.x; i < max(n, a.p.n_seqs) * stride; i += 1024) {
             const uint32_t s = i / stride, j = i % stride;
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(1024) void advance_few_kernel(AdvanceArgs a, Advanc
         if (keeps && load_now(w.stays + x.last)) granted = false;
     }
     if (b < n) first_new[b] = granted ? x.have - copies : NO_PAGE;
-    __syncthreads();
+    barrier();
     for (uint32_t i = threadIdx.x; i < min(asked, free_count); i += 1024) {
         uint32_t lo = 0, hi = n;           // the last sequence that begins at or before i and asks for something
         while (hi - lo > 1) {
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(1024) void advance_few_kernel(AdvanceArgs a, Advanc
         if (!granted) atomicAdd(&refused, 1u);
         else if (need) atomicAdd(&taken, need);
     }
-    __syncthreads();
+    barrier();
     if (b == 0) {
         a.status[0] = free_count - taken;
         a.status[1] = refused;

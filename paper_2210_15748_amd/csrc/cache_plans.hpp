@@ -48,7 +48,7 @@ inline size_t attend_bytes(uint64_t slots, uint32_t dim, size_t* sums) {
     return (out + slots * 2 * sizeof(float) + 255) / 256 * 256;
 }
 
-// length: the most keys that a row looks at (with lists: n_select pages of them)
+// length: about the most keys that the rows of a unit look at (with lists: n_select pages of them)
 inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads, uint32_t group, uint32_t dim, uint64_t length, bool lists) {
     AttendPlan p{};
     const uint64_t rows = lists ? group : max_tokens * group;
@@ -61,7 +61,7 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
     p.units = (uint32_t)(lists ? seqs * max_tokens : seqs);
     p.groups = (uint64_t)p.units * heads * p.tiles;
     const uint64_t chunks = std::max<uint64_t>(1, divided_up(length, ATTEND_CHUNK));
-    const uint64_t target = attend_target(p.few, dim);
+    const uint64_t target = p.few ? attend_target(true, dim) : attend_target(false, dim) * ATTEND_MANY / p.rows;
     p.waves = 4;
     // a part has work for the four waves of a workgroup (one step each) or, of many rows, for a few steps
     uint64_t parts = std::min(std::max<uint64_t>(1, target / std::max<uint64_t>(1, p.groups)), divided_up(chunks, 4));
