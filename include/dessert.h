@@ -463,7 +463,7 @@ typedef struct {
  *   starts_dev    dev, [n_seqs + 1]: the new tokens of sequence b are rows starts[b] .. starts[b + 1] of the arrays of tokens,
  *                 in order (there may be none); or NULL: one new token each, row b
  *   n_tokens      rows of the arrays of tokens; those from starts[n_seqs] on are neither read nor written
- *   max_tokens    at least the largest number of new tokens of a sequence: further ones are left out
+ *   max_tokens    at least the largest number of new tokens of a sequence: further ones, at its end, are left out
  *   max_length    about the largest length: how work is divided goes by it, results do not depend on it but for rounding */
 typedef struct {
     const uint32_t *tables_dev, *lengths_dev, *starts_dev;

@@ -28,13 +28,15 @@ __device__ inline NewTokens new_tokens(const CacheBatch& b, uint32_t s) {
     NewTokens n;
     if (b.starts) {
         const uint32_t lo = b.starts[s], hi = b.starts[s + 1];
+        const uint32_t all = min(hi > lo ? hi - lo : 0u, CACHE_MOST);
         n.first = min(lo, b.n_tokens);
-        n.count = min(hi > lo ? hi - lo : 0u, min(b.n_tokens - n.first, b.max_tokens));
+        n.count = min(all, min(b.n_tokens - n.first, b.max_tokens));
+        n.begin = (int32_t)min(b.lengths[s], CACHE_MOST) - (int32_t)all;
     } else {
         n.first = s;
         n.count = 1;
+        n.begin = (int32_t)min(b.lengths[s], CACHE_MOST) - 1;
     }
-    n.begin = (int32_t)min(b.lengths[s], CACHE_MOST) - (int32_t)n.count;
     return n;
 }
 
