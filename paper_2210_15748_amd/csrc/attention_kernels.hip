@@ -581,9 +581,9 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
 #pragma unroll
         for (int j = 0; j < NG; ++j) weight[j] = p_factor(weight[j], m, top);
         half8 p[4];
-        // A step's P and sums from the same exponentials e^(s - m) weight where the weight is an ordinary number for all rows, otherwise (scales very
-        // far apart, or 0, or no numbers) from e^(s - m).
-        if (ONE && __all(weight[0] > 0x1p-60f && weight[0] < 0x1p60f)) {
+        // A step's P and sums from the same exponentials e^(s - m) weight where the weight is an ordinary number for all rows and the keys' scale
+        // one at all, otherwise (scales very far apart, or 0, or no numbers) from e^(s - m).
+        if (ONE && __all(weight[0] > 0x1p-60f && weight[0] < 0x1p60f && by[0] < __builtin_huge_valf())) {
             const float shift = __builtin_amdgcn_logf(weight[0]) - base;
             float part[4] = {};
 #pragma unroll

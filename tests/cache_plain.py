@@ -128,8 +128,8 @@ def append(c, tables, lengths, new, k, v):
                     fresh = rounded(x.astype(np.float64), np.float64(now)) if now > 0 else np.zeros(x.shape, np.int8)
                     old[s0:s1] = fresh
                     if keys:
-                        both = fresh if s0 == 0 else np.concatenate([bounds, fresh])
-                        bounds[:] = np.stack([both.min(axis=0), both.max(axis=0)])
+                        least, most_code = fresh.min(axis=0), fresh.max(axis=0)
+                        bounds[:] = np.stack([least, most_code] if s0 == 0 else [np.minimum(bounds[0], least), np.maximum(bounds[1], most_code)])
                     scales[page, h] = float(now)
         row += m
 
