@@ -89,8 +89,7 @@ __global__ __launch_bounds__(64 * W) void append_kernel(CachePages c, CacheBatch
     const int32_t lo = max(begin, (int32_t)(place << c.shift)), hi = min(end, (int32_t)((place + 1) << c.shift));
     if (place >= b.table_pages || lo >= hi) return;
     const uint32_t page = page_at(b, b.tables + (uint64_t)s * b.table_pages, place, c.n_pages);
-    if (page == NO_PAGE) return;
-    const uint64_t at = (uint64_t)page * c.heads + h;
+    const uint64_t at = (uint64_t)(page == NO_PAGE ? 0u : page) * c.heads + h;
     const uint32_t slot0 = lo & (P - 1), slot1 = slot0 + (uint32_t)(hi - lo);      // the new slots
     const uint64_t stride = values ? v_stride : k_stride;
     const T* x = (values ? v : k) + (uint64_t)(n.first + (uint32_t)(lo - n.begin)) * stride + (uint64_t)h * D;
@@ -106,9 +105,13 @@ __global__ __launch_bounds__(64 * W) void append_kernel(CachePages c, CacheBatch
             __builtin_memcpy(e[i], x + (uint64_t)(slot - slot0) * stride + d8 * 8, sizeof(e[i]));
         }
     };
+    float* scales = values ? c.vs : c.ks;
+    load(0);       // does not wait for the page's number
+    const float had = slot0 ? scales[at] : 0.f;
+    if (page == NO_PAGE) return;
     uint32_t peak = 0;
     for (uint32_t round = 0; round < rounds; ++round) {
-        load(round);
+        if (round) load(round);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -116,8 +119,6 @@ __global__ __launch_bounds__(64 * W) void append_kernel(CachePages c, CacheBatch
     }
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) peak = max(peak, (uint32_t)__shfl_xor((int)peak, o));
-    float* scales = values ? c.vs : c.ks;
-    const float had = slot0 ? scales[at] : 0.f;
     int8_t* bounds = c.bounds ? c.bounds + at * 2 * D : nullptr;
     if constexpr (W > 1) {
         if ((threadIdx.x & 63) == 0) peaks[threadIdx.x >> 6] = peak;
