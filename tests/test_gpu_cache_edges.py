@@ -192,3 +192,25 @@ def test_advance_that_asks_for_many_pages(ix, n, width, most):
             assert torch.equal(g_refs.cpu(), refs)
             for name in NAMES:
                 assert torch.equal(gc[name].cpu(), d[name]), name
+
+
+@pytest.mark.parametrize("told", [1, 700, 100000])
+@pytest.mark.parametrize("new", [1, 12, 80])
+def test_whatever_length_is_told(ix, told, new):
+    """max_length divides the work; sequences may be longer or shorter."""
+    lengths, page = [3000, 90, 1500], 32
+    pages = sum(-(-m // page) for m in lengths)
+    c = plain.make_cache(pages, 1, page, 64, 4)
+    tables = plain.make_tables(lengths, page, pages, 4)
+    q = torch.randn(3 * new, 2, 64, generator=torch.Generator().manual_seed(4)).to(torch.float16)
+    g = on_gpu(c)
+    b = dz.cache_batch(ix, tables.to(DEV), torch.tensor(lengths, dtype=torch.int32, device=DEV), plain.starts_of([new] * 3).to(DEV), n_tokens=3 * new,
+                       max_tokens=new, max_length=told)
+    out, lse = dz.cache_attention(ix, taken(ix, g), b, q.to(DEV))
+    close(out, lse, plain.attend(c, tables, lengths, [new] * 3, q, 0.125), torch.float16, 3000, 64)
+    # a workspace for more serves this call
+    more = dz.cache_batch(ix, tables.to(DEV), torch.tensor(lengths, dtype=torch.int32, device=DEV), plain.starts_of([new] * 3).to(DEV), n_tokens=3 * new + 50,
+                          max_tokens=new + 50, max_length=told + 1000)
+    room = torch.empty(dz.cache_attention_workspace_bytes(ix, taken(ix, g), more, 2), dtype=torch.uint8, device=DEV)
+    again = dz.cache_attention(ix, taken(ix, g), b, q.to(DEV), workspace=room)
+    assert torch.equal(again[0], out) and torch.equal(again[1], lse)

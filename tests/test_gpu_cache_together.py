@@ -135,9 +135,10 @@ def test_a_captured_step_replays_as_it_ran():
             graph = torch.cuda.CUDAGraph()
             with torch.cuda.graph(graph, stream=stream):
                 run_step(ix, gc, r, *src[2:], outs, ws)
-            made.append((graph, src, gc, r, outs, eager, (c, tables, lengths, refs, x, H, G, D, n)))
+            # a graph's replay reads and writes all of these: the workspaces have to live as long as it does, too
+            made.append((graph, src, gc, r, outs, ws, eager, (c, tables, lengths, refs, x, H, G, D, n)))
         for turn in range(4):
-            for graph, src, gc, r, outs, eager, _ in made:
+            for graph, src, gc, r, outs, _, eager, _ in made:
                 for k in gc:
                     gc[k].copy_(src[0][k])
                 r.copy_(src[1])
@@ -149,7 +150,7 @@ def test_a_captured_step_replays_as_it_ran():
                     assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), turn
                 (torch.randn(1000, 1000, device=DEV) @ torch.randn(1000, 1000, device=DEV)).sum().item()
     # and what they give is right
-    _, _, _, _, outs, _, (c, tables, lengths, refs, x, H, G, D, n) = made[1]
+    _, _, _, _, outs, _, _, (c, tables, lengths, refs, x, H, G, D, n) = made[1]
     t, l, _ = plain.advance(c, refs, tables, lengths, [1] * n, None)
     plain.append(layer(c, 0), t, l.tolist(), [1] * n, x[:, H * G:H * (G + 1)], x[:, H * (G + 1):])
     close(outs[7], outs[8], plain.attend(layer(c, 0), t, l.tolist(), [1] * n, x[:, :H * G], 0.125), torch.float16, 1000, D)
