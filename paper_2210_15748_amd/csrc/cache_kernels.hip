@@ -344,10 +344,6 @@ __device__ inline uint32_t sum_before(uint32_t x, uint32_t* parts, uint32_t& tot
         const uint32_t z = __shfl_up((int)y, o);
         if (lane >= (uint32_t)o) y += z;
     }
-    if constexpr (W == 1) {
-        total = __shfl((int)y, 63);
-        return y - x;
-    }
     barrier();
     if (lane == 63) parts[wave] = y;
     barrier();
@@ -390,22 +386,20 @@ __device__ inline void pick(const uint32_t* keys, uint32_t n, uint32_t n_select,
             hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
             there += (uint32_t)__shfl_xor((int)there, o);
         }
-        if constexpr (W > 1) {
-            if ((threadIdx.x & 63) == 0) {
-                parts[threadIdx.x >> 6] = lo;
-                parts[W + (threadIdx.x >> 6)] = hi;
-                parts[2 * W + (threadIdx.x >> 6)] = there;
-            }
-            barrier();
-            there = 0;
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                lo = min(lo, parts[w]);
-                hi = max(hi, parts[W + w]);
-                there += parts[2 * W + w];
-            }
-            barrier();
+        if ((threadIdx.x & 63) == 0) {
+            parts[threadIdx.x >> 6] = lo;
+            parts[W + (threadIdx.x >> 6)] = hi;
+            parts[2 * W + (threadIdx.x >> 6)] = there;
         }
+        barrier();
+        there = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            lo = min(lo, parts[w]);
+            hi = max(hi, parts[W + w]);
+            there += parts[2 * W + w];
+        }
+        barrier();
         if (there > n_select && hi) {
             const uint32_t differ = lo ^ hi;
             int bit = differ ? 31 - __clz((int)differ) : -1;
@@ -415,14 +409,12 @@ __device__ inline void pick(const uint32_t* keys, uint32_t n, uint32_t n_select,
                 uint32_t count = 0;
 #pragma unroll
                 for (int i = 0; i < EACH; ++i) count += (uint32_t)__popcll(__ballot(key[i] >= trial));
-                if constexpr (W > 1) {
-                    uint32_t* slot = parts + (bit & 1) * W;
-                    if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = count;
-                    barrier();
-                    count = 0;
+                uint32_t* slot = parts + (bit & 1) * W;      // by turns: one barrier a bit
+                if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = count;
+                barrier();
+                count = 0;
 #pragma unroll
-                    for (int w = 0; w < W; ++w) count += slot[w];
-                }
+                for (int w = 0; w < W; ++w) count += slot[w];
                 if (count >= n_select) border = trial;
                 exact = count == n_select;
             }

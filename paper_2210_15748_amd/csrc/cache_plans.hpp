@@ -92,7 +92,7 @@ inline size_t select_workspace(uint64_t tokens, uint64_t heads, uint64_t table_p
 
 // ---- pages ------------------------------------------------------------------------------------------------------------------
 struct AdvancePlan {
-    size_t writers, lowest, stays, free_pages, copies, totals, bytes;
+    size_t writers, lowest, stays, free_pages, copies, bytes;
 };
 inline AdvancePlan advance_plan(uint64_t pages, uint64_t seqs) {
     AdvancePlan p{};
@@ -102,7 +102,6 @@ inline AdvancePlan advance_plan(uint64_t pages, uint64_t seqs) {
         at += (n + 255) / 256 * 256;
         return here;
     };
-    p.totals = take(64);
     p.writers = take(pages * 4);
     p.lowest = take(pages * 4);
     p.stays = take(pages * 4);

@@ -44,7 +44,7 @@ int main() {
     for (uint64_t pages = 1; pages <= CACHE_MOST; pages = pages * 3 + 1)
         for (uint64_t n = 0; n <= CACHE_MOST; n = n * 5 + 1) {
             const AdvancePlan p = advance_plan(pages, n);
-            EXPECT(p.writers >= p.totals + 64 && p.lowest >= p.writers + 4 * pages && p.stays >= p.lowest + 4 * pages);
+            EXPECT(p.writers == 0 && p.lowest >= p.writers + 4 * pages && p.stays >= p.lowest + 4 * pages);
             EXPECT(p.free_pages >= p.stays + 4 * pages && p.copies >= p.free_pages + 4 * pages && p.bytes >= p.copies + 8 * n);
             EXPECT(p.bytes <= advance_plan(pages + 7, n + 3).bytes);
             const CompactPlan c = compact_plan(pages);
