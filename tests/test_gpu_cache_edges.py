@@ -214,3 +214,29 @@ def test_whatever_length_is_told(ix, told, new):
     room = torch.empty(dz.cache_attention_workspace_bytes(ix, taken(ix, g), more, 2), dtype=torch.uint8, device=DEV)
     again = dz.cache_attention(ix, taken(ix, g), b, q.to(DEV), workspace=room)
     assert torch.equal(again[0], out) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("scale", [0.125, -0.07, 0.0])
+def test_many_queries_of_every_size(ix, dtype, page, scale):
+    """More than 64 rows a head: large and small rows, rows of zeros, infinities and NaN, scales of either sign."""
+    lengths, new = [100, 164], [90, 77]
+    pages = sum(-(-m // page) for m in lengths)
+    c = plain.make_cache(pages, 2, page, 64, 4)
+    tables = plain.make_tables(lengths, page, pages, 4)
+    q = torch.randn(167, 4, 64, generator=torch.Generator().manual_seed(4))
+    q[:, 0] *= 60.0
+    q[:, 1] *= 1e-30 if dtype == torch.bfloat16 else 1e-4
+    q[0, 2] = 0
+    q[-1, 3, 5] = math.inf
+    q[0, 3, 5] = math.nan
+    q = q.to(dtype)
+    g = on_gpu(c)
+    for window in (0, 20):
+        out, lse = dz.cache_attention(ix, taken(ix, g), batch_of(ix, tables, lengths, new), q.to(DEV), scale, window=window)
+        close(out, lse, plain.attend(c, tables, lengths, new, q, scale, window), dtype, 164, 64)
+    if dtype == torch.bfloat16 and scale:
+        big = (q.float().nan_to_num(0, 0, 0) * 1e30).to(dtype)
+        out, lse = dz.cache_attention(ix, taken(ix, g), batch_of(ix, tables, lengths, new), big.to(DEV), scale * 1e-31)
+        close(out, lse, plain.attend(c, tables, lengths, new, big, scale * 1e-31), dtype, 164, 64)
