@@ -378,7 +378,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
 // ---- many rows: 128 or 256 to a workgroup, 32 to a wave, all over the same steps of 64 tokens ---------------------------------------
 // Keys and values are converted once for the workgroup's waves on their way into LDS, two steps' worth of it: while one is computed
 // with, the next one's codes are under way from memory.  Rows in LDS are 16 bytes apart from a multiple of their length: a wave's 16-byte
-// reads then spread over all banks.  3584 tokens of 32 heads of 128 channels over up to 8192 (350 GFLOP): 436 to 500 us, 700 to 800 TFLOP/s; matrix cores
+// reads then spread over all banks.  3584 tokens of 32 heads of 128 channels over up to 8192 (350 GFLOP): 436 to 500 us by card, 700 to 800 TFLOP/s; matrix cores
 // 31 % busy, vector ALU 48 % (32 exponentials a lane and step, the codes' conversion), mostly one after the other.
 // ONE: a step lies on one page (of 64 tokens or more), so its page and scales are the same for all.
 template <int ND, int W, bool ONE>
