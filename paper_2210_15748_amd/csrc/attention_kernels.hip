@@ -33,10 +33,30 @@ __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // In a branch: keeps the compiler from working it out for all and choosing afterwards.
 __device__ inline void rarely() { asm volatile("; seldom"); }
 
-// What e^(s - m) is multiplied by to be a part of P.  (The exponent passes 120 only with scales that are 2^100 apart.)
-__device__ inline float p_factor(float vs, float m, float top) {
-    return vs * exp2_fast(fminf((m == NEVER ? 0.f : m) - (top == NEVER ? 0.f : top) + P_TOP, 120.f));
-}
+// A value scale as part * 2^power, 0.5 <= part < 1 (parts of 0, infinities and NaN are what they are): m - top is about -log2(v_scale), and what it is
+// raised to stays in range only beside the scale's own power, which also makes subnormal scales ordinary ones.
+struct ValueScale {
+    float part, power;
+    __device__ explicit ValueScale(float vs) : part(__builtin_amdgcn_frexp_mantf(vs)), power((float)__builtin_amdgcn_frexp_expf(vs)) {}
+    // log2 of what it makes of a largest s log2(e)
+    __device__ float raised(float peak) const { return part < __builtin_huge_valf() ? peak + (__builtin_amdgcn_logf(part) + power) : NEVER; }
+    // What e^(s - m) is multiplied by to be a part of P.
+    __device__ float factor(float m, float top) const {
+        return part * exp2_fast(fminf(power + ((m == NEVER ? 0.f : m) - (top == NEVER ? 0.f : top)) + P_TOP, 120.f));
+    }
+};
+
+// 2^x as part * 2^power, 1 <= part < 2: what is multiplied by both in turn is rounded once, below the normal numbers too.
+struct Power {
+    float part;
+    int power;
+    __device__ explicit Power(float x) {
+        x = fmaxf(x, -1000.f);
+        const float n = floorf(x);
+        part = exp2_fast(x - n);
+        power = (int)n;
+    }
+};
 
 // The larger of a lane's and the one 32 lanes on.
 __device__ inline float over_halves(float x) {
@@ -289,7 +309,8 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) peak = fmaxf(peak, s[t][i]);
-        float high = vs < __builtin_huge_valf() ? peak + __builtin_amdgcn_logf(vs) : NEVER;
+        const ValueScale value(vs);
+        float high = value.raised(peak);
         high = fmaxf(high, __shfl_xor(high, 16));
         high = fmaxf(high, __shfl_xor(high, 32));
         peak = fmaxf(peak, __shfl_xor(peak, 16));
@@ -306,7 +327,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
             top = top_new;
         }
         const float base = m == NEVER ? 0.f : m;
-        const float weight = p_factor(vs, m, top);
+        const float weight = value.factor(m, top);
         half8 p[2];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -343,9 +364,11 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     for (int w = 0; w < W; ++w) most = fmaxf(most, sums[w][r][0]);
 #pragma unroll
     for (int w = 0; w < W; ++w) total += sums[w][r][1] * (sums[w][r][0] == most ? 1.f : exp2_fast(sums[w][r][0] - most));
-    const float mine = exp2_fast(top - P_TOP - (most == NEVER ? 0.f : most));
+    const Power mine(top - P_TOP - (most == NEVER ? 0.f : most));
 #pragma unroll
-    for (int d = 0; d < NV; ++d) o[d] *= mine;
+    for (int d = 0; d < NV; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[d][i] = ldexpf(o[d][i] * mine.part, mine.power);
 #pragma unroll
     for (int half = W / 2; half >= 1; half /= 2) {
         if (wave >= half && wave < 2 * half)
@@ -561,7 +584,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
             for (int i = 1; i < 32 / NG; ++i) x = fmaxf(x, s[(8 * j + i) / 16][(8 * j + i) % 16]);
             x *= by[j];
             peak = fmaxf(peak, x);
-            high = fmaxf(high, weight[j] < __builtin_huge_valf() ? x + __builtin_amdgcn_logf(weight[j]) : NEVER);
+            high = fmaxf(high, ValueScale(weight[j]).raised(x));
         }
         peak = over_halves(peak);
         high = over_halves(high);
@@ -582,7 +605,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         }
         const float base = m == NEVER ? 0.f : m;
 #pragma unroll
-        for (int j = 0; j < NG; ++j) weight[j] = p_factor(weight[j], m, top);
+        for (int j = 0; j < NG; ++j) weight[j] = ValueScale(weight[j]).factor(m, top);
         half8 p[4];
         // A step's P and sums from the same exponentials e^(s - m) weight where the weight is an ordinary number for all rows and the keys' scale
         // one at all, otherwise (scales very far apart, or 0, or no numbers) from e^(s - m).
@@ -641,7 +664,8 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     }
     l += __shfl_xor(l, 32);
     if (!there) return;
-    const float by = exp2_fast(top - P_TOP - (m == NEVER ? 0.f : m)) * (a.parts == 1 ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
+    const Power mine(top - P_TOP - (m == NEVER ? 0.f : m));
+    const float by = mine.part * (a.parts == 1 ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
     const uint64_t at = (uint64_t)token * q_heads + q_head;
     const uint64_t slot = (((uint64_t)unit_head * a.tiles + tile) * a.parts + part) * ROWS + wave * 32 + r;
 #pragma unroll
@@ -649,7 +673,9 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int ch = 32 * d + 8 * j + 4 * (int)h;
-            const float y[4] = {o[d][4 * j] * by, o[d][4 * j + 1] * by, o[d][4 * j + 2] * by, o[d][4 * j + 3] * by};
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = ldexpf(o[d][4 * j + i] * by, mine.power);
             if (a.parts == 1) store_out(a.out, at * D + ch, a.dtype, y);
             else __builtin_memcpy(a.part_out + slot * D + ch, y, 16);
         }

@@ -1,0 +1,59 @@
+"""Attention over the paged cache with scales of every size: outputs that bfloat16 holds come out right whatever the scales are."""
+import math
+
+import pytest
+import torch
+
+import paper_2210_15748_amd as dz
+
+import cache_plain as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NAMES = ("k", "v", "ks", "vs", "bounds")
+
+
+@pytest.fixture(scope="module")
+def ix():
+    return dz.create(128, 32, 7, seed=1)
+
+
+# (lengths, new tokens, query heads of a key head): one workgroup of eight waves; split and joined, by a wave a row; split far, joined by a workgroup
+# a row; many rows in one part; many rows split
+FORMS = {"few": ([700, 333], [1, 1], 2), "few split": ([3000, 90], [1, 3], 2), "few split far": ([9000], [1], 1), "many": ([250, 200], [90, 60], 2),
+         "many split": ([1500, 300], [70, 70], 2)}
+
+
+def check(ix, c, lengths, new, group, page, scale=0.125, q=None, window=0):
+    P, H, _, D = c["k"].shape
+    tables = plain.make_tables(lengths, page, P, 3)
+    if q is None:
+        q = torch.randn(sum(new), H * group, D, generator=torch.Generator().manual_seed(5)).to(torch.bfloat16)
+    want = plain.attend(c, tables, lengths, new, q, scale, window)
+    b = dz.cache_batch(ix, tables.to(DEV), torch.tensor(lengths, dtype=torch.int32, device=DEV), plain.starts_of(new).to(DEV), n_tokens=sum(new),
+                       max_tokens=max(new), max_length=max(lengths))
+    g = {k: v.to(DEV) for k, v in c.items()}
+    out, lse = dz.cache_attention(ix, dz.cache(ix, *(g[n] for n in NAMES)), b, q.to(DEV), scale, window=window)
+    t_out, t_lse = plain.attend_tolerance(*want, torch.bfloat16, max(lengths), D)
+    t_out = t_out + 2.0 ** -134      # half the step of bfloat16's subnormal numbers (32-bit ones': 2^-150 an addition)
+    out, lse = out.cpu().double(), lse.cpu().double()
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    assert bool(((out - want[0]).abs() <= t_out).all()), float(((out - want[0]).abs() / t_out).max())
+    assert bool(((lse - want[1]).abs() <= t_lse).all()), float(((lse - want[1]).abs() / t_lse).max())
+    return want[0]
+
+
+def pool(lengths, page, dim, seed=4):
+    return plain.make_cache(sum(-(-n // page) for n in lengths), 1, page, dim, seed)
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("power", [-104, -108, -110, -113, -118, -126, -133])
+def test_small_value_scales(ix, form, page, power):
+    lengths, new, group = FORMS[form]
+    c = pool(lengths, page, 64)
+    c["vs"] = torch.ldexp(c["vs"] / 0.022, torch.tensor(power))
+    assert float(c["vs"].max()) < 2.0 ** power and bool((c["vs"] > 0).all())
+    want = check(ix, c, lengths, new, group, page)
+    assert float(want.abs().max()) > 2.0 ** power
