@@ -364,7 +364,8 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     for (int w = 0; w < W; ++w) most = fmaxf(most, sums[w][r][0]);
 #pragma unroll
     for (int w = 0; w < W; ++w) total += sums[w][r][1] * (sums[w][r][0] == most ? 1.f : exp2_fast(sums[w][r][0] - most));
-    const Power mine(top - P_TOP - (most == NEVER ? 0.f : most));
+    Power mine(top - P_TOP - (most == NEVER ? 0.f : most));
+    mine.part *= total == 0.f ? 0.f : 1.f / total;      // means, of a part too: sums may pass the largest number where the values are near it
 #pragma unroll
     for (int d = 0; d < NV; ++d)
 #pragma unroll
@@ -383,10 +384,9 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     if (wave != 0 || tile * 16 + r >= u.rows) return;
     if (a.parts == 1) {
         const uint64_t at = (uint64_t)token * q_heads + q_head;
-        const float by = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
         for (int d = 0; d < NV; ++d) {
-            const float y[4] = {o[d][0] * by, o[d][1] * by, o[d][2] * by, o[d][3] * by};
+            const float y[4] = {o[d][0], o[d][1], o[d][2], o[d][3]};
             store_out(a.out, at * D + 16 * d + 4 * g, a.dtype, y);
         }
         if (a.lse && g == 0) a.lse[at] = total == 0.f ? NEVER : (most + log2f(total)) * LN2;
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     l += __shfl_xor(l, 32);
     if (!there) return;
     const Power mine(top - P_TOP - (m == NEVER ? 0.f : m));
-    const float by = mine.part * (a.parts == 1 ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
+    const float by = mine.part * (l == 0.f ? 0.f : 1.f / l);      // means, of a part too
     const uint64_t at = (uint64_t)token * q_heads + q_head;
     const uint64_t slot = (((uint64_t)unit_head * a.tiles + tile) * a.parts + part) * ROWS + wave * 32 + r;
 #pragma unroll
@@ -718,26 +718,26 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
     m = over_workgroup(m, true, most4);
     for (uint32_t i = threadIdx.x; i < parts; i += 256) {
         const float2 s = a.part_sums[slot0 + (uint64_t)i * rows];
-        const float f = s.x == m ? 1.f : exp2_fast(s.x - m);
+        const float f = (s.x == m ? 1.f : exp2_fast(s.x - m)) * s.y;
         factors[i] = f;
-        l += s.y * f;
+        l += f;
     }
     l = over_workgroup(l, false, sum4);
+    const float by = l == 0.f ? 0.f : 1.f / l;
     const uint32_t part0 = threadIdx.x / per, d = threadIdx.x % per * 4;
     f32x4 x = {};
     if (part0 < lanes) {
         const float* from = a.part_out + slot0 * D + d;
         const uint64_t apart = (uint64_t)rows * D;
 #pragma unroll 4
-        for (uint32_t i = part0; i < parts; i += lanes) x += *(const f32x4*)(from + i * apart) * factors[i];
+        for (uint32_t i = part0; i < parts; i += lanes) x += *(const f32x4*)(from + i * apart) * (factors[i] * by);
     }
     joined[threadIdx.x] = x;
     barrier();
     if (part0 != 0) return;
     for (uint32_t i = 1; i < lanes; ++i) x += joined[i * per + threadIdx.x];
     const uint64_t at = (uint64_t)(u.first_token + row / a.group) * (a.cache.heads * a.group) + u.head * a.group + row % a.group;
-    const float by = l == 0.f ? 0.f : 1.f / l;
-    const float y[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
+    const float y[4] = {x[0], x[1], x[2], x[3]};
     store_out(a.out, at * D + d, a.dtype, y);
     if (a.lse && d == 0) a.lse[at] = l == 0.f ? NEVER : (m + log2f(l)) * LN2;
 }
@@ -761,11 +761,12 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
     m = __shfl(m, 0);
-    const float f = lane >= parts ? 0.f : s.x == m ? 1.f : exp2_fast(s.x - m);
-    float l = s.y * f;
+    float f = lane >= parts ? 0.f : (s.x == m ? 1.f : exp2_fast(s.x - m)) * s.y;
+    float l = f;
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) l += __shfl_xor(l, o);
     l = __shfl(l, 0);
+    f *= l == 0.f ? 0.f : 1.f / l;
     // of heads of up to 128 channels each half of the wave sees to every other part
     const uint32_t halves = per <= 32 ? 2 : 1, half = halves == 2 ? lane >> 5 : 0, at4 = halves == 2 ? lane & 31 : lane;
     f32x4 x = {};
@@ -789,8 +790,7 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
         for (int i = 0; i < 4; ++i) x[i] += __shfl_xor(x[i], 32);
     if (half || at4 >= per) return;
     const uint64_t at = (uint64_t)(u.first_token + row / a.group) * (a.cache.heads * a.group) + u.head * a.group + row % a.group;
-    const float by = l == 0.f ? 0.f : 1.f / l;
-    const float y[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
+    const float y[4] = {x[0], x[1], x[2], x[3]};
     store_out(a.out, at * D + lane * 4, a.dtype, y);
     if (a.lse && lane == 0) a.lse[at] = l == 0.f ? NEVER : (m + log2f(l)) * LN2;
 }

@@ -329,7 +329,7 @@ struct AttendArgs {
     void* out;                 // [tokens][heads * group][dim]
     float* lse;                // [tokens][heads * group] or nullptr
     uint32_t parts, part_chunks, tiles;
-    float* part_out;           // [workgroups][parts][rows][dim]
+    float* part_out;           // [workgroups][parts][rows][dim], a part's means
     float2* part_sums;         // [workgroups][parts][rows] maximum (in powers of two), sum
 };
 hipError_t launch_cache_attention(AttendArgs a, const AttendPlan& p, void* workspace, hipStream_t stream);

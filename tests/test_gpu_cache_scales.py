@@ -57,3 +57,16 @@ def test_small_value_scales(ix, form, page, power):
     assert float(c["vs"].max()) < 2.0 ** power and bool((c["vs"] > 0).all())
     want = check(ix, c, lengths, new, group, page)
     assert float(want.abs().max()) > 2.0 ** power
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("power", [100, 112, 120])
+def test_large_value_scales(ix, form, page, power):
+    """Values near the largest that bfloat16 holds: their mean is one of them, though their sum is none."""
+    lengths, new, group = FORMS[form]
+    c = pool(lengths, page, 64)
+    c["vs"] = torch.ldexp(c["vs"] / 0.022, torch.tensor(power))
+    c["v"] = c["v"].abs()
+    q = torch.zeros(sum(new), group, 64, dtype=torch.bfloat16)
+    check(ix, c, lengths, new, group, page, q=q)
