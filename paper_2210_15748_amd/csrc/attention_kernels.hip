@@ -38,25 +38,40 @@ __device__ inline void rarely() { asm volatile("; seldom"); }
 struct ValueScale {
     float part, power;
     __device__ explicit ValueScale(float vs) : part(__builtin_amdgcn_frexp_mantf(vs)), power((float)__builtin_amdgcn_frexp_expf(vs)) {}
+    __device__ float log2() const { return __builtin_amdgcn_logf(part) + power; }
     // log2 of what it makes of a largest s log2(e)
-    __device__ float raised(float peak) const { return part < __builtin_huge_valf() ? peak + (__builtin_amdgcn_logf(part) + power) : NEVER; }
+    __device__ float raised(float peak) const { return part < __builtin_huge_valf() ? peak + log2() : NEVER; }
     // What e^(s - m) is multiplied by to be a part of P.
     __device__ float factor(float m, float top) const {
-        return part * exp2_fast(fminf(power + ((m == NEVER ? 0.f : m) - (top == NEVER ? 0.f : top)) + P_TOP, 120.f));
+        return part * exp2_fast(power + ((m == NEVER ? 0.f : m) - (top == NEVER ? 0.f : top)) + P_TOP);
     }
+    // The same for one s log2(e) without that factor, which may be too large for a float where e^(s - m) is too small for one.  (Parts of 0
+    // may come with any exponent, others with none above P_TOP + SLACK + 1.)
+    __device__ float weight(float s, float top) const { return part * exp2_fast(fminf(s + (power - (top == NEVER ? 0.f : top) + P_TOP), 100.f)); }
 };
+// With factors below this P comes of products with e^(s - m): where that is below the normal numbers, they are nothing in fp16.
+constexpr float MOST_FACTOR = 0x1p100f;
 
-// 2^x as part * 2^power, 1 <= part < 2: what is multiplied by both in turn is rounded once, below the normal numbers too.
+// 2^x as part * 2^power, 1 <= part < 2: what is multiplied by both in turn may be as large as 2^x is small.
 struct Power {
     float part;
     int power;
+    Power() = default;
+    __device__ Power(float part, int power) : part(part), power(power) {}
     __device__ explicit Power(float x) {
         x = fmaxf(x, -1000.f);
         const float n = floorf(x);
         part = exp2_fast(x - n);
         power = (int)n;
     }
+    __device__ float as_float() const { return ldexpf(part, power); }
 };
+
+__device__ inline f32x4 times(f32x4 x, const Power& p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = ldexpf(x[i] * p.part, p.power);
+    return x;
+}
 
 // The larger of a lane's and the one 32 lanes on.
 __device__ inline float over_halves(float x) {
@@ -329,20 +344,24 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         const float base = m == NEVER ? 0.f : m;
         const float weight = value.factor(m, top);
         half8 p[2];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float e = exp2_fast(s[t][i] - base);
-                l += e;
-                p[t / 2][t % 2 * 4 + i] = (f16_t)(e * weight);
-            }
-        if (!whole && !(fabsf(weight) < __builtin_huge_valf())) {
-            rarely();      // what is not seen may have any scale
+        if (__any(!(fabsf(weight) < MOST_FACTOR))) {
+            rarely();      // scales very far apart, or no numbers; what is not seen may have any scale
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[t / 2][t % 2 * 4 + i] = s[t][i] == NEVER ? (f16_t)0.f : p[t / 2][t % 2 * 4 + i];
+                for (int i = 0; i < 4; ++i) {
+                    l += exp2_fast(s[t][i] - base);
+                    p[t / 2][t % 2 * 4 + i] = s[t][i] == NEVER ? (f16_t)0.f : (f16_t)value.weight(s[t][i], top);
+                }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e = exp2_fast(s[t][i] - base);
+                    l += e;
+                    p[t / 2][t % 2 * 4 + i] = (f16_t)(e * weight);
+                }
         }
 #pragma unroll
         for (int d = 0; d < NV; ++d) {
@@ -367,9 +386,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     Power mine(top - P_TOP - (most == NEVER ? 0.f : most));
     mine.part *= total == 0.f ? 0.f : 1.f / total;      // means, of a part too: sums may pass the largest number where the values are near it
 #pragma unroll
-    for (int d = 0; d < NV; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[d][i] = ldexpf(o[d][i] * mine.part, mine.power);
+    for (int d = 0; d < NV; ++d) o[d] = times(o[d], mine);
 #pragma unroll
     for (int half = W / 2; half >= 1; half /= 2) {
         if (wave >= half && wave < 2 * half)
@@ -553,13 +570,13 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         }
         // behind the barrier nobody reads the other buffer: the next step goes there beside the products (behind the last step nothing of use)
         put(buffer ^ 1);
-        float by[NG], weight[NG];
+        float by[NG], scale[NG], weight[NG];
         uint32_t gone = absent;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
             by[j] = ks[j] * factor;
             by[j] = by[j] < LEAST_SCALE ? LEAST_SCALE : by[j];
-            weight[j] = vs[j];
+            scale[j] = vs[j];
         }
         next();
         fetch(c + 2);
@@ -584,7 +601,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
             for (int i = 1; i < 32 / NG; ++i) x = fmaxf(x, s[(8 * j + i) / 16][(8 * j + i) % 16]);
             x *= by[j];
             peak = fmaxf(peak, x);
-            high = fmaxf(high, ValueScale(weight[j]).raised(x));
+            high = fmaxf(high, ValueScale(scale[j]).raised(x));
         }
         peak = over_halves(peak);
         high = over_halves(high);
@@ -605,7 +622,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         }
         const float base = m == NEVER ? 0.f : m;
 #pragma unroll
-        for (int j = 0; j < NG; ++j) weight[j] = ValueScale(weight[j]).factor(m, top);
+        for (int j = 0; j < NG; ++j) weight[j] = ValueScale(scale[j]).factor(m, top);
         half8 p[4];
         // A step's P and sums from the same exponentials e^(s - m) weight where the weight is an ordinary number for all rows and the keys' scale
         // one at all, otherwise (scales very far apart, or 0, or no numbers) from e^(s - m).
@@ -622,37 +639,48 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
                 }
             l += (part[0] + part[1] + (part[2] + part[3])) / weight[0];
         } else {
+            bool ordinary = true;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) ordinary &= fabsf(weight[j]) < MOST_FACTOR && fabsf(by[j]) < __builtin_huge_valf();
+            const bool apart = !__all(ordinary);
+            float base_of = base;
+            if (apart) {
+                rarely();      // scales very far apart, or no numbers; what is not seen may have any scale: P's exponents in place of the scores
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float value = scale[ONE ? 0 : j];
+                    asm volatile("" : "+s"(value));      // taken apart again here rather than kept in registers from above
+                    const float shift = ValueScale(value).log2() + (P_TOP - (top == NEVER ? 0.f : top));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float x = s[j / 2][j % 2 * 8 + i];
+                        const bool shown = x != NEVER;
+                        x *= by[ONE ? 0 : j];
+                        l += shown ? exp2_fast(x - base) : 0.f;
+                        x = shown ? x + shift : NEVER;
+                        s[j / 2][j % 2 * 8 + i] = x;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < NG; ++j) by[j] = weight[j] = 1.f;
+                base_of = 0.f;
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float e = exp2_fast(fmaf(s[j / 2][j % 2 * 8 + i], by[ONE ? 0 : j], -base));
+                    const float e = exp2_fast(fmaf(s[j / 2][j % 2 * 8 + i], by[ONE ? 0 : j], -base_of));
                     s[j / 2][j % 2 * 8 + i] = e;
                     p[j][i] = (f16_t)(e * weight[ONE ? 0 : j]);
                 }
-            if (!inside) {
-                float sum = 0.f;
+            if (!apart) {
 #pragma unroll
-                for (int j = 0; j < NG; ++j) sum += fabsf(weight[j]) + fabsf(by[j]);
-                if (__any(!(sum < __builtin_huge_valf()))) {      // what is not seen may have any scale
-                    rarely();
+                for (int j = 0; j < 4; ++j) {
+                    float part = 0.f;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int32_t at = from + 16 * j + 8 * (int32_t)h + i;
-                            const bool shown = (at <= pos) & (at >= least) & !(gone >> j & 1);
-                            s[j / 2][j % 2 * 8 + i] = shown ? s[j / 2][j % 2 * 8 + i] : 0.f;
-                            p[j][i] = shown ? p[j][i] : (f16_t)0.f;
-                        }
+                    for (int i = 0; i < 8; ++i) part += s[j / 2][j % 2 * 8 + i];
+                    l += part;
                 }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float part = 0.f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) part += s[j / 2][j % 2 * 8 + i];
-                l += part;
             }
         }
 #pragma unroll
@@ -700,7 +728,8 @@ __device__ inline float over_workgroup(float x, bool max, float* parts) {
 
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t rows, uint32_t used) {
     __shared__ f32x4 joined[256];
-    __shared__ float factors[MOST_PARTS], most4[4], sum4[4];
+    __shared__ Power factors[MOST_PARTS];
+    __shared__ float most4[4], sum4[4];
     const uint32_t D = a.cache.dim, per = D / 4, lanes = 256 / per;
     uint32_t id = blockIdx.x;
     const uint32_t rr = id % used;       // used: rows of a workgroup that a unit can have
@@ -718,9 +747,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
     m = over_workgroup(m, true, most4);
     for (uint32_t i = threadIdx.x; i < parts; i += 256) {
         const float2 s = a.part_sums[slot0 + (uint64_t)i * rows];
-        const float f = (s.x == m ? 1.f : exp2_fast(s.x - m)) * s.y;
+        Power f(s.x == m ? 0.f : s.x - m);
+        f.part *= s.y;
         factors[i] = f;
-        l += f;
+        l += f.as_float();
     }
     l = over_workgroup(l, false, sum4);
     const float by = l == 0.f ? 0.f : 1.f / l;
@@ -730,7 +760,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
         const float* from = a.part_out + slot0 * D + d;
         const uint64_t apart = (uint64_t)rows * D;
 #pragma unroll 4
-        for (uint32_t i = part0; i < parts; i += lanes) x += *(const f32x4*)(from + i * apart) * (factors[i] * by);
+        for (uint32_t i = part0; i < parts; i += lanes) x += times(*(const f32x4*)(from + i * apart), Power{factors[i].part * by, factors[i].power});
     }
     joined[threadIdx.x] = x;
     barrier();
@@ -761,12 +791,13 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
     m = __shfl(m, 0);
-    float f = lane >= parts ? 0.f : (s.x == m ? 1.f : exp2_fast(s.x - m)) * s.y;
-    float l = f;
+    Power f(s.x == m ? 0.f : s.x - m);
+    f.part *= s.y;
+    float l = f.as_float();
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) l += __shfl_xor(l, o);
     l = __shfl(l, 0);
-    f *= l == 0.f ? 0.f : 1.f / l;
+    f.part *= l == 0.f ? 0.f : 1.f / l;
     // of heads of up to 128 channels each half of the wave sees to every other part
     const uint32_t halves = per <= 32 ? 2 : 1, half = halves == 2 ? lane >> 5 : 0, at4 = halves == 2 ? lane & 31 : lane;
     f32x4 x = {};
@@ -781,8 +812,8 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
         for (uint32_t j = 0; j < 8; ++j)
             if (j < 8 / halves) {
                 const uint32_t i = i0 + j * halves + half;
-                const float by = __shfl(f, i & 63);
-                if (i < parts) x += v[j] * by;
+                const Power by{__shfl(f.part, i & 63), __shfl(f.power, i & 63)};
+                if (i < parts) x += times(v[j], by);
             }
     }
     if (halves == 2)

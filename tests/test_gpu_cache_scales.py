@@ -70,3 +70,25 @@ def test_large_value_scales(ix, form, page, power):
     c["v"] = c["v"].abs()
     q = torch.zeros(sum(new), group, 64, dtype=torch.bfloat16)
     check(ix, c, lengths, new, group, page, q=q)
+
+
+# Powers of two of two kinds of pages' value scales, and of e^s on the second kind's keys (1 on the first's)
+APART = [(-20, 20, -30), (-63, 63, -120), (-100, 20, -115), (0, 119, -124), (-75, 75, -145), (-110, 100, -205)]
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("small,large,depth", APART)
+def test_value_scales_far_apart_that_scores_make_up_for(ix, form, page, small, large, depth):
+    """Keys with next to no weight and values so large that they count all the same, among keys with all the weight and small values."""
+    lengths, new, group = FORMS[form]
+    c = pool(lengths, page, 64)
+    g = torch.Generator().manual_seed(depth)
+    P = c["k"].shape[0]
+    second = torch.rand(P, generator=g) < 0.4
+    c["k"][:] = 0
+    c["k"][second] = -127
+    c["ks"][:] = -depth * math.log(2.0) / (127 * 64 * 0.125)
+    c["vs"] = torch.ldexp(c["vs"] / 0.022, torch.where(second, large, small)[:, None])
+    q = torch.ones(sum(new), group, 64, dtype=torch.bfloat16)
+    check(ix, c, lengths, new, group, page, q=q)
