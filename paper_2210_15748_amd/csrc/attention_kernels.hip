@@ -52,6 +52,12 @@ struct ValueScale {
 // With factors below this P comes of products with e^(s - m): where that is below the normal numbers, they are nothing in fp16.
 constexpr float MOST_FACTOR = 0x1p100f;
 
+// A key scale times a call's factor and the power of two that undoes a query row's: rows of tiny numbers over huge keys (or the other way round)
+// have scores of an ordinary size, so no product of two of the three may be rounded to a subnormal number.
+__device__ inline float score_scale(float ks, float factor, int power) {
+    return ldexpf(__builtin_amdgcn_frexp_mantf(ks) * factor, __builtin_amdgcn_frexp_expf(ks) + power);
+}
+
 // 2^x as part * 2^power, 1 <= part < 2: what is multiplied by both in turn may be as large as 2^x is small.
 struct Power {
     float part;
@@ -228,7 +234,8 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     const uint32_t token = u.first_token + row / a.group, q_head = u.head * a.group + row % a.group;
     const int32_t pos = u.begin + (int32_t)(row / a.group);
     const int32_t least = a.window ? max(pos - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
-    float factor;
+    const float factor = a.scale * LOG2E;
+    int power;
     u32x4 raw[ND];
 #pragma unroll
     for (int f = 0; f < ND; ++f)
@@ -287,7 +294,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[f][i] = query_element(x[i], peak, e);
         }
-        factor = ldexpf(a.scale * LOG2E, -e);
+        power = -e;
     }
     for (; c < c1; c += W) {
         // where the scores of this lane lie; a missing page's lie behind every row
@@ -306,7 +313,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         }
         if (c + W < c1) fetch_keys(k_page, key_token(c + W));
         const bool whole = __all(at0 + 15 <= pos && at0 >= least);
-        const float by = ks * factor;
+        const float by = score_scale(ks, factor, power);
         float peak = NEVER;
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[t] *= by;
@@ -460,7 +467,8 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     const int32_t least_last = a.window ? max(pos_last - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
 
     half8 q[D / 16];
-    float factor;
+    const float factor = fabsf(a.scale) * LOG2E;
+    int power;
     {
         u32x4 raw[D / 16];
 #pragma unroll
@@ -480,7 +488,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[f][i] = query_element(a.scale < 0.f ? -x[i] : x[i], peak, e);
         }
-        factor = ldexpf(fabsf(a.scale) * LOG2E, -e);
+        power = -e;
     }
 
     // a step's codes: `PER` runs of 16 keys' channels and 16 values' tokens a thread; the pages of its four 16 tokens and their scales
@@ -574,7 +582,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         uint32_t gone = absent;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            by[j] = ks[j] * factor;
+            by[j] = score_scale(ks[j], factor, power);
             by[j] = by[j] < LEAST_SCALE ? LEAST_SCALE : by[j];
             scale[j] = vs[j];
         }

@@ -92,3 +92,16 @@ def test_value_scales_far_apart_that_scores_make_up_for(ix, form, page, small, l
     c["vs"] = torch.ldexp(c["vs"] / 0.022, torch.where(second, large, small)[:, None])
     q = torch.ones(sum(new), group, 64, dtype=torch.bfloat16)
     check(ix, c, lengths, new, group, page, q=q)
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("q_power,k_power", [(-110, 104), (-120, 114), (-122, 116), (-126, 119), (120, -127), (124, -131), (125, -133)])
+def test_queries_and_key_scales_of_opposite_sizes(ix, form, page, q_power, k_power):
+    """Scores of an ordinary size, of tiny queries and huge keys or the other way round."""
+    lengths, new, group = FORMS[form]
+    c = pool(lengths, page, 64)
+    c["ks"] = torch.ldexp(c["ks"] / 0.022, torch.tensor(k_power))
+    q = torch.ldexp(torch.randn(sum(new), group, 64, generator=torch.Generator().manual_seed(5)), torch.tensor(q_power)).to(torch.bfloat16)
+    assert torch.isfinite(q).all()
+    check(ix, c, lengths, new, group, page, q=q)
