@@ -351,7 +351,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         const float base = m == NEVER ? 0.f : m;
         const float weight = value.factor(m, top);
         half8 p[2];
-        if (__any(!(fabsf(weight) < MOST_FACTOR))) {
+        if (__builtin_expect(__any(!(fabsf(weight) < MOST_FACTOR)), 0)) {
             rarely();      // scales very far apart, or no numbers; what is not seen may have any scale
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -578,7 +578,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         }
         // behind the barrier nobody reads the other buffer: the next step goes there beside the products (behind the last step nothing of use)
         put(buffer ^ 1);
-        float by[NG], scale[NG], weight[NG];
+        float by[NG], scale[NG];
         uint32_t gone = absent;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
@@ -629,13 +629,11 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
             for (int d = 0; d < ND; ++d) vf[d] = *(const half8*)&v_tile[buffer][(32 * d + r) * VS + 8 * h];
         }
         const float base = m == NEVER ? 0.f : m;
-#pragma unroll
-        for (int j = 0; j < NG; ++j) weight[j] = ValueScale(scale[j]).factor(m, top);
         half8 p[4];
-        // A step's P and sums from the same exponentials e^(s - m) weight where the weight is an ordinary number for all rows and the keys' scale
-        // one at all, otherwise (scales very far apart, or 0, or no numbers) from e^(s - m).
-        if (ONE && __all(weight[0] > 0x1p-60f && weight[0] < 0x1p60f && by[0] < __builtin_huge_valf())) {
-            const float shift = __builtin_amdgcn_logf(weight[0]) - base;
+        // A step's P and sums from the same exponentials e^(s - m) weight where the weight, 2^(shift + base), is an ordinary number for all rows and the
+        // keys' scale one at all, otherwise (scales very far apart, or 0, or no numbers) from e^(s - m).
+        const float shift = ValueScale(scale[0]).log2() + (P_TOP - (top == NEVER ? 0.f : top));
+        if (ONE && __all(fabsf(shift + base) < 60.f && by[0] < __builtin_huge_valf())) {
             float part[4] = {};
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -645,27 +643,30 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
                     part[j] += e;
                     p[j][i] = (f16_t)e;
                 }
-            l += (part[0] + part[1] + (part[2] + part[3])) / weight[0];
+            l += (part[0] + part[1] + (part[2] + part[3])) * exp2_fast(-shift - base);
         } else {
+            float weight[NG];
+#pragma unroll
+            for (int j = 0; j < NG; ++j) weight[j] = ValueScale(scale[j]).factor(m, top);
             bool ordinary = true;
 #pragma unroll
             for (int j = 0; j < NG; ++j) ordinary &= fabsf(weight[j]) < MOST_FACTOR && fabsf(by[j]) < __builtin_huge_valf();
             const bool apart = !__all(ordinary);
             float base_of = base;
-            if (apart) {
+            if (__builtin_expect(apart, 0)) {
                 rarely();      // scales very far apart, or no numbers; what is not seen may have any scale: P's exponents in place of the scores
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float value = scale[ONE ? 0 : j];
                     asm volatile("" : "+s"(value));      // taken apart again here rather than kept in registers from above
-                    const float shift = ValueScale(value).log2() + (P_TOP - (top == NEVER ? 0.f : top));
+                    const float shift_of = ValueScale(value).log2() + (P_TOP - (top == NEVER ? 0.f : top));
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         float x = s[j / 2][j % 2 * 8 + i];
                         const bool shown = x != NEVER;
                         x *= by[ONE ? 0 : j];
                         l += shown ? exp2_fast(x - base) : 0.f;
-                        x = shown ? x + shift : NEVER;
+                        x = shown ? x + shift_of : NEVER;
                         s[j / 2][j % 2 * 8 + i] = x;
                     }
                 }
