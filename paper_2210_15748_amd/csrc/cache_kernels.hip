@@ -236,10 +236,10 @@ __global__ __launch_bounds__(64 * W) void append_kernel(CachePages c, CacheBatch
 }
 
 // ---- pages by their bounds ----------------------------------------------------------------------------------------------------
-// Scores as numbers that order the same; NaN as high as +inf.  0: no page.
+// Scores as numbers that order the same; NaN as high as +inf, -0 as +0.  0: no page.
 __device__ inline uint32_t ordered(float x) {
     if (!(x == x)) x = __builtin_huge_valf();
-    const uint32_t u = __float_as_uint(x);
+    const uint32_t u = x == 0.f ? 0u : __float_as_uint(x);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 constexpr uint32_t KEY_ALWAYS = 0xFFFFFFFFu;

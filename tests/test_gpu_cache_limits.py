@@ -1,0 +1,46 @@
+"""Calls on the paged cache at the limits of their definitions."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2210_15748_amd as dz
+
+import cache_plain as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NAMES = ("k", "v", "ks", "vs", "bounds")
+
+
+@pytest.fixture(scope="module")
+def ix():
+    return dz.create(128, 32, 7, seed=1)
+
+
+def taken(ix, c):
+    return dz.cache(ix, *(c[n].to(DEV) for n in NAMES))
+
+
+@pytest.mark.parametrize("places", [300, 1500, 5000, 17001])
+@pytest.mark.parametrize("zeros", ["key scales", "query scales", "products"])
+def test_select_takes_either_zero_for_a_tie(ix, places, zeros):
+    """Negative sums times a scale of 0, or of a product that is 0, are -0: no less than the +0 of positive ones, so the lower place goes first."""
+    page = 16
+    c = plain.make_cache(64, 1, page, 32, 5)
+    g = torch.Generator().manual_seed(places)
+    c["bounds"] = torch.sort(c["bounds"], dim=2).values
+    tables = torch.randint(0, 64, (1, places), generator=g, dtype=torch.int32)
+    codes, scales = torch.randint(-127, 128, (2, 32), generator=g, dtype=torch.int8), torch.ones(2)
+    c["bounds"][::2] = torch.where(codes[0] < 0, 100, -100).to(torch.int8)      # every other page's sums are negative for the first row
+    codes[1] = codes[0]
+    if zeros == "key scales":
+        c["ks"][:] = torch.where(torch.rand(64, 1, generator=g) < 0.8, 0.0, 0.5)
+    elif zeros == "query scales":
+        scales[:] = 0.0
+    else:
+        c["ks"][:], scales[:] = 1e-30, 1e-30
+    b = dz.cache_batch(ix, tables.to(DEV), torch.tensor([places * page], dtype=torch.int32, device=DEV))
+    for n_select, first, last in ((1, 0, 0), (places // 3, 0, 0), (places // 2, 2, 3), (places - 1, 0, 0)):
+        want = plain.select(c, tables, [places * page], [1], codes, scales, n_select, first, last)
+        got = dz.cache_select(ix, taken(ix, c), b, codes.to(DEV), scales.to(DEV), n_select, first, last)
+        assert np.array_equal(got.cpu().numpy(), want), n_select
