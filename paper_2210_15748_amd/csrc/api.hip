@@ -1625,7 +1625,7 @@ dessert_status_t dessert_cache_attention(const dessert_index_t* ix, const desser
         if ((uint64_t)a.batch.max_tokens * a.group > CACHE_MOST || units > MAX_WORKGROUPS || units * a.cache.heads > MAX_WORKGROUPS)
             return fail(DESSERT_EINVAL, "too many tokens for one call");
         p = attend_plan(a.batch.n_seqs, a.batch.max_tokens, a.cache.heads, a.group, a.cache.dim, attended(*batch, a.cache.page_tokens, n_select, window), n_select != 0);
-        if (p.groups * p.parts > MAX_WORKGROUPS) return fail(DESSERT_EINVAL, "too many tokens for one call");
+        if (p.groups * p.parts > 0xFFFFFFFFull) return fail(DESSERT_EINVAL, "too many tokens for one call");
         st = check_workspace(workspace_dev, workspace_bytes, p.bytes);
         if (st != DESSERT_OK) return st;
     }

@@ -215,7 +215,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     __shared__ f32x4 joined[W / 2][NV][64];
     __shared__ float sums[W][16][2];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    uint32_t id = blockIdx.x;
+    uint32_t id = a.first + blockIdx.x;
     const uint32_t part = id % a.parts;
     id /= a.parts;
     const uint32_t group_index = id;
@@ -439,8 +439,8 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     // Workgroups go to the 8 XCDs in turn: where the heads of all sequences are a multiple of 8, an XCD gets all tiles of some of them, one after the
     // other, and their keys and values stay in its L2.  A head's longest tiles come first.  (Tiles of a long and a short sequence by turns
     // would be as bad as can be: an XCD's workgroups go to its parts in turn as well, and some would get the long ones only.)
-    uint32_t id = blockIdx.x;
-    const uint32_t unit_heads = gridDim.x / (a.parts * a.tiles), xcds = unit_heads % 8 ? 1 : 8, lane_of = id % xcds;
+    uint32_t id = a.first + blockIdx.x;
+    const uint32_t xcds = a.unit_heads % 8 ? 1 : 8, lane_of = id % xcds;
     id /= xcds;
     const uint32_t tile = a.tiles - 1 - id % a.tiles;
     id /= a.tiles;
@@ -836,8 +836,8 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
 }
 
 template <int ND>
-void launch_attend(const AttendArgs& a, const AttendPlan& p, hipStream_t stream) {
-    const dim3 grid((uint32_t)(p.groups * p.parts));
+void launch_attend(const AttendArgs& a, const AttendPlan& p, uint32_t workgroups, hipStream_t stream) {
+    const dim3 grid(workgroups);
     if (p.few && p.waves == 4) {
         if (a.pages) attend_few_kernel<ND, 4, true><<<grid, dim3(256), 0, stream>>>(a);
         else attend_few_kernel<ND, 4, false><<<grid, dim3(256), 0, stream>>>(a);
@@ -864,18 +864,22 @@ hipError_t launch_cache_attention(AttendArgs a, const AttendPlan& p, void* works
     a.parts = p.parts;
     a.part_chunks = p.part_chunks;
     a.tiles = p.tiles;
+    a.unit_heads = p.units * a.cache.heads;
     a.part_out = (float*)workspace;
     a.part_sums = (float2*)((char*)workspace + p.sums);
-    switch (a.cache.dim / 32) {
-        case 1: launch_attend<1>(a, p, stream); break;
-        case 2: launch_attend<2>(a, p, stream); break;
-        case 3: launch_attend<3>(a, p, stream); break;
-        case 4: launch_attend<4>(a, p, stream); break;
-        case 5: launch_attend<5>(a, p, stream); break;
-        case 6: launch_attend<6>(a, p, stream); break;
-        case 7: launch_attend<7>(a, p, stream); break;
-        default: launch_attend<8>(a, p, stream); break;
-    }
+    attend_launches(p, [&](uint32_t first, uint32_t workgroups) {
+        a.first = first;
+        switch (a.cache.dim / 32) {
+            case 1: launch_attend<1>(a, p, workgroups, stream); break;
+            case 2: launch_attend<2>(a, p, workgroups, stream); break;
+            case 3: launch_attend<3>(a, p, workgroups, stream); break;
+            case 4: launch_attend<4>(a, p, workgroups, stream); break;
+            case 5: launch_attend<5>(a, p, workgroups, stream); break;
+            case 6: launch_attend<6>(a, p, workgroups, stream); break;
+            case 7: launch_attend<7>(a, p, workgroups, stream); break;
+            default: launch_attend<8>(a, p, workgroups, stream); break;
+        }
+    });
     if (p.parts > 1) {
         const uint32_t used = (uint32_t)std::min<uint64_t>(p.rows, (uint64_t)a.group * (a.pages ? 1 : a.batch.max_tokens));
         const uint64_t rows = p.groups * used;

@@ -5,6 +5,8 @@
 
 #include <algorithm>
 
+#include "launch_slices.hpp"
+
 namespace dessert {
 
 constexpr uint32_t CACHE_MIN_PAGE = 16, CACHE_MAX_PAGE = 256, CACHE_MAX_DIM = 256;
@@ -62,7 +64,7 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
     p.groups = (uint64_t)p.units * heads * p.tiles;
     const uint64_t chunks = std::max<uint64_t>(1, divided_up(length, ATTEND_CHUNK));
     const uint64_t target = p.few ? attend_target(true, dim) : attend_target(false, dim) * ATTEND_MANY / p.rows;
-    p.waves = 4;
+    p.waves = p.few ? 4 : p.rows / 32;
     // a part has work for the four waves of a workgroup (one step each) or, of many rows, for a few steps
     uint64_t parts = std::min(std::max<uint64_t>(1, target / std::max<uint64_t>(1, p.groups)), divided_up(chunks, 4));
     // up to 16 steps are done by one workgroup of eight waves rather than split and joined (16 sequences up to 1000 of dim 128: 14.1 us, split 16.0; up
@@ -75,6 +77,12 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
     p.parts = (uint32_t)divided_up(chunks, p.part_chunks);
     if (p.parts > 1) p.bytes = attend_bytes(p.groups * p.parts * p.rows, dim, &p.sums);
     return p;
+}
+
+// The launches of a plan's workgroups: launch(first, workgroups) (groups * parts are fewer than 2^32).
+template <typename F>
+void attend_launches(const AttendPlan& p, F launch) {
+    in_launches(p.groups * p.parts, 1, 64 * p.waves, [&](uint64_t first, uint64_t, uint32_t workgroups) { launch((uint32_t)first, workgroups); });
 }
 
 // What serves every call of these sizes or smaller ones: a call that is split has at most its form's target of workgroups.

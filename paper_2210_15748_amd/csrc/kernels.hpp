@@ -328,7 +328,8 @@ struct AttendArgs {
     float scale;
     void* out;                 // [tokens][heads * group][dim]
     float* lse;                // [tokens][heads * group] or nullptr
-    uint32_t parts, part_chunks, tiles;
+    uint32_t parts, part_chunks, tiles, unit_heads;   // unit_heads: of all units
+    uint32_t first;            // a launch's first workgroup
     float* part_out;           // [workgroups][parts][rows][dim], a part's means
     float2* part_sums;         // [workgroups][parts][rows] maximum (in powers of two), sum
 };

@@ -44,3 +44,29 @@ def test_select_takes_either_zero_for_a_tie(ix, places, zeros):
         want = plain.select(c, tables, [places * page], [1], codes, scales, n_select, first, last)
         got = dz.cache_select(ix, taken(ix, c), b, codes.to(DEV), scales.to(DEV), n_select, first, last)
         assert np.array_equal(got.cpu().numpy(), want), n_select
+
+
+def test_attention_of_more_workgroups_than_a_launch_has(ix):
+    """70 000 sequences with room for 32 768 new tokens each: 9 million workgroups of 512 threads, most of them without work.  Tokens of the first and the
+    last sequences, which different launches see to."""
+    page, D, n, rows = 16, 128, 70000, 32768
+    g = torch.Generator().manual_seed(1)
+    c = plain.make_cache(200, 1, page, D, 3)
+    tables = torch.randint(0, 200, (n, 3), generator=g, dtype=torch.int32)
+    lengths = torch.randint(1, 48, (n,), generator=g, dtype=torch.int32)
+    new = torch.zeros(n, dtype=torch.int32)
+    new[:50] = 1
+    new[-300:] = 1
+    lengths[0], new[0] = 40, 33
+    lengths[-1], new[-1] = 48, 48
+    starts = torch.cat([torch.zeros(1, dtype=torch.int32), new.cumsum(0).to(torch.int32)])
+    used = int(starts[-1])
+    q = torch.randn(rows, 1, D, generator=g).to(torch.float16)
+    b = dz.cache_batch(ix, tables.to(DEV), lengths.to(DEV), starts.to(DEV), n_tokens=rows, max_tokens=rows, max_length=48)
+    out, lse = torch.full((rows, 1, D), 7.0, dtype=torch.float16, device=DEV), torch.full((rows, 1), 7.0, device=DEV)
+    dz.cache_attention(ix, taken(ix, c), b, q.to(DEV), 0.09, out=out, out_lse=lse)
+    some = torch.nonzero(new).flatten()
+    want = plain.attend(c, tables[some], lengths[some].tolist(), new[some].tolist(), q[:used], 0.09)
+    t_out, t_lse = plain.attend_tolerance(*want, torch.float16, 48, D)
+    assert bool(((out[:used].cpu().double() - want[0]).abs() <= t_out).all()) and bool(((lse[:used].cpu().double() - want[1]).abs() <= t_lse).all())
+    assert bool((out[used:] == 7).all()) and bool((lse[used:] == 7).all())
