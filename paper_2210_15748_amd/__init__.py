@@ -789,14 +789,15 @@ def cache_select(ix: Index, cache: Cache, batch: CacheBatch, q_codes: torch.Tens
     n = batch.n_tokens
     q_ptr = _kept(ix, q_codes, (None, cache.dim), "q_codes", _INT8)
     rows = q_codes.shape[0]
-    if n == 0 or rows % n:
+    if rows % n if n else rows:
         raise ValueError(f"q_codes has {rows} rows for {n} tokens")
+    heads = rows // n if n else cache.n_heads      # of no tokens: any number of heads
     s_ptr = _vector(ix, q_scales, rows, "q_scales", made, _FLOAT32)
     n_first, n_last = _size(n_first, "n_first"), _size(n_last, "n_last")
     out = _output(ix, out, (n, cache.n_heads, _size(n_select, "n_select")), "out", made, torch.uint32)
     ws_ptr, ws_bytes = _workspace(ix, workspace, made, cache_select_workspace_bytes, cache, batch)
     _lend(ix, made)
-    _check(lib().dessert_cache_select(ix.handle, cache.address, batch.address, q_ptr, s_ptr, rows // n, n_select, n_first, n_last, ws_ptr, ws_bytes, out.data_ptr()))
+    _check(lib().dessert_cache_select(ix.handle, cache.address, batch.address, q_ptr, s_ptr, heads, n_select, n_first, n_last, ws_ptr, ws_bytes, out.data_ptr()))
     return out
 
 

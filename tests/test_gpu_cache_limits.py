@@ -70,3 +70,28 @@ def test_attention_of_more_workgroups_than_a_launch_has(ix):
     t_out, t_lse = plain.attend_tolerance(*want, torch.float16, 48, D)
     assert bool(((out[:used].cpu().double() - want[0]).abs() <= t_out).all()) and bool(((lse[:used].cpu().double() - want[1]).abs() <= t_lse).all())
     assert bool((out[used:] == 7).all()) and bool((lse[used:] == 7).all())
+
+
+@pytest.mark.parametrize("starts", [False, True])
+def test_batches_without_tokens(ix, starts):
+    """Every call takes them, with starts and without, and changes nothing."""
+    c = {k: v.to(DEV) for k, v in plain.make_cache(6, 2, 16, 32, 1).items()}
+    before = {k: v.clone() for k, v in c.items()}
+    cache = dz.cache(ix, *(c[n] for n in NAMES))
+    i32 = dict(dtype=torch.int32, device=DEV)
+    b = (dz.cache_batch(ix, torch.zeros(3, 2, **i32), torch.full((3,), 9, **i32), torch.zeros(4, **i32), n_tokens=0) if starts
+         else dz.cache_batch(ix, torch.zeros(0, 2, **i32), torch.zeros(0, **i32)))
+    x = torch.zeros(0, 2, 32, dtype=torch.float16, device=DEV)
+    dz.cache_append(ix, cache, b, x, x)
+    codes, scales = torch.zeros(0, 32, dtype=torch.int8, device=DEV), torch.zeros(0, device=DEV)
+    ids = dz.cache_select(ix, cache, b, codes, scales, 5, 1, 1)
+    assert ids.shape == (0, 2, 5) and ids.dtype == torch.uint32
+    given = torch.zeros(0, 2, 5, dtype=torch.uint32, device=DEV)
+    assert dz.cache_select(ix, cache, b, codes, scales, 5, out=given) is given
+    with pytest.raises(ValueError, match="1 rows for 0 tokens"):
+        dz.cache_select(ix, cache, b, torch.zeros(1, 32, dtype=torch.int8, device=DEV), torch.zeros(1, device=DEV), 5)
+    for pages in (None,):
+        out, lse = dz.cache_attention(ix, cache, b, torch.zeros(0, 4, 32, dtype=torch.float16, device=DEV), pages=pages)
+        assert out.shape == (0, 4, 32) and lse.shape == (0, 4)
+    torch.cuda.synchronize()
+    assert all(torch.equal(c[n], before[n]) for n in NAMES)
