@@ -1613,7 +1613,7 @@ dessert_status_t dessert_cache_attention(const dessert_index_t* ix, const desser
     if (st == DESSERT_OK) st = check_group(n_q_heads, a.cache, &a.group);
     if (st == DESSERT_OK) st = check_tokens(q_dev, q_stride, dtype, n_q_heads, a.cache.dim, a.batch.n_tokens, "q_dev");
     if (st != DESSERT_OK) return st;
-    if ((pages_dev != nullptr) != (n_select != 0)) return fail(DESSERT_EINVAL, "pages_dev and n_select go together: both or neither");
+    if (a.batch.n_tokens && (pages_dev != nullptr) != (n_select != 0)) return fail(DESSERT_EINVAL, "pages_dev and n_select go together: both or neither");
     if ((uint64_t)n_select * a.cache.page_tokens > CACHE_MOST) return fail(DESSERT_EINVAL, "n_select is too large");
     if (a.batch.n_tokens && !out_dev) return fail(DESSERT_EINVAL, "out_dev is NULL");
     if ((uintptr_t)out_dev % 2 || (uintptr_t)out_lse_dev % 4 || (uintptr_t)pages_dev % 4)

@@ -90,7 +90,7 @@ def test_batches_without_tokens(ix, starts):
     assert dz.cache_select(ix, cache, b, codes, scales, 5, out=given) is given
     with pytest.raises(ValueError, match="1 rows for 0 tokens"):
         dz.cache_select(ix, cache, b, torch.zeros(1, 32, dtype=torch.int8, device=DEV), torch.zeros(1, device=DEV), 5)
-    for pages in (None,):
+    for pages in (None, ids):
         out, lse = dz.cache_attention(ix, cache, b, torch.zeros(0, 4, 32, dtype=torch.float16, device=DEV), pages=pages)
         assert out.shape == (0, 4, 32) and lse.shape == (0, 4)
     torch.cuda.synchronize()
