@@ -95,3 +95,36 @@ def test_batches_without_tokens(ix, starts):
         assert out.shape == (0, 4, 32) and lse.shape == (0, 4)
     torch.cuda.synchronize()
     assert all(torch.equal(c[n], before[n]) for n in NAMES)
+
+
+def test_compaction_past_32_bit_offsets(ix):
+    """Pages whose codes lie 2^32 bytes and more into the pool, moved lowest to lowest: contents, counts, numbers and tables, each as defined."""
+    page, H, D = 256, 8, 256
+    pages = (1 << 32) // (page * H * D) + 40
+    torch.cuda.empty_cache()
+    i32 = dict(dtype=torch.int32, device=DEV)
+    big = dict(k=torch.zeros(pages, H, page, D, dtype=torch.int8, device=DEV), v=torch.zeros(pages, H, D, page, dtype=torch.int8, device=DEV),
+               ks=torch.zeros(pages, H, device=DEV), vs=torch.zeros(pages, H, device=DEV), bounds=torch.zeros(pages, H, 2, D, dtype=torch.int8, device=DEV))
+    last = pages - 1
+    assert last * page * H * D > 1 << 32
+    held = {1: 1, 3: 2, last - 9: 5, last: 4}        # page: how many tables hold it
+    small = plain.make_cache(len(held), H, page, D, 1)
+    for s, p in enumerate(held):
+        for n in NAMES:
+            big[n][p] = small[n][s].to(DEV)
+    refs = torch.zeros(pages, **i32)
+    for p, n in held.items():
+        refs[p] = n
+    tables = torch.tensor([[last, 3, 1, -1], [3, last - 9, -1, -1], [last, 7, 7, 7]], **i32)      # behind a length anything may stand
+    lengths = torch.tensor([700, 512, 1], **i32)
+    numbers, live = dz.cache_compact(ix, dz.cache(ix, *(big[n] for n in NAMES)), refs, tables, lengths)
+    assert live.tolist() == [4]
+    assert tables.tolist() == [[2, 3, 1, -1], [3, 0, -1, -1], [2, 7, 7, 7]]
+    moved = {1: 1, 3: 3, last - 9: 0, last: 2}
+    want_numbers, want_refs = torch.full((pages,), -1, dtype=torch.int32), torch.zeros(pages, dtype=torch.int32)
+    for s, (p, n) in enumerate(held.items()):
+        want_numbers[p] = moved[p]
+        want_refs[moved[p]] = n
+        for name in NAMES:
+            assert torch.equal(big[name][moved[p]].cpu(), small[name][s]), (p, name)
+    assert torch.equal(numbers.cpu(), want_numbers) and torch.equal(refs.cpu(), want_refs)
