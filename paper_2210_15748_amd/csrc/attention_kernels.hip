@@ -33,30 +33,30 @@ __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // In a branch: keeps the compiler from working it out for all and choosing afterwards.
 __device__ inline void rarely() { asm volatile("; seldom"); }
 
-// A value scale as part * 2^power, 0.5 <= part < 1 (parts of 0, infinities and NaN are what they are): m - top is about -log2(v_scale), and what it is
-// raised to stays in range only beside the scale's own power, which also makes subnormal scales ordinary ones.
-struct ValueScale {
-    float part, power;
-    __device__ explicit ValueScale(float vs) : part(__builtin_amdgcn_frexp_mantf(vs)), power((float)__builtin_amdgcn_frexp_expf(vs)) {}
-    __device__ float log2() const { return __builtin_amdgcn_logf(part) + power; }
-    // log2 of what it makes of a largest s log2(e)
-    __device__ float raised(float peak) const { return part < __builtin_huge_valf() ? peak + log2() : NEVER; }
-    // What e^(s - m) is multiplied by to be a part of P.
-    __device__ float factor(float m, float top) const {
-        return part * exp2_fast(power + ((m == NEVER ? 0.f : m) - (top == NEVER ? 0.f : top)) + P_TOP);
-    }
-    // The same for one s log2(e) without that factor, which may be too large for a float where e^(s - m) is too small for one.  (Parts of 0
-    // may come with any exponent, others with none above P_TOP + SLACK + 1.)
-    __device__ float weight(float s, float top) const { return part * exp2_fast(fminf(s + (power - (top == NEVER ? 0.f : top) + P_TOP), 100.f)); }
-};
+// log2 of a scale, a subnormal one too (v_log_f32 takes those for 0).
+__device__ inline float log2_scale(float x) { return __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(x)) + (float)__builtin_amdgcn_frexp_expf(x); }
+
+// A value scale by its logarithm: m - top is about -log2(v_scale), and what is raised to it alone would leave the range of a float with scales that do
+// not.  (A logarithm that is rounded to 2^-17 at most is right to that part of P, which goes on with 2^-11.)
+__device__ inline float or_zero(float x) { return x == NEVER ? 0.f : x; }
+// log2 of what a scale makes of a largest s log2(e); scales that are no numbers raise nothing.
+__device__ inline float raised(float peak, float log2_vs) { return log2_vs < __builtin_huge_valf() ? peak + log2_vs : NEVER; }
+// What e^(s - m) is multiplied by to be a part of P.
+__device__ inline float p_factor(float log2_vs, float m, float top) { return exp2_fast(log2_vs + (or_zero(m) - or_zero(top) + P_TOP)); }
+// What is added to s log2(e) for P's exponent, without that factor, which may be too large for a float where e^(s - m) is too small for one.
+__device__ inline float p_shift(float log2_vs, float top) { return log2_vs + (P_TOP - or_zero(top)); }
 // With factors below this P comes of products with e^(s - m): where that is below the normal numbers, they are nothing in fp16.
 constexpr float MOST_FACTOR = 0x1p100f;
 
 // A key scale times a call's factor and the power of two that undoes a query row's: rows of tiny numbers over huge keys (or the other way round)
 // have scores of an ordinary size, so no product of two of the three may be rounded to a subnormal number.
-__device__ inline float score_scale(float ks, float factor, int power) {
-    return ldexpf(__builtin_amdgcn_frexp_mantf(ks) * factor, __builtin_amdgcn_frexp_expf(ks) + power);
-}
+struct ScoreScale {
+    float part;      // the key scale's, times the factor
+    int power;
+    __device__ ScoreScale(float part, int power) : part(part), power(power) {}
+    __device__ static ScoreScale of(float ks, float factor) { return {__builtin_amdgcn_frexp_mantf(ks) * factor, __builtin_amdgcn_frexp_expf(ks)}; }
+    __device__ float with(int row_power) const { return ldexpf(part, power + row_power); }
+};
 
 // 2^x as part * 2^power, 1 <= part < 2: what is multiplied by both in turn may be as large as 2^x is small.
 struct Power {
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         }
         if (c + W < c1) fetch_keys(k_page, key_token(c + W));
         const bool whole = __all(at0 + 15 <= pos && at0 >= least);
-        const float by = score_scale(ks, factor, power);
+        const float by = ScoreScale::of(ks, factor).with(power);
         float peak = NEVER;
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[t] *= by;
@@ -331,8 +331,8 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) peak = fmaxf(peak, s[t][i]);
-        const ValueScale value(vs);
-        float high = value.raised(peak);
+        const float log2_vs = log2_scale(vs);
+        float high = raised(peak, log2_vs);
         high = fmaxf(high, __shfl_xor(high, 16));
         high = fmaxf(high, __shfl_xor(high, 32));
         peak = fmaxf(peak, __shfl_xor(peak, 16));
@@ -348,8 +348,8 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
             m = m_new;
             top = top_new;
         }
-        const float base = m == NEVER ? 0.f : m;
-        const float weight = value.factor(m, top);
+        const float base = or_zero(m);
+        const float weight = p_factor(log2_vs, m, top);
         half8 p[2];
         if (__builtin_expect(__any(!(fabsf(weight) < MOST_FACTOR)), 0)) {
             rarely();      // scales very far apart, or no numbers; what is not seen may have any scale
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     l += exp2_fast(s[t][i] - base);
-                    p[t / 2][t % 2 * 4 + i] = s[t][i] == NEVER ? (f16_t)0.f : (f16_t)value.weight(s[t][i], top);
+                    p[t / 2][t % 2 * 4 + i] = s[t][i] == NEVER ? (f16_t)0.f : (f16_t)exp2_fast(s[t][i] + p_shift(log2_vs, top));
                 }
         } else {
 #pragma unroll
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     for (int w = 0; w < W; ++w) most = fmaxf(most, sums[w][r][0]);
 #pragma unroll
     for (int w = 0; w < W; ++w) total += sums[w][r][1] * (sums[w][r][0] == most ? 1.f : exp2_fast(sums[w][r][0] - most));
-    Power mine(top - P_TOP - (most == NEVER ? 0.f : most));
+    Power mine(top - P_TOP - or_zero(most));
     mine.part *= total == 0.f ? 0.f : 1.f / total;      // means, of a part too: sums may pass the largest number where the values are near it
 #pragma unroll
     for (int d = 0; d < NV; ++d) o[d] = times(o[d], mine);
@@ -494,7 +494,9 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     // a step's codes: `PER` runs of 16 keys' channels and 16 values' tokens a thread; the pages of its four 16 tokens and their scales
     u32x4 kc[PER], vc[PER];
     uint32_t absent, next_absent;
-    float ks[NG], vs[NG], next_ks, next_vs;
+    float k_part[NG], v_log2[NG], next_ks, next_vs;     // the key scale times the call's factor as part and power of two, the value scale's logarithm
+    int k_power[NG];
+    uint64_t odd;       // scales of the step that are no numbers, or values' of 0
     // A lane keeps the page and the scales of one of the four: vector loads, which come in order with the codes, a step ahead of their use.
     uint32_t own_page = page_at(a.batch, table, (c0 * 64 + 16 * (lane & 3)) >> a.cache.shift, a.cache.n_pages);
     auto fetch = [&](uint32_t c) {
@@ -546,10 +548,14 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     };
     auto next = [&]() {
         absent = next_absent;
+        const ScoreScale k = ScoreScale::of(next_ks, factor);      // by the lane that has the page
+        const float v = log2_scale(next_vs);
+        odd = __ballot(!(fabsf(k.part) < __builtin_huge_valf() && fabsf(v) < __builtin_huge_valf())) & (ONE ? 1 : 15);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            ks[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(next_ks), j));
-            vs[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(next_vs), j));
+            k_part[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(k.part), j));
+            k_power[j] = __builtin_amdgcn_readlane(k.power, j);
+            v_log2[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), j));
         }
     };
 
@@ -578,13 +584,14 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         }
         // behind the barrier nobody reads the other buffer: the next step goes there beside the products (behind the last step nothing of use)
         put(buffer ^ 1);
-        float by[NG], scale[NG];
+        float by[NG], log2_vs[NG];
         uint32_t gone = absent;
+        const bool numbers = odd == 0;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            by[j] = score_scale(ks[j], factor, power);
+            by[j] = ScoreScale(k_part[j], k_power[j]).with(power);
             by[j] = by[j] < LEAST_SCALE ? LEAST_SCALE : by[j];
-            scale[j] = vs[j];
+            log2_vs[j] = v_log2[j];
         }
         next();
         fetch(c + 2);
@@ -601,15 +608,21 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
                     s[mt][i] = ((at <= pos) & (at >= least) & !(gone >> j & 1)) ? s[mt][i] : NEVER;
                 }
         }
-        float peak = NEVER, high = NEVER;
+        float peak = NEVER, high = NEVER, peaks[NG];
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
             float x = s[j / 2][j % 2 * 8];
 #pragma unroll
             for (int i = 1; i < 32 / NG; ++i) x = fmaxf(x, s[(8 * j + i) / 16][(8 * j + i) % 16]);
-            x *= by[j];
-            peak = fmaxf(peak, x);
-            high = fmaxf(high, ValueScale(scale[j]).raised(x));
+            peaks[j] = x * by[j];
+            peak = fmaxf(peak, peaks[j]);
+            high = fmaxf(high, peaks[j] + log2_vs[j]);
+        }
+        if (!numbers) {
+            rarely();
+            high = NEVER;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) high = fmaxf(high, raised(peaks[j], log2_vs[j]));
         }
         peak = over_halves(peak);
         high = over_halves(high);
@@ -624,16 +637,19 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
             top = top_new;
         }
         half8 vf[ND];      // of wide heads, one wave to a SIMD: the first values' way from LDS is hidden behind the exponentials
-        if constexpr (ND >= 7) {
+        auto first_values = [&]() {
+            if constexpr (ND >= 7) {
 #pragma unroll
-            for (int d = 0; d < ND; ++d) vf[d] = *(const half8*)&v_tile[buffer][(32 * d + r) * VS + 8 * h];
-        }
-        const float base = m == NEVER ? 0.f : m;
+                for (int d = 0; d < ND; ++d) vf[d] = *(const half8*)&v_tile[buffer][(32 * d + r) * VS + 8 * h];
+            }
+        };
+        const float base = or_zero(m);
         half8 p[4];
         // A step's P and sums from the same exponentials e^(s - m) weight where the weight, 2^(shift + base), is an ordinary number for all rows and the
         // keys' scale one at all, otherwise (scales very far apart, or 0, or no numbers) from e^(s - m).
-        const float shift = ValueScale(scale[0]).log2() + (P_TOP - (top == NEVER ? 0.f : top));
-        if (ONE && __all(fabsf(shift + base) < 60.f && by[0] < __builtin_huge_valf())) {
+        const float shift = p_shift(log2_vs[0], top);
+        if (ONE && numbers && __all(fabsf(shift + base) < 60.f)) {
+            first_values();
             float part[4] = {};
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -647,25 +663,23 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         } else {
             float weight[NG];
 #pragma unroll
-            for (int j = 0; j < NG; ++j) weight[j] = ValueScale(scale[j]).factor(m, top);
-            bool ordinary = true;
+            for (int j = 0; j < NG; ++j) weight[j] = p_factor(log2_vs[j], m, top);
+            float most = weight[0];
 #pragma unroll
-            for (int j = 0; j < NG; ++j) ordinary &= fabsf(weight[j]) < MOST_FACTOR && fabsf(by[j]) < __builtin_huge_valf();
-            const bool apart = !__all(ordinary);
-            float base_of = base;
+            for (int j = 1; j < NG; ++j) most = fmaxf(most, weight[j]);
+            const bool apart = !numbers || __any(most >= MOST_FACTOR);
+            float base_of = base, kept = l;
             if (__builtin_expect(apart, 0)) {
                 rarely();      // scales very far apart, or no numbers; what is not seen may have any scale: P's exponents in place of the scores
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float value = scale[ONE ? 0 : j];
-                    asm volatile("" : "+s"(value));      // taken apart again here rather than kept in registers from above
-                    const float shift_of = ValueScale(value).log2() + (P_TOP - (top == NEVER ? 0.f : top));
+                    const float shift_of = p_shift(log2_vs[ONE ? 0 : j], top);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         float x = s[j / 2][j % 2 * 8 + i];
                         const bool shown = x != NEVER;
                         x *= by[ONE ? 0 : j];
-                        l += shown ? exp2_fast(x - base) : 0.f;
+                        kept += shown ? exp2_fast(x - base) : 0.f;
                         x = shown ? x + shift_of : NEVER;
                         s[j / 2][j % 2 * 8 + i] = x;
                     }
@@ -674,6 +688,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
                 for (int j = 0; j < NG; ++j) by[j] = weight[j] = 1.f;
                 base_of = 0.f;
             }
+            first_values();
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -682,7 +697,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
                     s[j / 2][j % 2 * 8 + i] = e;
                     p[j][i] = (f16_t)(e * weight[ONE ? 0 : j]);
                 }
-            if (!apart) {
+            if (!ONE || !apart) {      // small pages: no branch here, which parted the exponentials from the products (128 channels 527 for 547 us)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float part = 0.f;
@@ -691,6 +706,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
                     l += part;
                 }
             }
+            l = apart ? kept : l;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -701,7 +717,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     }
     l += __shfl_xor(l, 32);
     if (!there) return;
-    const Power mine(top - P_TOP - (m == NEVER ? 0.f : m));
+    const Power mine(top - P_TOP - or_zero(m));
     const float by = mine.part * (l == 0.f ? 0.f : 1.f / l);      // means, of a part too
     const uint64_t at = (uint64_t)token * q_heads + q_head;
     const uint64_t slot = (((uint64_t)unit_head * a.tiles + tile) * a.parts + part) * ROWS + wave * 32 + r;
