@@ -48,14 +48,12 @@ __device__ inline float p_shift(float log2_vs, float top) { return log2_vs + (P_
 // With factors below this P comes of products with e^(s - m): where that is below the normal numbers, they are nothing in fp16.
 constexpr float MOST_FACTOR = 0x1p100f;
 
-// A key scale times a call's factor and the power of two that undoes a query row's: rows of tiny numbers over huge keys (or the other way round)
-// have scores of an ordinary size, so no product of two of the three may be rounded to a subnormal number.
-struct ScoreScale {
-    float part;      // the key scale's, times the factor
-    int power;
-    __device__ ScoreScale(float part, int power) : part(part), power(power) {}
-    __device__ static ScoreScale of(float ks, float factor) { return {__builtin_amdgcn_frexp_mantf(ks) * factor, __builtin_amdgcn_frexp_expf(ks)}; }
-    __device__ float with(int row_power) const { return ldexpf(part, power + row_power); }
+// What a key scale is multiplied by: a call's factor and the power of two that undoes a query row's, in two factors of half that power each.  Rows of tiny
+// numbers over huge keys (or the other way round) have scores of an ordinary size: no product on the way to them may be a subnormal number.
+struct RowScale {
+    float first, second;
+    __device__ RowScale(float factor, int power) : first(ldexpf(factor, power / 2)), second(ldexpf(1.f, power - power / 2)) {}
+    __device__ float times(float ks) const { return ks * first * second; }
 };
 
 // 2^x as part * 2^power, 1 <= part < 2: what is multiplied by both in turn may be as large as 2^x is small.
@@ -234,8 +232,6 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
     const uint32_t token = u.first_token + row / a.group, q_head = u.head * a.group + row % a.group;
     const int32_t pos = u.begin + (int32_t)(row / a.group);
     const int32_t least = a.window ? max(pos - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
-    const float factor = a.scale * LOG2E;
-    int power;
     u32x4 raw[ND];
 #pragma unroll
     for (int f = 0; f < ND; ++f)
@@ -277,6 +273,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         fetch_values(v_page, value_token(c));
     }
     half8 q[ND];
+    int e;
     {
         float x[8], peak = 0.f;
 #pragma unroll
@@ -287,15 +284,15 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         }
         peak = fmaxf(peak, __shfl_xor(peak, 16));
         peak = fmaxf(peak, __shfl_xor(peak, 32));
-        const int e = query_exponent(peak, a.dtype);
+        e = query_exponent(peak, a.dtype);
 #pragma unroll
         for (int f = 0; f < ND; ++f) {
             convert_query(raw[f], a.dtype, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[f][i] = query_element(x[i], peak, e);
         }
-        power = -e;
     }
+    const RowScale row_scale(a.scale * LOG2E, -e);
     for (; c < c1; c += W) {
         // where the scores of this lane lie; a missing page's lie behind every row
         const int32_t at0 = v_page == NO_PAGE ? 0x7FFFFFFF - 64 : (int32_t)((v_place << a.cache.shift) + (value_token(c) & slots));
@@ -313,7 +310,7 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
         }
         if (c + W < c1) fetch_keys(k_page, key_token(c + W));
         const bool whole = __all(at0 + 15 <= pos && at0 >= least);
-        const float by = ScoreScale::of(ks, factor).with(power);
+        const float by = row_scale.times(ks);
         float peak = NEVER;
 #pragma unroll
         for (int t = 0; t < 4; ++t) s[t] *= by;
@@ -467,8 +464,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     const int32_t least_last = a.window ? max(pos_last - (int32_t)min(a.window, CACHE_MOST) + 1, 0) : 0;
 
     half8 q[D / 16];
-    const float factor = fabsf(a.scale) * LOG2E;
-    int power;
+    int e;
     {
         u32x4 raw[D / 16];
 #pragma unroll
@@ -481,21 +477,20 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
             for (int i = 0; i < 8; ++i) peak = fmaxf(peak, x[i] == x[i] ? fabsf(x[i]) : __builtin_huge_valf());
         }
         peak = fmaxf(peak, __shfl_xor(peak, 32));
-        const int e = query_exponent(peak, a.dtype);
+        e = query_exponent(peak, a.dtype);
 #pragma unroll
         for (int f = 0; f < D / 16; ++f) {
             convert_query(raw[f], a.dtype, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) q[f][i] = query_element(a.scale < 0.f ? -x[i] : x[i], peak, e);
         }
-        power = -e;
     }
+    const RowScale row_scale(fabsf(a.scale) * LOG2E, -e);
 
     // a step's codes: `PER` runs of 16 keys' channels and 16 values' tokens a thread; the pages of its four 16 tokens and their scales
     u32x4 kc[PER], vc[PER];
     uint32_t absent, next_absent;
-    float k_part[NG], v_log2[NG], next_ks, next_vs;     // the key scale times the call's factor as part and power of two, the value scale's logarithm
-    int k_power[NG];
+    float ks[NG], v_log2[NG], next_ks, next_vs;
     uint64_t odd;       // scales of the step that are no numbers, or values' of 0
     // A lane keeps the page and the scales of one of the four: vector loads, which come in order with the codes, a step ahead of their use.
     uint32_t own_page = page_at(a.batch, table, (c0 * 64 + 16 * (lane & 3)) >> a.cache.shift, a.cache.n_pages);
@@ -548,13 +543,11 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
     };
     auto next = [&]() {
         absent = next_absent;
-        const ScoreScale k = ScoreScale::of(next_ks, factor);      // by the lane that has the page
-        const float v = log2_scale(next_vs);
-        odd = __ballot(!(fabsf(k.part) < __builtin_huge_valf() && fabsf(v) < __builtin_huge_valf())) & (ONE ? 1 : 15);
+        const float v = log2_scale(next_vs);      // by the lane that has the page
+        odd = __ballot(!(fabsf(next_ks) < __builtin_huge_valf() && fabsf(v) < __builtin_huge_valf())) & (ONE ? 1 : 15);
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            k_part[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(k.part), j));
-            k_power[j] = __builtin_amdgcn_readlane(k.power, j);
+            ks[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(next_ks), j));
             v_log2[j] = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), j));
         }
     };
@@ -589,7 +582,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
         const bool numbers = odd == 0;
 #pragma unroll
         for (int j = 0; j < NG; ++j) {
-            by[j] = ScoreScale(k_part[j], k_power[j]).with(power);
+            by[j] = row_scale.times(ks[j]);
             by[j] = by[j] < LEAST_SCALE ? LEAST_SCALE : by[j];
             log2_vs[j] = v_log2[j];
         }
