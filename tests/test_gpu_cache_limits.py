@@ -128,3 +128,20 @@ def test_compaction_past_32_bit_offsets(ix):
         for name in NAMES:
             assert torch.equal(big[name][moved[p]].cpu(), small[name][s]), (p, name)
     assert torch.equal(numbers.cpu(), want_numbers) and torch.equal(refs.cpu(), want_refs)
+
+
+def test_compaction_of_many_layers(ix):
+    """More layers than a launch takes; tables and counts are changed once."""
+    L, pages = 70, 9
+    c = plain.make_cache(pages, 1, 16, 32, 1, layers=L)
+    tables, lengths = torch.tensor([[8, 2, 5], [5, -1, -1]], dtype=torch.int32), [40, 9]
+    refs = torch.zeros(pages, dtype=torch.int32)
+    refs[[8, 2, 5]] = torch.tensor([1, 1, 2], dtype=torch.int32)
+    g = {k: v.to(DEV) for k, v in c.items()}
+    g_refs, g_tables = refs.to(DEV), tables.to(DEV)
+    numbers, live = dz.cache_compact(ix, [dz.cache(ix, *(g[n][i] for n in NAMES)) for i in range(L)], g_refs, g_tables,
+                                     torch.tensor(lengths, dtype=torch.int32, device=DEV))
+    want, n = plain.compact(c, refs, tables, lengths)
+    assert live.tolist() == [n] and torch.equal(numbers.cpu(), want) and torch.equal(g_refs.cpu(), refs) and torch.equal(g_tables.cpu(), tables)
+    for name in NAMES:
+        assert torch.equal(g[name].cpu(), c[name]), name
