@@ -447,7 +447,7 @@ dessert_status_t dessert_head_logprobs(const dessert_index_t *index, const int8_
  *   dim           of a head: a multiple of 32, at most 256
  *   k_codes_dev   dev, 16-byte aligned, [n_pages][n_heads][page_tokens][dim]
  *   v_codes_dev   dev, 16-byte aligned, [n_pages][n_heads][dim][page_tokens]: a channel's tokens side by side
- *   k_scales_dev, v_scales_dev   dev, [n_pages][n_heads], not negative
+ *   k_scales_dev, v_scales_dev   dev, [n_pages][n_heads], not negative, of any size
  *   bounds_dev    dev, 16-byte aligned, [n_pages][n_heads][2][dim]: the smallest and the largest key code of a channel, or
  *                 NULL without dessert_cache_select */
 typedef struct {
@@ -463,8 +463,10 @@ typedef struct {
  *   starts_dev    dev, [n_seqs + 1]: the new tokens of sequence b are rows starts[b] .. starts[b + 1] of the arrays of tokens,
  *                 in order (there may be none); or NULL: one new token each, row b
  *   n_tokens      rows of the arrays of tokens; those from starts[n_seqs] on are neither read nor written
- *   max_tokens    at least the largest number of new tokens of a sequence: further ones, at its end, are left out
- *   max_length    about the largest length: how work is divided goes by it, results do not depend on it but for rounding */
+ *   max_tokens    at least the largest number of new tokens of a sequence, at most n_tokens: further ones, at its end, are left out
+ *   max_length    about the largest length: how work is divided goes by it, results do not depend on it but for rounding.
+ * Attention's work is divided by one rule for all sequences of a call: one long sequence among short ones, or a prompt beside single
+ * tokens, is done sooner in a call of its own. */
 typedef struct {
     const uint32_t *tables_dev, *lengths_dev, *starts_dev;
     uint32_t n_seqs, table_pages, n_tokens, max_tokens, max_length;
@@ -524,7 +526,8 @@ dessert_status_t dessert_cache_select(const dessert_index_t *index, const desser
  * holders is copied first, in all layers; where all holders are sequences that write to it, the first of them keeps it.  Pages
  * are taken from the free ones, lowest first, in the order of the sequences.  A sequence that the free pages (counted before
  * anything is taken) do not reach any more, or that does not fit the table, gets none: it stays as it was, its length without
- * add[b]; so does one whose last page is still shared by such a sequence.
+ * add[b]; so does one whose last page is still shared by such a sequence.  What stands in a table behind a sequence's length is not
+ * looked at: who shortens a sequence by whole pages takes them from refs, too.
  *   layers          host, [n_layers]: caches of the same sizes; pages are copied in all of them
  *   refs_dev        dev, in and out, [n_pages]
  *   tables_dev, lengths_dev   dev, [n_seqs][table_pages], [n_seqs] of the old sequences

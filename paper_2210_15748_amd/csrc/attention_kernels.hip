@@ -4,8 +4,8 @@
 // in one pass over the keys with a running m.  All products go to the matrix cores in fp16, which holds codes exactly; queries of bf16 are
 // first scaled by a power of two a row, which makes their 8 bits exact in fp16 (but for parts below 2^-37 of the row's largest).
 // e^s v_scale is rounded to fp16 (off by at most 2^-11 of itself: the rounding of an fp16 result), 2^12 being the largest of a row so far, which
-// keeps all down to 2^-26 of the largest a normal number however far apart the scales of pages are; sums, maxima and the outputs are held
-// in 32 bits.  Below, exponents are in powers of two: m the largest s log2(e), top the largest s log2(e) + log2(v_scale).
+// keeps all down to 2^-26 of the largest a normal number however far apart the scales of pages are and of whatever size; sums, maxima and
+// the outputs, means of the values from the first division on, are held in 32 bits.  Below, exponents are in powers of two: m the largest s log2(e), top the largest s log2(e) + log2(v_scale).
 // Scores are formed as K Q^T: a lane then holds consecutive tokens of one row, and these are what it has to give as its part of P for
 // O^T = V^T P^T, so P goes from one product to the next in registers.
 #include "cache_common.hpp"
@@ -205,8 +205,8 @@ __device__ inline uint32_t page_of(const AttendArgs& a, const uint32_t* table, c
 // ---- few rows: 16 to a workgroup, each of its W waves takes every W-th step of 64 tokens --------------------------------------
 // Keys and values come from memory straight into the layout of the products: a lane reads 16 bytes of a key (or of a value channel's
 // 16 tokens), converts them, and no LDS is used before the waves' results are joined.  Bound by memory: one token over 131072 of 8 heads of
-// 128 channels (268 MB) 51 us, 5.2 TB/s, and 6 for the join; 64 sequences up to 4096 in pages of 16 (340 MB) 73 us, 4.7 TB/s; 4 sequences up to 500 of
-// 64 channels 6.3 us.  Two waves to a SIMD with all registers they ask for: with three the spilled ones cost a third.
+// 128 channels (268 MB) 52 us, 5.2 TB/s, and 6.5 for the join; 64 sequences up to 4096 in pages of 16 (340 MB) 73 us, 4.7 TB/s; 4 sequences up to 500 of
+// 64 channels 6.5 us.  Two waves to a SIMD with all registers they ask for: with three the spilled ones cost a third.
 template <int ND, int W, bool LISTS>
 __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(AttendArgs a) {
     constexpr int D = ND * 32, NV = D / 16;
@@ -422,8 +422,8 @@ __global__ __launch_bounds__(64 * W, ND <= 5 ? 2 : 1) void attend_few_kernel(Att
 // ---- many rows: 128 or 256 to a workgroup, 32 to a wave, all over the same steps of 64 tokens ---------------------------------------
 // Keys and values are converted once for the workgroup's waves on their way into LDS, two steps' worth of it: while one is computed
 // with, the next one's codes are under way from memory.  Rows in LDS are 16 bytes apart from a multiple of their length: a wave's 16-byte
-// reads then spread over all banks.  3584 tokens of 32 heads of 128 channels over up to 8192 (350 GFLOP): 436 to 500 us by card, 700 to 800 TFLOP/s; matrix cores
-// 31 % busy, vector ALU 48 % (32 exponentials a lane and step, the codes' conversion), mostly one after the other.
+// reads then spread over all banks.  3584 tokens of 32 heads of 128 channels over up to 8192 (350 GFLOP): 430 to 500 us by card, 700 to 815 TFLOP/s; matrix cores
+// 31 % busy, vector ALU 47 % (32 exponentials a lane and step, the codes' conversion), mostly one after the other.
 // ONE: a step lies on one page (of 64 tokens or more), so its page and scales are the same for all.
 template <int ND, int W, bool ONE>
 __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many_kernel(AttendArgs a) {
@@ -733,7 +733,7 @@ __global__ __launch_bounds__(64 * W, W == 8 || ND <= 4 ? 2 : 1) void attend_many
 
 // ---- the parts of the keys' axis joined: a workgroup a row ---------------------------------------------------------------------
 // First the parts' factors, a thread a part, then their outputs, the parts spread over groups of lanes that hold 4 channels each.  Latency: 64 parts of 32
-// rows 6.3 us (47 when every thread went through all the sums).
+// rows 6.5 us (47 when every thread went through all the sums).
 constexpr uint32_t MOST_PARTS = ATTEND_MOST_GROUPS;
 
 __device__ inline float over_workgroup(float x, bool max, float* parts) {

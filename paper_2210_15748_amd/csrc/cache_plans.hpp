@@ -21,7 +21,7 @@ constexpr uint32_t ATTEND_CHUNK = 64;
 // Rows (query heads of one key head and the new tokens they belong to) of a workgroup, for few rows and for many.
 constexpr uint32_t ATTEND_FEW = 16, ATTEND_MANY = 128;
 // Up to so many rows of a unit the form for few takes, 16 at a time.  (16 sequences up to 8192, 8 heads of dim 128, us with the one for many / for few:
-// 32 rows 96 / 76, 48 rows 111 / 98, 64 rows 110 / 112; 32 sequences up to 1000 of dim 64: 32 rows 29 / 14, 64 rows 36 / 24.)
+// 32 rows 98 / 78, 48 rows 111 / 101, 64 rows 113 / 110; 32 sequences up to 1000 of dim 64: 32 rows 28 / 15, 64 rows 36 / 20.)
 constexpr uint32_t ATTEND_FEW_ROWS = 64;
 // Workgroups that a call is split into along the keys where it has fewer: as many as the chip holds at once (its registers decide), so that
 // none begins when others end.
@@ -56,8 +56,8 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
     const uint64_t rows = lists ? group : max_tokens * group;
     p.few = lists || rows <= ATTEND_FEW_ROWS;
     p.rows = p.few ? ATTEND_FEW : ATTEND_MANY;
-    // (3584 tokens of 32 heads over up to 8192, in us with 128 / 256 rows to a workgroup: 324 / 373 at dim 32, 357 / 391 at 64, 442 / 432 at 96,
-    // 497 / 479 at 128, 852 / 601 at 160, 1068 / 840 at 192, 1350 / 1622 at 256: there the registers of half as many waves are too few)
+    // (3584 tokens of 32 heads over up to 8192, in us with 128 / 256 rows to a workgroup: 293 / 351 at dim 32, 332 / 382 at 64, 435 / 421 at 96,
+    // 484 / 474 at 128, 813 / 564 at 160, 1004 / 684 at 192, 1204 / 2405 at 256: there the registers of half as many waves are too few)
     if (!p.few && dim >= 128 && dim <= 192 && seqs * heads * divided_up(rows, 2 * ATTEND_MANY) >= 256) p.rows = 2 * ATTEND_MANY;
     p.tiles = (uint32_t)std::max<uint64_t>(1, divided_up(rows, p.rows));
     p.units = (uint32_t)(lists ? seqs * max_tokens : seqs);
@@ -67,8 +67,8 @@ inline AttendPlan attend_plan(uint64_t seqs, uint64_t max_tokens, uint32_t heads
     p.waves = p.few ? 4 : p.rows / 32;
     // a part has work for the four waves of a workgroup (one step each) or, of many rows, for a few steps
     uint64_t parts = std::min(std::max<uint64_t>(1, target / std::max<uint64_t>(1, p.groups)), divided_up(chunks, 4));
-    // up to 16 steps are done by one workgroup of eight waves rather than split and joined (16 sequences up to 1000 of dim 128: 14.1 us, split 16.0; up
-    // to 700 11.8 and 15.1; of wider heads its waves have too few registers)
+    // up to 16 steps are done by one workgroup of eight waves rather than split and joined (16 sequences up to 1000 of dim 128: 14.8 us, split 16.1; up
+    // to 700 12.3 and 15.2; of wider heads its waves have too few registers)
     if (p.few && parts > 1 && chunks <= 16 && dim <= 160) {
         p.waves = 8;
         parts = 1;
