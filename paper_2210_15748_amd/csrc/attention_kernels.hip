@@ -5,7 +5,8 @@
 // first scaled by a power of two a row, which makes their 8 bits exact in fp16 (but for parts below 2^-37 of the row's largest).
 // e^s v_scale is rounded to fp16 (off by at most 2^-11 of itself: the rounding of an fp16 result), 2^12 being the largest of a row so far, which
 // keeps all down to 2^-26 of the largest a normal number however far apart the scales of pages are and of whatever size; sums, maxima and
-// the outputs, means of the values from the first division on, are held in 32 bits.  Below, exponents are in powers of two: m the largest s log2(e), top the largest s log2(e) + log2(v_scale).
+// the outputs, means from the first division on, are held in 32 bits.  Below, exponents are in powers of two: m the largest s log2(e), top
+// the largest s log2(e) + log2(v_scale).
 // Scores are formed as K Q^T: a lane then holds consecutive tokens of one row, and these are what it has to give as its part of P for
 // O^T = V^T P^T, so P goes from one product to the next in registers.
 #include "cache_common.hpp"
@@ -56,7 +57,7 @@ struct RowScale {
     __device__ float times(float ks) const { return ks * first * second; }
 };
 
-// 2^x as part * 2^power, 1 <= part < 2: what is multiplied by both in turn may be as large as 2^x is small.
+// 2^x as part * 2^power, 1/2 <= part < 1: what is multiplied by both in turn may be as large as 2^x is small.
 struct Power {
     float part;
     int power;
@@ -64,11 +65,12 @@ struct Power {
     __device__ Power(float part, int power) : part(part), power(power) {}
     __device__ explicit Power(float x) {
         x = fmaxf(x, -1000.f);
-        const float n = floorf(x);
+        const float n = floorf(x) + 1.f;
         part = exp2_fast(x - n);
         power = (int)n;
     }
     __device__ float as_float() const { return ldexpf(part, power); }
+    __device__ Power times(float w) const { return {part * __builtin_amdgcn_frexp_mantf(w), power + __builtin_amdgcn_frexp_expf(w)}; }
 };
 
 __device__ inline f32x4 times(f32x4 x, const Power& p) {
@@ -765,8 +767,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
     m = over_workgroup(m, true, most4);
     for (uint32_t i = threadIdx.x; i < parts; i += 256) {
         const float2 s = a.part_sums[slot0 + (uint64_t)i * rows];
-        Power f(s.x == m ? 0.f : s.x - m);
-        f.part *= s.y;
+        const Power f = Power(s.x == m ? 0.f : s.x - m).times(s.y);
         factors[i] = f;
         l += f.as_float();
     }
@@ -778,7 +779,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, uint32_t
         const float* from = a.part_out + slot0 * D + d;
         const uint64_t apart = (uint64_t)rows * D;
 #pragma unroll 4
-        for (uint32_t i = part0; i < parts; i += lanes) x += times(*(const f32x4*)(from + i * apart), Power{factors[i].part * by, factors[i].power});
+        for (uint32_t i = part0; i < parts; i += lanes) x += times(*(const f32x4*)(from + i * apart), factors[i].times(by));
     }
     joined[threadIdx.x] = x;
     barrier();
@@ -809,13 +810,12 @@ __global__ __launch_bounds__(256) void attend_join_few_kernel(AttendArgs a, uint
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
     m = __shfl(m, 0);
-    Power f(s.x == m ? 0.f : s.x - m);
-    f.part *= s.y;
+    Power f = Power(s.x == m ? 0.f : s.x - m).times(s.y);
     float l = f.as_float();
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) l += __shfl_xor(l, o);
     l = __shfl(l, 0);
-    f.part *= l == 0.f ? 0.f : 1.f / l;
+    f = f.times(l == 0.f ? 0.f : 1.f / l);
     // of heads of up to 128 channels each half of the wave sees to every other part
     const uint32_t halves = per <= 32 ? 2 : 1, half = halves == 2 ? lane >> 5 : 0, at4 = halves == 2 ? lane & 31 : lane;
     f32x4 x = {};

@@ -105,3 +105,22 @@ def test_queries_and_key_scales_of_opposite_sizes(ix, form, page, q_power, k_pow
     q = torch.ldexp(torch.randn(sum(new), group, 64, generator=torch.Generator().manual_seed(5)), torch.tensor(q_power)).to(torch.bfloat16)
     assert torch.isfinite(q).all()
     check(ix, c, lengths, new, group, page, q=q)
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("depth", [-20, -60])
+def test_few_keys_of_all_the_weight_among_many_large_values(ix, form, page, depth):
+    """One page with the weight of a row; parts of the other keys' axis whose sums are many times its, and whose values are near the largest number."""
+    lengths, new, group = FORMS[form]
+    c = pool(lengths, page, 64)
+    tables = plain.make_tables(lengths, page, c["k"].shape[0], 3)
+    first = tables[:, 0].long()
+    c["k"][:] = -127
+    c["k"][first] = 0
+    c["ks"][:] = -depth * math.log(2.0) / (127 * 64 * 0.125)
+    c["vs"] = torch.ldexp(c["vs"] / 0.022, torch.tensor(120))
+    c["vs"][first] *= 2.0 ** -110
+    c["v"] = torch.full_like(c["v"], 127)
+    q = torch.ones(sum(new), group, 64, dtype=torch.bfloat16)
+    check(ix, c, lengths, new, group, page, q=q)
