@@ -705,7 +705,8 @@ def cache_batch(ix: Index, tables: torch.Tensor, lengths: torch.Tensor, starts: 
                 n_tokens: Optional[int] = None, max_tokens: Optional[int] = None, max_length: Optional[int] = None) -> CacheBatch:
     """dessert_cache_batch_t: tables [seqs, table pages] and lengths [seqs] int32 / uint32 (-1: no page), starts [seqs + 1] or None (one new token
     each).  With starts, n_tokens (rows of the arrays of tokens) is needed; max_tokens (new tokens of a sequence, at most)
-    is taken to be that where it is not given, max_length (which decides how work is divided) what the tables hold."""
+    is taken to be that where it is not given (the form of attention goes by it: a few
+    tokens each are done sooner where it says so), max_length (which decides how work is divided) what the tables hold."""
     t_ptr = _kept(ix, tables, (None, None), "tables", _TOKEN_TYPES)
     n, width = tables.shape
     l_ptr = _kept(ix, lengths, (n,), "lengths", _TOKEN_TYPES)
